@@ -38,6 +38,7 @@
 #ifndef AQMB_H
 #define AQMB_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -55,7 +56,9 @@ typedef enum {
   AQMB_EHIP = 4           /* a HIP runtime call or kernel launch failed; see aqmb_last_error() */
 } aqmb_status;
 
-typedef enum { AQMB_F16 = 0, AQMB_BF16 = 1, AQMB_F32 = 2 } aqmb_dtype;
+/* AQMB_F8: OCP e4m3 (largest value 448, no infinities); AQMB_I8: signed 8-bit integers. Both are taken
+ * only by the operators between the layers (aqmb_rms_norm and below), always with scales. */
+typedef enum { AQMB_F16 = 0, AQMB_BF16 = 1, AQMB_F32 = 2, AQMB_F8 = 3, AQMB_I8 = 4 } aqmb_dtype;
 
 typedef struct {
   int32_t d_out;          /* output rows of W, >= 1 */
@@ -362,6 +365,211 @@ aqmb_status aqmb_beam_search_weighted(const aqmb_desc* desc, int k, int beam, co
  * needs it. Returns a negative value for a null or invalid descriptor or k outside [1, M].
  */
 double aqmb_bits_per_weight(const aqmb_desc* desc, int k);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The operators between the layers of a decode step: the norm that feeds a projection, the product
+ * with plain 4-bit weights (for the layers of a model that are not additively coded), attention of
+ * one new token over a paged key-value cache, and the cache's upkeep. The conventions above hold,
+ * except that data pointers need only the alignment of their elements and rows may be strided
+ * (strides in elements, the last dimension dense). Sums, softmax statistics and scales are held in
+ * binary32. Nothing here allocates device memory except aqmb_w4_create.
+ */
+
+/*
+ * Root-mean-square norm of each row with the residual's addition:
+ *   h = x + residual (binary32; h = x without a residual), residual_out = h rounded to `dtype`,
+ *   v_t = h_t * (1 / sqrt(mean(h^2) + eps)) * (weight_t + weight_offset)
+ * and y = v rounded once (nearest even) for y_dtype F16, BF16 or F32; or, for y_dtype F8 or I8, per
+ * group of `scale_group` columns (0: the whole row; the last group of a row may be shorter):
+ *   a = max(max |v|, 2^-100), y = round(v * (L / a)) to nearest even, scale = a / L,
+ *   L = 448 for F8, 127 for I8
+ * so that y * scale stands for v. A group that holds a value that is not finite gets the scale NaN
+ * and y = 0. h is not rounded before it is squared or scaled; a row whose squares overflow binary32
+ * gives zeros, as the formula does.
+ *   x        [rows][cols], `dtype` in {F16, BF16}, row stride x_stride
+ *   residual, residual_out  [rows][cols] `dtype`, row stride residual_stride: both or neither given
+ *   weight   [cols] `dtype`
+ *   y        [rows][cols] y_dtype, row stride y_stride
+ *   scales   [rows][ceil(cols / scale_group)] fp32, dense; NULL unless y_dtype is F8 or I8
+ * y may be x and residual_out may be residual or x (same strides); no other overlap.
+ * 1 <= cols <= AQMB_MAX_NORM_COLS; scale_group 0, 32, 64 or 128.
+ * Errors: EINVAL (null or misaligned pointer, rows or cols < 1, a stride below cols, one residual
+ * pointer without the other, scales missing or not wanted, negative or NaN eps), EUNSUPPORTED
+ * (dtype, cols above the limit, scale_group), EHIP.
+ */
+#define AQMB_MAX_NORM_COLS 32768
+aqmb_status aqmb_rms_norm(const void* x, aqmb_dtype dtype, int64_t x_stride, const void* residual,
+                          void* residual_out, int64_t residual_stride, const void* weight, float weight_offset,
+                          float eps, int rows, int cols, void* y, aqmb_dtype y_dtype, int64_t y_stride,
+                          float* scales, int scale_group, aqmb_stream_t stream);
+
+/*
+ * Layers of 4-bit integers with a scale (and, optionally, a zero point) for every group of
+ * group_size consecutive weights of a row:
+ *   W[i][t] = scales[i][t / group_size] * (q[i][t] - zeros[i][t / group_size])
+ *   weights  [d_out][ceil(d_in / 2)] uint8: q[i][t] is the low nibble of byte t / 2 for even t, the
+ *            high nibble for odd t (an odd row's last high nibble is ignored)
+ *   scales   [d_out][ceil(d_in / group_size)] fp16 bit patterns
+ *   zeros    the same shape, uint8; NULL: 8 everywhere (symmetric quantization)
+ * d_in need not be a multiple of the group size. The library copies everything into device memory
+ * it owns, re-tiled for the matrix cores; aqmb_w4_create is synchronous (the caller may free its
+ * buffers afterwards). A layer is read-only after creation.
+ * Errors: EINVAL (null pointer, sizes < 1, d_out * d_in >= 2^32), EUNSUPPORTED (group_size other
+ * than 32, 64, 128), ENOMEM, EHIP; on error *out is NULL. aqmb_w4_destroy waits for the device;
+ * NULL is a no-op, EINVAL for a handle that is not a live layer.
+ */
+typedef struct aqmb_w4_s* aqmb_w4_t;
+typedef struct {
+  int32_t d_out;
+  int32_t d_in;
+  int32_t group_size;     /* 32, 64 or 128 */
+} aqmb_w4_desc;
+aqmb_status aqmb_w4_create(aqmb_w4_t* out, const aqmb_w4_desc* desc, const uint8_t* weights,
+                           const uint16_t* scales, const uint8_t* zeros, aqmb_stream_t stream);
+aqmb_status aqmb_w4_destroy(aqmb_w4_t layer);
+aqmb_status aqmb_w4_get_desc(aqmb_w4_t layer, aqmb_w4_desc* out);
+
+/*
+ * Decode product with such a layer, y[b][i] = sum_t X[b][t] W[i][t] for b < batch, where
+ * X = x for x_dtype F16 or BF16, and X[b][t] = x[b][t] * x_scales[b][t / x_scale_group] for F8 and
+ * I8 (what aqmb_rms_norm writes; x_scale_group 0: one scale for each row). Within a group the
+ * products q * x and the sum of x (for the zero point) are formed on the matrix cores: exact
+ * products, sums in binary32 (I8: exact in int32); the groups are scaled and added in binary32, in
+ * a fixed order; one rounding to y_dtype in {F16, BF16, F32}. An x that is not finite makes all of
+ * its row's outputs not finite.
+ *   x  [batch][d_in], row stride x_stride; y [batch][d_out], row stride y_stride
+ * 1 <= batch <= AQMB_MAX_BATCH.
+ * Errors: EINVAL (bad handle, null or misaligned pointer, batch < 1, a stride below the row,
+ * x_scales missing or not wanted, layer on another device), EUNSUPPORTED (batch > AQMB_MAX_BATCH,
+ * dtype, x_scale_group other than 0 and the layer's group size), EHIP.
+ */
+aqmb_status aqmb_w4_gemv(aqmb_w4_t layer, const void* x, aqmb_dtype x_dtype, int64_t x_stride,
+                         const float* x_scales, int x_scale_group, int batch, void* y, aqmb_dtype y_dtype,
+                         int64_t y_stride, aqmb_stream_t stream);
+
+/*
+ * A paged key-value cache of one attention layer: n_pages pages of page_size token slots. The
+ * caller owns the memory; this struct only describes it.
+ *   k, v     page p starts at element p * page_stride; inside a page, dense,
+ *            AQMB_KV_HEAD_MAJOR [n_kv_heads][page_size][head_dim] or
+ *            AQMB_KV_SLOT_MAJOR [page_size][n_kv_heads][head_dim]
+ *   dtype    F16, BF16, or F8 with one scale for every token and head:
+ *   k_scale, v_scale  fp32, dense, [n_pages][n_kv_heads][page_size] or
+ *            [n_pages][page_size][n_kv_heads] as the layout; NULL unless dtype is F8
+ * head_dim: a multiple of 8 up to 256; page_size 1..32768; page_stride >= n_kv_heads * page_size *
+ * head_dim and a multiple of 8; k and v 16-byte aligned (8-byte for F8).
+ */
+typedef enum { AQMB_KV_HEAD_MAJOR = 0, AQMB_KV_SLOT_MAJOR = 1 } aqmb_kv_layout;
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t page_stride;
+  int32_t dtype;          /* aqmb_dtype */
+  int32_t layout;         /* aqmb_kv_layout */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} aqmb_kv_cache;
+
+/*
+ * Attention of one new token per sequence over the cache: for every sequence s and head h,
+ *   score_t = scale * <q[s][h], K_t>, out[s][h] = sum_t softmax(score)_t V_t, over the positions
+ *   t < lengths[s], and t >= lengths[s] - window where window > 0
+ * with K_t, V_t of head h / (n_heads / n_kv_heads) in slot t % page_size of page
+ * page_table[s][t / page_size]. A sequence with no position gives out = 0 and lse = -infinity.
+ * lse (may be NULL): the logarithm of the softmax's denominator, log sum_t exp(score_t), fp32
+ * [n_seqs][n_heads], with which results over disjoint parts of a context can be joined.
+ *   q, out      [n_seqs][n_heads][head_dim] F16 or BF16 (`dtype`; the cache's own type, or any of
+ *               the two with an F8 cache), stride between sequences q_stride / out_stride, each a
+ *               multiple of 8; 16-byte aligned
+ *   page_table  int32, row s at s * table_stride; only the entries that positions < lengths[s]
+ *               need are read. A page outside [0, n_pages) is skipped: its positions do not exist.
+ *   lengths     int32 [n_seqs], device memory; values outside [0, max_length] are clamped
+ *   max_length  an upper bound of the lengths, <= table_stride * page_size: fixes how the work is
+ *               split, so results do not depend on other sequences' lengths
+ * Slots that hold no token may hold anything (NaN included). Scores and softmax are binary32; the
+ * probabilities enter the matrix cores as two 16-bit parts. One rounding to `dtype`.
+ * workspace: aqmb_paged_attention_workspace_bytes bytes of device memory, 16-byte aligned, written
+ * by the call (calls that share one must be ordered); 0 bytes: NULL is fine.
+ * Errors: EINVAL (null or misaligned pointer, sizes < 1, n_heads not a multiple of n_kv_heads,
+ * max_length < 0 or above the table, negative window, workspace too small, scales missing or not
+ * wanted), EUNSUPPORTED (dtype, head_dim, page_size), EHIP.
+ */
+aqmb_status aqmb_paged_attention(const aqmb_kv_cache* cache, const void* q, aqmb_dtype dtype, int64_t q_stride,
+                                 int n_heads, const int32_t* page_table, int64_t table_stride,
+                                 const int32_t* lengths, int n_seqs, int max_length, float scale, int window,
+                                 void* out, int64_t out_stride, float* lse, void* workspace,
+                                 size_t workspace_bytes, aqmb_stream_t stream);
+aqmb_status aqmb_paged_attention_workspace_bytes(const aqmb_kv_cache* cache, int n_heads, int n_seqs,
+                                                 int max_length, int window, size_t* bytes);
+
+/*
+ * Write new tokens into the cache: token i's keys and values go to slot slots[i] % page_size of page
+ * slots[i] / page_size. A slot outside [0, n_pages * page_size) (such as -1 for padding) is skipped;
+ * slots of one call must differ. For an F8 cache each token and head is scaled as aqmb_rms_norm
+ * scales a group (L = 448, its a the largest magnitude of the head's values).
+ *   k, v   [n_tokens][n_kv_heads][head_dim] F16 or BF16 (`dtype`; the cache's own type, or any of
+ *          the two for an F8 cache), stride between tokens k_stride / v_stride
+ *   slots  int64 [n_tokens], device memory
+ * Errors: EINVAL (null or misaligned pointer, n_tokens < 1, stride below a token), EUNSUPPORTED, EHIP.
+ */
+aqmb_status aqmb_kv_append(const aqmb_kv_cache* cache, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, aqmb_dtype dtype, const int64_t* slots, int n_tokens,
+                           aqmb_stream_t stream);
+
+/*
+ * Copy page src[i] to page dst[i], keys, values and scales, in every cache of `caches` (the layers of
+ * a model; all of the same shape and type), in one launch. A pair with a page outside [0, n_pages) is
+ * skipped. No page may be a dst twice, nor a dst of one pair and the src of another.
+ *   src, dst  int32 [n_pairs], device memory
+ * 1 <= n_caches <= AQMB_MAX_CACHES.
+ * Errors: EINVAL (null pointer, n_caches or n_pairs < 1, caches that differ), EUNSUPPORTED
+ * (n_caches above the limit), EHIP.
+ */
+#define AQMB_MAX_CACHES 64
+aqmb_status aqmb_kv_copy_pages(const aqmb_kv_cache* caches, int n_caches, const int32_t* src, const int32_t* dst,
+                               int n_pairs, aqmb_stream_t stream);
+
+/*
+ * Bookkeeping of the pages on the host: which pages each sequence holds, with reference counts.
+ * No call touches the GPU; calls on one pool must not overlap. Sequences are small integers
+ * 0..max_seqs-1, given out lowest first.
+ *   aqmb_pages_add      a new, empty sequence. ENOMEM when max_seqs are live.
+ *   aqmb_pages_fork     a new sequence that shares all pages of `seq`, the last, partly filled one
+ *                       included. ENOMEM as above.
+ *   aqmb_pages_extend   n_tokens more tokens: slots[n_tokens] receives their cache slots (the
+ *                       argument of aqmb_kv_append). Where the first of them falls into a page that
+ *                       another sequence shares, the sequence gets a page of its own and
+ *                       (*copy_src, *copy_dst) say which page to copy before writing, else both
+ *                       are -1. ENOMEM, with nothing changed, when too few pages are free.
+ *   aqmb_pages_free     ends a sequence; pages that no other one shares become free.
+ *   aqmb_pages_compact  moves used pages from the end of the pool into free ones at its start, so
+ *                       that the used pages are 0..used-1: the *n_pairs copies to make are written
+ *                       to src / dst (room for n_pages / 2 each), and every sequence's table is
+ *                       changed already. The copies do not overlap (the argument of
+ *                       aqmb_kv_copy_pages); make them before the next append.
+ *   aqmb_pages_table    the sequence's length and pages: *n_used = ceil(length / page_size) entries
+ *                       go to table (room for `capacity` >= that many; EINVAL otherwise, with *length and
+ *                       *n_used set). table may be NULL with capacity 0 to ask for the sizes only.
+ *   aqmb_pages_counts   pages free, and sequences live. Either pointer may be NULL.
+ * Free pages are given out lowest first. Errors otherwise: EINVAL (bad handle, null pointer, a
+ * sequence that is not live, n_tokens < 0, sizes < 1), ENOMEM (host memory).
+ */
+typedef struct aqmb_pages_s* aqmb_pages_t;
+aqmb_status aqmb_pages_create(aqmb_pages_t* out, int n_pages, int page_size, int max_seqs);
+aqmb_status aqmb_pages_destroy(aqmb_pages_t pool);
+aqmb_status aqmb_pages_add(aqmb_pages_t pool, int* seq);
+aqmb_status aqmb_pages_fork(aqmb_pages_t pool, int seq, int* child);
+aqmb_status aqmb_pages_extend(aqmb_pages_t pool, int seq, int n_tokens, int64_t* slots, int32_t* copy_src,
+                              int32_t* copy_dst);
+aqmb_status aqmb_pages_free(aqmb_pages_t pool, int seq);
+aqmb_status aqmb_pages_compact(aqmb_pages_t pool, int32_t* src, int32_t* dst, int* n_pairs);
+aqmb_status aqmb_pages_table(aqmb_pages_t pool, int seq, int32_t* table, int capacity, int* n_used, int* length);
+aqmb_status aqmb_pages_counts(aqmb_pages_t pool, int* n_free, int* n_live);
 
 /* Static description of a status code. Never NULL. */
 const char* aqmb_strerror(aqmb_status status);

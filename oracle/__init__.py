@@ -14,12 +14,14 @@ checked against the paper by eye:
                   the distortion of every prefix level and the average-bits formula;
 * ``search``    - residual k-means encoding, exhaustive / beam code search on tiny
                   groups (plain or data-weighted error), and the beam searches with
-                  decisions taken in binary32 (the references of the GPU searches).
+                  decisions taken in binary32 (the references of the GPU searches);
+* ``decode``    - the operators between the layers of a decode step (norm, 8-bit scaling, 4-bit
+                  weights, attention over a paged cache), from their definitions.
 
 Every function cites the passage of the paper it follows. Pins live in
 ``tests/test_oracle_*.py``; functions without a pin say "parity unpinned".
 """
-from . import formats, aq, search  # noqa: F401
+from . import formats, aq, search, decode  # noqa: F401
 from .aq import (reconstruct, linear, dequant_canonical, gemm_reference, wmse_frobenius,
                  wmse_trace, prefix_distortions, bits_per_weight, code_bits_per_weight)  # noqa: F401
 from .search import (encode_residual_kmeans, brute_force_codes, beam_search_codes, beam_search_codes_f32,  # noqa: F401

@@ -18,7 +18,9 @@ from typing import Optional
 
 __all__ = ["Status", "DType", "Desc", "AqmbError", "GemvKernel", "GemmTiling", "lib", "create", "destroy", "get_desc",
            "gemv", "gemv_select", "gemm", "gemm_select", "dequant", "bits_per_weight", "strerror", "last_error",
-           "validate", "QuantLinear", "LIB_PATH"]
+           "validate", "QuantLinear", "LIB_PATH", "KVLayout", "W4Desc", "rms_norm", "w4_create", "w4_destroy",
+           "w4_get_desc", "w4_gemv", "W4Linear", "KVCache", "paged_attention", "paged_attention_workspace_bytes",
+           "kv_append", "kv_copy_pages", "PagePool"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libaqmb.so")
 
@@ -35,6 +37,14 @@ class DType(enum.IntEnum):
     F16 = 0
     BF16 = 1
     F32 = 2
+    F8 = 3       # e4m3; only the operators between the layers take it, with scales
+    I8 = 4
+
+
+class KVLayout(enum.IntEnum):
+    """aqmb_kv_layout: the order inside a page of a key-value cache."""
+    HEAD_MAJOR = 0
+    SLOT_MAJOR = 1
 
 
 class GemvKernel(enum.IntEnum):
@@ -57,6 +67,18 @@ class GemmTiling(enum.IntEnum):
 class Desc(ctypes.Structure):
     _fields_ = [("d_out", ctypes.c_int32), ("d_in", ctypes.c_int32), ("group_size", ctypes.c_int32),
                 ("num_codebooks", ctypes.c_int32), ("code_bits", ctypes.c_int32)]
+
+
+class W4Desc(ctypes.Structure):
+    _fields_ = [("d_out", ctypes.c_int32), ("d_in", ctypes.c_int32), ("group_size", ctypes.c_int32)]
+
+
+class KVCacheDesc(ctypes.Structure):
+    """aqmb_kv_cache."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class AqmbError(RuntimeError):
@@ -94,6 +116,27 @@ def _load() -> ctypes.CDLL:
     L.aqmb_prefix_distortion_noalloc.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp]
     L.aqmb_beam_search.argtypes = [ctypes.POINTER(Desc), i32, i32, vp, vp, vp, vp, vp, vp]
     L.aqmb_beam_search_weighted.argtypes = [ctypes.POINTER(Desc), i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    i64, f32, ip = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(i32)
+    cp = ctypes.POINTER(KVCacheDesc)
+    L.aqmb_rms_norm.argtypes = [vp, i32, i64, vp, vp, i64, vp, f32, f32, i32, i32, vp, i32, i64, vp, i32, vp]
+    L.aqmb_w4_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(W4Desc), vp, vp, vp, vp]
+    L.aqmb_w4_destroy.argtypes = [vp]
+    L.aqmb_w4_get_desc.argtypes = [vp, ctypes.POINTER(W4Desc)]
+    L.aqmb_w4_gemv.argtypes = [vp, vp, i32, i64, vp, i32, i32, vp, i32, i64, vp]
+    L.aqmb_paged_attention.argtypes = [cp, vp, i32, i64, i32, vp, i64, vp, i32, i32, f32, i32, vp, i64, vp, vp,
+                                       ctypes.c_size_t, vp]
+    L.aqmb_paged_attention_workspace_bytes.argtypes = [cp, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    L.aqmb_kv_append.argtypes = [cp, vp, i64, vp, i64, i32, vp, i32, vp]
+    L.aqmb_kv_copy_pages.argtypes = [cp, i32, vp, vp, i32, vp]
+    L.aqmb_pages_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32]
+    L.aqmb_pages_destroy.argtypes = [vp]
+    L.aqmb_pages_add.argtypes = [vp, ip]
+    L.aqmb_pages_fork.argtypes = [vp, i32, ip]
+    L.aqmb_pages_extend.argtypes = [vp, i32, i32, vp, ip, ip]
+    L.aqmb_pages_free.argtypes = [vp, i32]
+    L.aqmb_pages_compact.argtypes = [vp, vp, vp, ip]
+    L.aqmb_pages_table.argtypes = [vp, i32, vp, i32, ip, ip]
+    L.aqmb_pages_counts.argtypes = [vp, ip, ip]
     L.aqmb_validate.argtypes = [ctypes.POINTER(Desc), i32, i32, i32, i32, i32, vp, vp]
     L.aqmb_bits_per_weight.argtypes = [ctypes.POINTER(Desc), i32]
     L.aqmb_bits_per_weight.restype = ctypes.c_double
@@ -106,7 +149,11 @@ def _load() -> ctypes.CDLL:
               "aqmb_gemm_select", "aqmb_gemm_ws", "aqmb_gemm_workspace_bytes",
               "aqmb_dequant", "aqmb_prefix_distortion", "aqmb_prefix_distortion_noalloc", "aqmb_beam_search",
               "aqmb_beam_search_weighted",
-              "aqmb_validate"):
+              "aqmb_validate", "aqmb_rms_norm", "aqmb_w4_create", "aqmb_w4_destroy", "aqmb_w4_get_desc",
+              "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes", "aqmb_kv_append",
+              "aqmb_kv_copy_pages", "aqmb_pages_create", "aqmb_pages_destroy", "aqmb_pages_add", "aqmb_pages_fork",
+              "aqmb_pages_extend", "aqmb_pages_free", "aqmb_pages_compact", "aqmb_pages_table",
+              "aqmb_pages_counts"):
         getattr(L, f).restype = st
     return L
 
@@ -475,6 +522,416 @@ class QuantLinear:
     def close(self):
         if self.handle:
             destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ------------------------------------------------------------------------------------------------
+# The operators between the layers. These take tensors: types, sizes and strides come from them, and
+# what the library cannot see (a tensor's size and device) is checked here.
+_TORCH_DT8 = {**_TORCH_DT, torch.float8_e4m3fn: int(DType.F8), torch.int8: int(DType.I8)}
+
+
+def _refuse(where: str, message: str, status: Status = Status.EINVAL):
+    raise AqmbError(status, where, message)
+
+
+def _dt8(t, what: str, where: str) -> int:
+    d = _TORCH_DT8.get(t.dtype)
+    if d is None:
+        _refuse(where, f"{what} has dtype {t.dtype}", Status.EUNSUPPORTED)
+    return d
+
+
+def _here(where: str, **tensors) -> None:
+    """Every tensor lives on the current device."""
+    dev = _get_device() if _get_device is not None else torch.cuda.current_device()
+    for what, t in tensors.items():
+        if t is not None and t.get_device() != dev:
+            _refuse(where, f"{what} is on {t.device}, device {dev} is current")
+
+
+def _rows(t, rows: int, cols: int, what: str, where: str) -> int:
+    """The row stride of a [rows][cols] tensor whose rows are dense (of one row: the row itself)."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        _refuse(where, f"{what} is {tuple(t.shape)}, not ({rows}, {cols})")
+    s0, s1 = t.stride()
+    if s1 != 1 and cols != 1:
+        _refuse(where, f"{what}: the elements of a row must be adjacent")
+    return cols if rows == 1 else s0
+
+
+def _dense(t, dtype, n: int, what: str, where: str) -> None:
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(where, f"{what} must be dense, of {n} elements of {dtype}")
+
+
+def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=None, residual_out=None, scales=None,
+             scale_group: int = 0, stream=None) -> None:
+    """aqmb_rms_norm: y = rms_norm(x + residual) * (weight + weight_offset) for the rows of x
+    [rows][cols] fp16 or bf16; y is a tensor of the same shape: fp16, bf16, fp32, or (with scales
+    [rows][ceil(cols / scale_group)] fp32; scale_group 0 is the whole row) float8_e4m3fn or int8.
+    With a residual, x + residual is rounded into residual_out."""
+    where = "aqmb_rms_norm"
+    if x.dim() != 2:
+        _refuse(where, f"x is {tuple(x.shape)}, not (rows, cols)")
+    rows, cols = x.shape
+    xs = _rows(x, rows, cols, "x", where)
+    ys = _rows(y, rows, cols, "y", where)
+    dt, rs = _dt8(x, "x", where), 0
+    _here(where, x=x, weight=weight, y=y, residual=residual, residual_out=residual_out, scales=scales)
+    _dense(weight, x.dtype, cols, "weight", where)
+    if residual is not None:
+        if residual_out is None or residual.dtype != x.dtype or residual_out.dtype != x.dtype:
+            _refuse(where, "residual and residual_out go together, in the type of x")
+        rs = _rows(residual, rows, cols, "residual", where)
+        if _rows(residual_out, rows, cols, "residual_out", where) != rs:
+            _refuse(where, "residual and residual_out have different row strides")
+    if scales is not None:
+        if scale_group < 0:
+            _refuse(where, f"scale_group = {scale_group}")
+        _dense(scales, torch.float32, rows * (-(-cols // scale_group) if scale_group else 1), "scales", where)
+    st = lib.aqmb_rms_norm(x.data_ptr(), dt, xs, _ptr(residual), _ptr(residual_out), rs, weight.data_ptr(),
+                           weight_offset, eps, rows, cols, y.data_ptr(), _dt8(y, "y", where), ys, _ptr(scales),
+                           scale_group, _stream(stream))
+    if st:
+        _check(st, where)
+
+
+def w4_create(d_out: int, d_in: int, group_size: int, weights, scales, zeros=None, stream=None) -> int:
+    """aqmb_w4_create: weights [d_out][ceil(d_in/2)] uint8 (low nibble first), scales
+    [d_out][ceil(d_in/group_size)] fp16, zeros the same shape uint8 or None (8). Returns the handle."""
+    where = "aqmb_w4_create"
+    if d_out < 1 or d_in < 1 or group_size < 1:
+        _refuse(where, f"d_out = {d_out}, d_in = {d_in} and group_size = {group_size} must be >= 1")
+    groups = -(-d_in // group_size)
+    _here(where, weights=weights, scales=scales, zeros=zeros)
+    _dense(weights, torch.uint8, d_out * ((d_in + 1) // 2), "weights", where)
+    _dense(scales, torch.float16, d_out * groups, "scales", where)
+    if zeros is not None:
+        _dense(zeros, torch.uint8, d_out * groups, "zeros", where)
+    h = ctypes.c_void_p()
+    desc = W4Desc(d_out, d_in, group_size)
+    _check(lib.aqmb_w4_create(ctypes.byref(h), ctypes.byref(desc), _ptr(weights), _ptr(scales), _ptr(zeros),
+                              _stream(stream)), where)
+    return h.value
+
+
+def w4_destroy(layer: int) -> None:
+    _check(lib.aqmb_w4_destroy(layer), "aqmb_w4_destroy")
+
+
+def w4_get_desc(layer: int) -> W4Desc:
+    d = W4Desc()
+    _check(lib.aqmb_w4_get_desc(layer, ctypes.byref(d)), "aqmb_w4_get_desc")
+    return d
+
+
+def _w4_gemv(layer: int, d_out: int, d_in: int, group_size: int, x, y, x_scales, stream) -> None:
+    where = "aqmb_w4_gemv"
+    if x.dim() != 2:
+        _refuse(where, f"x is {tuple(x.shape)}, not (batch, d_in)")
+    batch, group = x.shape[0], 0
+    xs = _rows(x, batch, d_in, "x", where)
+    ys = _rows(y, batch, d_out, "y", where)
+    _here(where, x=x, y=y, x_scales=x_scales)
+    if x_scales is not None:
+        groups = -(-d_in // group_size)
+        # One scale per row, or one per group (the same thing where a row is one group).
+        if x_scales.numel() != batch:
+            group = group_size
+        _dense(x_scales, torch.float32, batch * (groups if group else 1), "x_scales", where)
+    st = lib.aqmb_w4_gemv(layer, x.data_ptr(), _dt8(x, "x", where), xs, _ptr(x_scales), group, batch, y.data_ptr(),
+                          _dt8(y, "y", where), ys, _stream(stream))
+    if st:
+        _check(st, where)
+
+
+def w4_gemv(layer: int, x, y, x_scales=None, stream=None) -> None:
+    """aqmb_w4_gemv: y [batch][d_out] = x [batch][d_in] times the layer's weights, 1 <= batch <= 16; x
+    fp16, bf16, or float8_e4m3fn / int8 with x_scales [batch][1] or [batch][groups of the layer] fp32."""
+    d = w4_get_desc(layer)
+    _w4_gemv(layer, d.d_out, d.d_in, d.group_size, x, y, x_scales, stream)
+
+
+class W4Linear:
+    """A linear layer of 4-bit weights with group scales, y = x W^T for up to 16 rows of x.
+
+    weights [d_out][ceil(d_in/2)] uint8, scales [d_out][groups] fp16, zeros [d_out][groups] uint8 or
+    None; d_in defaults to 2 * weights.shape[1]. ``gemv`` writes into a given y, ``forward`` (and a
+    call) allocates it, in the type of x or out_dtype (8-bit x: bf16)."""
+
+    def __init__(self, weights, scales, zeros=None, *, d_in: Optional[int] = None, group_size: int = 128):
+        self.handle = None
+        if weights.dim() != 2:
+            _refuse("W4Linear", f"weights are {tuple(weights.shape)}, not (d_out, ceil(d_in / 2))")
+        self.d_out, self.d_in = weights.shape[0], 2 * weights.shape[1] if d_in is None else d_in
+        self.group_size = group_size
+        self.handle = w4_create(self.d_out, self.d_in, group_size, weights, scales, zeros)
+
+    def gemv(self, x, y, x_scales=None, stream=None) -> None:
+        _w4_gemv(self.handle, self.d_out, self.d_in, self.group_size, x, y, x_scales, stream)
+
+    def forward(self, x, x_scales=None, out_dtype=None):
+        x2 = x if x.dim() == 2 and x.stride(-1) == 1 else x.reshape(-1, x.shape[-1]).contiguous()
+        dt = out_dtype or (x.dtype if x.dtype in _TORCH_DT else torch.bfloat16)
+        y = torch.empty((x2.shape[0], self.d_out), dtype=dt, device=x.device)
+        self.gemv(x2, y, x_scales)
+        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.d_out)
+
+    __call__ = forward
+
+    def close(self):
+        if self.handle:
+            w4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KVCache:
+    """A paged key-value cache of one attention layer over tensors of the caller.
+
+    k, v: [n_pages][n_kv_heads][page_size][head_dim] (layout "head") or
+    [n_pages][page_size][n_kv_heads][head_dim] ("slot"), dense inside a page: fp16, bf16, or
+    float8_e4m3fn with k_scale, v_scale fp32 of the same shape without head_dim, dense. ``allocate``
+    makes the tensors. The methods take the arguments of paged_attention and kv_append."""
+
+    _LAYOUTS = {"head": KVLayout.HEAD_MAJOR, "slot": KVLayout.SLOT_MAJOR}
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, *, layout: str = "head"):
+        where = "KVCache"
+        if layout not in self._LAYOUTS:
+            _refuse(where, f"layout {layout!r} is not 'head' or 'slot'")
+        dt = _TORCH_DT8.get(k.dtype)
+        if dt not in (DType.F16, DType.BF16, DType.F8):
+            _refuse(where, f"k has dtype {k.dtype}", Status.EUNSUPPORTED)
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+            _refuse(where, "k and v must be 4-dimensional, alike in shape, type and strides")
+        if 0 in k.shape:
+            _refuse(where, f"an empty cache {tuple(k.shape)}")
+        page = k[0].numel()
+        if not k[0].is_contiguous() or (k.shape[0] > 1 and k.stride(0) < page):
+            _refuse(where, "a page must be dense")
+        n = k.shape[0] * k.shape[1] * k.shape[2]
+        if (dt == DType.F8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            _refuse(where, "an 8-bit cache, and no other, has k_scale and v_scale")
+        for what, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is not None:
+                _dense(t, torch.float32, n, what, where)
+                if t.device != k.device:
+                    _refuse(where, f"{what} is on {t.device}, k on {k.device}")
+        if not k.is_cuda or v.device != k.device:
+            _refuse(where, "k and v must be on one GPU")
+        lay = self._LAYOUTS[layout]
+        heads, size = (k.shape[1], k.shape[2]) if lay == KVLayout.HEAD_MAJOR else (k.shape[2], k.shape[1])
+        self.k, self.v, self.k_scale, self.v_scale, self.layout = k, v, k_scale, v_scale, layout
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape[0], heads, size, k.shape[3]
+        self.device_index = k.get_device()
+        self.desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale),
+                                k.stride(0) if k.shape[0] > 1 else page, int(dt), int(lay), k.shape[0], size, heads,
+                                k.shape[3])
+        self._ref = ctypes.byref(self.desc)
+        self._plans = {}
+
+    @classmethod
+    def allocate(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype=torch.bfloat16, *,
+                 layout: str = "head", device="cuda") -> "KVCache":
+        a, b = (n_kv_heads, page_size) if layout == "head" else (page_size, n_kv_heads)
+        k, v = (torch.empty((n_pages, a, b, head_dim), dtype=dtype, device=device) for _ in range(2))
+        ks, vs = (torch.empty((n_pages, a, b), dtype=torch.float32, device=device) if dtype == torch.float8_e4m3fn
+                  else None for _ in range(2))
+        return cls(k, v, ks, vs, layout=layout)
+
+    def _current(self, where: str) -> None:
+        dev = _get_device() if _get_device is not None else torch.cuda.current_device()
+        if dev != self.device_index:
+            _refuse(where, f"the cache is on device {self.device_index}, device {dev} is current")
+
+    def workspace_bytes(self, n_heads: int, n_seqs: int, max_length: int, window: int = 0) -> int:
+        """aqmb_paged_attention_workspace_bytes (a function of these numbers, so asked once for each)."""
+        key = (n_heads, n_seqs, max_length, window)
+        n = self._plans.get(key)
+        if n is None:
+            b = ctypes.c_size_t(0)
+            _check(lib.aqmb_paged_attention_workspace_bytes(self._ref, n_heads, n_seqs, max_length, window,
+                                                            ctypes.byref(b)), "aqmb_paged_attention_workspace_bytes")
+            if len(self._plans) >= 4096:
+                self._plans.clear()
+            n = self._plans[key] = b.value
+        return n
+
+    def attention(self, q, page_table, lengths, out, *, scale: float, max_length: Optional[int] = None,
+                  window: int = 0, lse=None, workspace=None, stream=None) -> None:
+        """aqmb_paged_attention: out [n_seqs][n_heads][head_dim] for one query token of every sequence;
+        page_table [n_seqs][pages] and lengths [n_seqs] int32 on the GPU. max_length bounds the lengths
+        (default: what the table holds). Without a workspace one is taken from PyTorch's allocator on the
+        call's stream."""
+        where = "aqmb_paged_attention"
+        self._current(where)
+        _here(where, q=q, page_table=page_table, lengths=lengths, out=out, lse=lse, workspace=workspace)
+        if q.dim() != 3 or q.shape[2] != self.head_dim:
+            _refuse(where, f"q is {tuple(q.shape)}, not (n_seqs, n_heads, {self.head_dim})")
+        n, heads, dim = q.shape
+        for what, t in (("q", q), ("out", out)):
+            if t.shape != q.shape or t.dtype != q.dtype:
+                _refuse(where, f"{what} is {tuple(t.shape)} of {t.dtype}, not {tuple(q.shape)} of {q.dtype}")
+            if t.numel() and ((t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and heads != 1)):
+                _refuse(where, f"{what}: the heads of a sequence must be dense")
+        if page_table.dim() != 2 or page_table.shape[0] != n or page_table.dtype != torch.int32 \
+                or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            _refuse(where, f"page_table must be int32 [{n}][pages] with dense rows")
+        _dense(lengths, torch.int32, n, "lengths", where)
+        if lse is not None:
+            _dense(lse, torch.float32, n * heads, "lse", where)
+        per = page_table.shape[1]
+        if max_length is None:
+            max_length = min(per * self.page_size, 1 << 30)
+        elif max_length > per * self.page_size:
+            _refuse(where, f"max_length = {max_length} needs more pages than the table's {per}")
+        row = heads * dim
+        dt = _dt8(q, "q", where)
+        need = self.workspace_bytes(heads, n, max_length, window)
+        if workspace is None and need:
+            if stream is None:
+                workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+            else:   # the allocator ties memory to the stream that is current
+                s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)
+                with torch.cuda.stream(s):
+                    workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        st = lib.aqmb_paged_attention(self._ref, q.data_ptr(), dt, q.stride(0) if n > 1 else row, heads,
+                                      page_table.data_ptr(), page_table.stride(0) if n > 1 else per, lengths.data_ptr(),
+                                      n, max_length, scale, window, out.data_ptr(), out.stride(0) if n > 1 else row,
+                                      _ptr(lse), _ptr(workspace), _nbytes(workspace) or 0 if workspace is not None else 0,
+                                      _stream(stream))
+        if st:
+            _check(st, where)
+
+    def append(self, k, v, slots, stream=None) -> None:
+        """aqmb_kv_append: write k, v [n_tokens][n_kv_heads][head_dim] (fp16 or bf16) into slots int64
+        [n_tokens] on the GPU (page * page_size + offset; outside the cache: skipped)."""
+        where = "aqmb_kv_append"
+        self._current(where)
+        _here(where, k=k, v=v, slots=slots)
+        n, dim, heads = slots.numel(), self.head_dim, self.n_kv_heads
+        _dense(slots, torch.int64, n, "slots", where)
+        for what, t in (("k", k), ("v", v)):
+            if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != dim or t.dtype != k.dtype:
+                _refuse(where, f"{what} is {tuple(t.shape)} of {t.dtype}, not ({n}, {heads}, {dim}) of {k.dtype}")
+            if n and ((t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and heads != 1)):
+                _refuse(where, f"{what}: the heads of a token must be dense")
+        row = heads * dim
+        st = lib.aqmb_kv_append(self._ref, k.data_ptr(), k.stride(0) if n > 1 else row, v.data_ptr(),
+                                v.stride(0) if n > 1 else row, _dt8(k, "k", where), slots.data_ptr(), n, _stream(stream))
+        if st:
+            _check(st, where)
+
+
+def paged_attention(cache: KVCache, q, page_table, lengths, out, **kw) -> None:
+    """aqmb_paged_attention (see KVCache.attention)."""
+    cache.attention(q, page_table, lengths, out, **kw)
+
+
+def paged_attention_workspace_bytes(cache: KVCache, n_heads: int, n_seqs: int, max_length: int, window: int = 0) -> int:
+    return cache.workspace_bytes(n_heads, n_seqs, max_length, window)
+
+
+def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
+    """aqmb_kv_append (see KVCache.append)."""
+    cache.append(k, v, slots, stream)
+
+
+def kv_copy_pages(caches, src, dst, stream=None) -> None:
+    """aqmb_kv_copy_pages: page src[i] to page dst[i] (int32, on the GPU) in every KVCache of `caches`."""
+    where = "aqmb_kv_copy_pages"
+    caches = list(caches)
+    _here(where, src=src, dst=dst)
+    for c in caches:
+        c._current(where)
+    n = src.numel()
+    _dense(src, torch.int32, n, "src", where)
+    _dense(dst, torch.int32, n, "dst", where)
+    descs = (KVCacheDesc * max(len(caches), 1))(*[c.desc for c in caches])
+    st = lib.aqmb_kv_copy_pages(descs, len(caches), src.data_ptr(), dst.data_ptr(), n, _stream(stream))
+    if st:
+        _check(st, where)
+
+
+class PagePool:
+    """aqmb_pages_*: which pages of a cache each sequence holds, on the host. Sequences are small integers.
+
+    extend returns (slots int64 tensor, copies) where copies is [] or [(src, dst)]: the page to copy in
+    every layer's cache before the tokens are written; compact returns such a list for the whole pool.
+    table returns the pages as an int32 tensor. All of them are CPU tensors and lists: one upload of a
+    step's tables, slots and copies serves all layers."""
+
+    def __init__(self, n_pages: int, page_size: int, max_seqs: int):
+        self.handle = None
+        h = ctypes.c_void_p()
+        _check(lib.aqmb_pages_create(ctypes.byref(h), n_pages, page_size, max_seqs), "aqmb_pages_create")
+        self.handle, self.n_pages, self.page_size, self.max_seqs = h.value, n_pages, page_size, max_seqs
+
+    def add(self) -> int:
+        s = ctypes.c_int()
+        _check(lib.aqmb_pages_add(self.handle, ctypes.byref(s)), "aqmb_pages_add")
+        return s.value
+
+    def fork(self, seq: int) -> int:
+        s = ctypes.c_int()
+        _check(lib.aqmb_pages_fork(self.handle, seq, ctypes.byref(s)), "aqmb_pages_fork")
+        return s.value
+
+    def extend(self, seq: int, n_tokens: int):
+        slots = torch.empty((max(n_tokens, 0),), dtype=torch.int64)
+        src, dst = ctypes.c_int32(), ctypes.c_int32()
+        _check(lib.aqmb_pages_extend(self.handle, seq, n_tokens, slots.data_ptr(), ctypes.byref(src),
+                                     ctypes.byref(dst)), "aqmb_pages_extend")
+        return slots, [(src.value, dst.value)] if src.value >= 0 else []
+
+    def free(self, seq: int) -> None:
+        _check(lib.aqmb_pages_free(self.handle, seq), "aqmb_pages_free")
+
+    def compact(self):
+        room = max(1, self.n_pages // 2)
+        src, dst, n = (ctypes.c_int32 * room)(), (ctypes.c_int32 * room)(), ctypes.c_int()
+        _check(lib.aqmb_pages_compact(self.handle, src, dst, ctypes.byref(n)), "aqmb_pages_compact")
+        return list(zip(src[:n.value], dst[:n.value]))
+
+    def _sizes(self, seq: int):
+        n, length = ctypes.c_int(), ctypes.c_int()
+        _check(lib.aqmb_pages_table(self.handle, seq, None, 0, ctypes.byref(n), ctypes.byref(length)),
+               "aqmb_pages_table")
+        return n.value, length.value
+
+    def length(self, seq: int) -> int:
+        return self._sizes(seq)[1]
+
+    def table(self, seq: int):
+        n, length = ctypes.c_int(), ctypes.c_int()
+        pages = torch.empty((self._sizes(seq)[0],), dtype=torch.int32)
+        if pages.numel():
+            _check(lib.aqmb_pages_table(self.handle, seq, pages.data_ptr(), pages.numel(), ctypes.byref(n),
+                                        ctypes.byref(length)), "aqmb_pages_table")
+        return pages
+
+    def counts(self):
+        """(free pages, live sequences)"""
+        f, s = ctypes.c_int(), ctypes.c_int()
+        _check(lib.aqmb_pages_counts(self.handle, ctypes.byref(f), ctypes.byref(s)), "aqmb_pages_counts")
+        return f.value, s.value
+
+    def close(self):
+        if self.handle:
+            _check(lib.aqmb_pages_destroy(self.handle), "aqmb_pages_destroy")
             self.handle = None
 
     def __del__(self):

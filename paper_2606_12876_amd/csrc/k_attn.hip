@@ -1,0 +1,430 @@
+// Attention of one new token per sequence over a paged key-value cache.
+//
+//   score_t = scale <q, K_t>,  out = sum_t exp(score_t - m) V_t / sum_t exp(score_t - m)
+//
+// K and V are read once and nothing else is large, so HBM bounds it; everything below serves loads in
+// flight. A workgroup takes a chunk of one sequence's positions for the (up to 16) query heads of one
+// key-value head, its waves take turns at tiles of 32 positions, each with a running maximum and sum
+// of its own. Both products run on the matrix cores without LDS:
+//   S^T = K Q^T  rows: 16 positions, columns: heads. Lane (r, quarter) supplies the key of position
+//                8 (r / 4) + r % 4 (second product: 4 more), so that the result leaves it with head r's
+//                scores of positions 8 quarter .. 8 quarter + 7:
+//   O^T = V^T P^T  is fed exactly that as its second operand. The first comes from the lane's own loads:
+//                8 positions x 8 neighbouring values, transposed in registers (one byte permutation for
+//                every two values).
+// A column is a head in both, so maximum, sum and rescaling stay within a lane, but for two exchanges
+// between the quarters per tile.
+//
+// Probabilities enter the second product as two 16-bit parts (value and remainder): rounding them once
+// to bf16 would cost as much as rounding the result does when few positions carry the weight. With an
+// fp16 cache they are formed 2^14 larger, so that small ones keep their digits above fp16's smallest
+// subnormal. An F8 cache is widened to bf16 for V (its scale joins the probability) and to the type of q
+// for K (its scale joins the score): both exact.
+//
+// Chunks of a sequence are joined by a second kernel from (max, sum, unnormalised out) in the workspace.
+#include "device.h"
+#include "ops.h"
+
+namespace aqmb {
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kTile = 32, kWaves = 4, kChunkMax = 4096;
+
+// The binary32 number next below a positive one; 0 for 0.
+__device__ __forceinline__ float below(float x) {
+  return __builtin_bit_cast(float, __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, x), 1u));
+}
+
+// split: two probabilities (>= 0) as two 16-bit parts each, cut off rather than rounded and from just
+// below, so that both parts of a positive one are positive: an infinite value of V then gives infinity,
+// not the NaN that inf * 0 or inf - inf would be.
+template <int T> struct Mma;
+template <> struct Mma<AQMB_F16> {
+  static __device__ __forceinline__ f32x4_t mul(u32x4_t a, u32x4_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16x2(lo, hi); }
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& a, uint32_t& b) {
+    a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(below(x), below(y)));
+    b = pack_f16x2(fmaxf(x - f16lo(a), 0x1p-24f), fmaxf(y - f16hi(a), 0x1p-24f));
+  }
+  static constexpr float kShift = 14.f;
+};
+template <> struct Mma<AQMB_BF16> {
+  static __device__ __forceinline__ f32x4_t mul(u32x4_t a, u32x4_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& a, uint32_t& b) {
+    a = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, below(y)), __builtin_bit_cast(uint32_t, below(x)), 0x07060302u);
+    b = pack_bf16x2(x - bf16lo(a), y - bf16hi(a));
+  }
+  static constexpr float kShift = 0.f;
+};
+
+// Four e4m3 values (one dword) widened to 16 bits, exactly.
+template <int T>
+__device__ __forceinline__ uint2 widen_f8(uint32_t w) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return make_uint2(Mma<T>::pack(a.x, a.y), Mma<T>::pack(b.x, b.y));
+}
+
+// Raw loads of 8 (DC >= 8) or 4 values of the cache.
+template <bool F8, int N> struct Raw;
+template <> struct Raw<false, 8> { typedef u32x4_t T; };
+template <> struct Raw<false, 4> { typedef uint2 T; };
+template <> struct Raw<true, 8> { typedef uint2 T; };
+template <> struct Raw<true, 4> { typedef uint32_t T; };
+
+template <int T, bool F8>
+__device__ __forceinline__ u32x4_t as16(typename Raw<F8, 8>::T r) {
+  if constexpr (F8) {
+    const uint2 a = widen_f8<T>(r.x), b = widen_f8<T>(r.y);
+    return u32x4_t{a.x, a.y, b.x, b.y};
+  } else {
+    return r;
+  }
+}
+template <int T, bool F8>
+__device__ __forceinline__ uint2 as16h(typename Raw<F8, 4>::T r) {
+  if constexpr (F8) return widen_f8<T>(r);
+  else return r;
+}
+
+__device__ __forceinline__ uint32_t lo_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t hi_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+struct AttnDev {
+  AttnArgs a;
+  uint32_t page_magic;     // 2^32 / page_size + 1 (page_size > 1)
+  int group, head_tiles;
+};
+
+// T: type of q and of the products with K; PT: type of the products with V. DC: values of V per lane
+// and position, head_dim <= 16 DC.
+template <int T, int PT, bool F8, int DC>
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
+  const AttnArgs& a = A.a;
+  constexpr int kS = DC / 2;             // steps of 32 along head_dim for S
+  constexpr int VN = DC >= 8 ? 8 : 4;    // values per V load
+  constexpr int VL = DC / VN;            // V loads per position
+  constexpr size_t E = F8 ? 1 : 2;
+  extern __shared__ int pages[];         // the chunk's page numbers, -1 where there is none
+  __shared__ float s_ml[kWaves][2][16], s_join[2][16];
+
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int r = lane % 16, q = lane / 16;
+  const int split = blockIdx.x, kvh = blockIdx.y / A.head_tiles, ht = blockIdx.y % A.head_tiles, seq = blockIdx.z;
+  const int h0 = kvh * A.group + ht * 16;                       // first query head
+  const int nh = min(16, A.group - ht * 16);
+  const int len = max(0, min(a.lengths[seq], a.max_length));
+  const int lo = a.window > 0 ? max(0, len - a.window) : 0;
+  const int c0 = (lo & ~7) + split * a.chunk, c1 = min(len, c0 + a.chunk);
+  if (c0 >= len) {                                              // no positions here
+    if (split == 0 && a.n_splits == 1) {
+      for (int e = threadIdx.x; e < nh * a.head_dim; e += 64 * kWaves) {
+        const int h = h0 + e / a.head_dim;
+        ((uint16_t*)a.out)[seq * a.out_stride + (int64_t)h * a.head_dim + e % a.head_dim] = 0;
+      }
+      if (a.lse && threadIdx.x < nh) a.lse[(int64_t)seq * a.n_heads + h0 + threadIdx.x] = -__builtin_inff();
+    }
+    return;
+  }
+  const int p0 = c0 / a.page_size, np = (c1 - 1) / a.page_size - p0 + 1;
+  for (int i = threadIdx.x; i < np; i += 64 * kWaves) {
+    const int p = a.table[seq * a.table_stride + p0 + i];
+    pages[i] = p >= 0 && p < a.n_pages ? p : -1;
+  }
+
+  // Q^T as the second operand: lane (r, q) holds q[head r][32 s + 8 q ..].
+  u32x4_t qf[kS];
+  {
+    const uint16_t* qr = (const uint16_t*)a.q + seq * a.q_stride + (int64_t)(h0 + min(r, nh - 1)) * a.head_dim;
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      const int d = 32 * s + 8 * q;
+      qf[s] = d < a.head_dim ? *(const u32x4_t*)(qr + d) : u32x4_t{0, 0, 0, 0};
+    }
+  }
+  __syncthreads();
+
+  // Position -> page (LDS index) and slot; positions are relative to the chunk's first page.
+  const int base = p0 * a.page_size;
+  auto locate = [&](int pos, int& page, int& slot) {
+    const uint32_t rel = (uint32_t)(pos - base);
+    const uint32_t i = a.page_size == 1 ? rel : __umulhi(rel, A.page_magic);
+    page = pages[i];
+    slot = (int)(rel - i * (uint32_t)a.page_size);
+  };
+  const char* kb = (const char*)a.k + (int64_t)kvh * a.head_stride * E;
+  const char* vb = (const char*)a.v + (int64_t)kvh * a.head_stride * E;
+  const float scale2 = a.scale * 1.4426950408889634f;           // scores in units of log 2
+
+  f32x4_t o[DC];
+#pragma unroll
+  for (int e = 0; e < DC; ++e) o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -__builtin_inff(), l = 0.f;
+
+  for (int t0 = c0 + kTile * wave; t0 < c1; t0 += kTile * kWaves) {
+    // Keys of two positions, values of eight. Positions outside are read at the nearest one inside.
+    typename Raw<F8, 8>::T kr[2][kS];
+    typename Raw<F8, VN>::T vr[8][VL];
+    uint32_t vmask = 0;                                         // bit j: position 8 q + j takes part
+    float ks[8], vs[8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int pos = t0 + 8 * (r / 4) + r % 4 + 4 * b;
+      int page, slot;
+      locate(max(lo, min(pos, c1 - 1)), page, slot);
+      const char* p = kb + ((int64_t)max(page, 0) * a.page_stride + (int64_t)slot * a.slot_stride) * E;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        const int d = 32 * s + 8 * q;
+        kr[b][s] = *(const typename Raw<F8, 8>::T*)(p + (d < a.head_dim ? d : 0) * E);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int pos = t0 + 8 * q + j;
+      int page, slot;
+      locate(max(lo, min(pos, c1 - 1)), page, slot);
+      if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
+      const int64_t pg = max(page, 0);
+      const char* p = vb + (pg * a.page_stride + (int64_t)slot * a.slot_stride) * E;
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        const int d = r * DC + i * VN;
+        vr[j][i] = *(const typename Raw<F8, VN>::T*)(p + (d < a.head_dim ? d : 0) * E);
+      }
+      if constexpr (F8) {
+        const int64_t sc = pg * a.sc_page + (int64_t)kvh * a.sc_head + (int64_t)slot * a.sc_slot;
+        ks[j] = a.k_scale[sc];
+        vs[j] = a.v_scale[sc];
+      }
+    }
+
+    f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      u32x4_t ka = as16<T, F8>(kr[0][s]), kc = as16<T, F8>(kr[1][s]);
+      if (32 * s + 8 * q >= a.head_dim) ka = kc = u32x4_t{0, 0, 0, 0};
+      sa = Mma<T>::mul(ka, qf[s], sa);
+      sb = Mma<T>::mul(kc, qf[s], sb);
+    }
+    float p[8];
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      p[j] = (j < 4 ? sa[j] : sb[j - 4]) * scale2;
+      if constexpr (F8) p[j] *= ks[j];
+      if (!(vmask >> j & 1)) p[j] = -__builtin_inff();
+      top = fmaxf(top, p[j]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m2 = fmaxf(m, top);
+    const float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
+    if (__any(m2 > m)) {
+      const float f = __builtin_amdgcn_exp2f(m - m2 == 0.f ? 0.f : (m2 == -__builtin_inff() ? 0.f : m - m2));
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < DC; ++e) o[e] *= f;
+      m = m2;
+    }
+    uint32_t ph[4], pl[4];
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      float x = __builtin_amdgcn_exp2f(p[j] - mu), y = __builtin_amdgcn_exp2f(p[j + 1] - mu);
+      l += x + y;
+      if constexpr (F8) {
+        x = vmask >> j & 1 ? x * vs[j] : 0.f;
+        y = vmask >> (j + 1) & 1 ? y * vs[j + 1] : 0.f;
+      }
+      Mma<PT>::split(x, y, ph[j / 2], pl[j / 2]);
+    }
+    const u32x4_t pho = {ph[0], ph[1], ph[2], ph[3]}, plo = {pl[0], pl[1], pl[2], pl[3]};
+
+    // V^T: values of 8 positions, transposed. A value that takes no part must be 0, not garbage.
+    const bool clean = __all(vmask == 0xFFu);
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      uint32_t v[8][VN / 2];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (VN == 8) {
+          const u32x4_t w = as16<PT, F8>(vr[j][i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[j][e] = w[e];
+        } else {
+          const uint2 w = as16h<PT, F8>(vr[j][i]);
+          v[j][0] = w.x;
+          v[j][1] = w.y;
+        }
+      }
+      const bool in = r * DC + i * VN < a.head_dim;
+      if (!clean || 16 * DC != a.head_dim) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool keep = in && (vmask >> j & 1);
+#pragma unroll
+          for (int e = 0; e < VN / 2; ++e) v[j][e] = keep ? v[j][e] : 0;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        u32x4_t w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = e % 2 ? hi_halves(v[2 * j][e / 2], v[2 * j + 1][e / 2]) : lo_halves(v[2 * j][e / 2], v[2 * j + 1][e / 2]);
+        o[i * VN + e] = Mma<PT>::mul(w, pho, o[i * VN + e]);
+        o[i * VN + e] = Mma<PT>::mul(w, plo, o[i * VN + e]);
+      }
+    }
+  }
+
+  // The quarters' sums of one head, then the waves.
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (q == 0) {
+    s_ml[wave][0][r] = m;
+    s_ml[wave][1][r] = l;
+  }
+  __syncthreads();                        // also: every wave is done with pages
+  float M = -__builtin_inff(), L = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][0][r]);
+  const float Mu = M == -__builtin_inff() ? 0.f : M;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) L += s_ml[w][1][r] * __builtin_amdgcn_exp2f(s_ml[w][0][r] - Mu);
+  const float mine = __builtin_amdgcn_exp2f(m - Mu);            // 0 for a wave without positions
+  float* so = (float*)pages;              // [kWaves][nh][head_dim]
+  if (r < nh) {
+#pragma unroll
+    for (int e = 0; e < DC; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = (4 * q + i) * DC + e;
+        if (d < a.head_dim) so[(wave * nh + r) * a.head_dim + d] = o[e][i] * mine;
+      }
+  }
+  if (wave == 0 && q == 0) {              // the joined statistics, for the lines below
+    s_join[0][r] = M;
+    s_join[1][r] = L;
+  }
+  __syncthreads();
+  const bool one = a.n_splits == 1;
+  for (int e = threadIdx.x; e < nh * a.head_dim; e += 64 * kWaves) {
+    const int h = e / a.head_dim, d = e % a.head_dim;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v += so[(w * nh + h) * a.head_dim + d];
+    if (one) {
+      const float sum = s_join[1][h];
+      OutT<T>::store(a.out, seq * a.out_stride + (int64_t)(h0 + h) * a.head_dim + d, sum > 0.f ? v / sum : v);
+    } else {
+      a.part[(((int64_t)seq * a.n_heads + h0 + h) * a.n_splits + split) * a.head_dim + d] = v;
+    }
+  }
+  if (threadIdx.x < nh) {
+    const float mm = s_join[0][threadIdx.x], sum = s_join[1][threadIdx.x];
+    const int64_t at = (int64_t)seq * a.n_heads + h0 + threadIdx.x;
+    if (!one) {
+      float* ml = a.part + (int64_t)a.n_seqs * a.n_heads * a.n_splits * a.head_dim;
+      ml[(at * a.n_splits + split) * 2] = mm;
+      ml[(at * a.n_splits + split) * 2 + 1] = sum;
+    } else if (a.lse) {
+      a.lse[at] = sum > 0.f ? (mm - Mma<PT>::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -__builtin_inff();
+    }
+  }
+}
+
+// Joins the chunks of one (sequence, head): one workgroup, its waves take turns at the chunks.
+template <int T>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, float shift) {
+  __shared__ float so[4][256];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t at = (int64_t)blockIdx.y * a.n_heads + blockIdx.x;
+  const int seq = blockIdx.y;
+  const int len = max(0, min(a.lengths[seq], a.max_length));
+  const int lo = a.window > 0 ? max(0, len - a.window) : 0;
+  const int n = len > 0 ? (len - (lo & ~7) + a.chunk - 1) / a.chunk : 0;
+  const float* ml = a.part + (int64_t)a.n_seqs * a.n_heads * a.n_splits * a.head_dim + at * a.n_splits * 2;
+  float M = -__builtin_inff();
+  for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * i]);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+  const float Mu = M == -__builtin_inff() ? 0.f : M;
+  float L = 0.f;
+  for (int i = lane; i < n; i += 64) L += ml[2 * i + 1] * __builtin_amdgcn_exp2f(ml[2 * i] - Mu);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) L += __shfl_xor(L, d);
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  const float* part = a.part + at * a.n_splits * a.head_dim;
+  for (int i = wave; i < n; i += 4) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * i] - Mu);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c * 64 + lane < a.head_dim) v[c] += f * part[(int64_t)i * a.head_dim + c * 64 + lane];
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) so[wave][c * 64 + lane] = v[c];
+  __syncthreads();
+  if (threadIdx.x < a.head_dim) {
+    const float s = so[0][threadIdx.x] + so[1][threadIdx.x] + so[2][threadIdx.x] + so[3][threadIdx.x];
+    OutT<T>::store(a.out, seq * a.out_stride + (int64_t)blockIdx.x * a.head_dim + threadIdx.x, L > 0.f ? s / L : s);
+  }
+  if (a.lse && threadIdx.x == 0)
+    a.lse[at] = L > 0.f ? (M - shift + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -__builtin_inff();
+}
+
+AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu) {
+  // A window reaches from the 8 positions that its first one is in.
+  const int64_t span = window > 0 && window < max_length ? (int64_t)window + 7 : max_length;
+  const int64_t groups = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
+  const int64_t want = (2 * (int64_t)n_cu + groups - 1) / groups;           // workgroups along a sequence
+  int64_t chunk = (span + want - 1) / want;
+  const int64_t unit = kTile * kWaves;
+  chunk = (chunk + unit - 1) / unit * unit;
+  chunk = chunk < unit ? unit : chunk > kChunkMax ? kChunkMax : chunk;
+  const int64_t n = span > 0 ? (span + chunk - 1) / chunk : 1;
+  AttnPlan p;
+  p.chunk = (int)chunk;
+  p.n_splits = (int)n;
+  p.bytes = n == 1 ? 0 : (size_t)n_seqs * n_heads * n * (head_dim + 2) * sizeof(float);
+  return p;
+}
+
+template <int T, int PT, bool F8>
+static hipError_t go(const AttnArgs& a, hipStream_t st) {
+  AttnDev A;
+  A.a = a;
+  A.page_magic = a.page_size > 1 ? (uint32_t)((1ull << 32) / (uint32_t)a.page_size + 1) : 0;
+  A.group = a.n_heads / a.n_kv;
+  A.head_tiles = (A.group + 15) / 16;
+  const int nh = A.group < 16 ? A.group : 16;
+  const size_t tab = (size_t)(a.chunk / a.page_size + 2) * sizeof(int);
+  const size_t acc = (size_t)kWaves * nh * a.head_dim * sizeof(float);
+  const size_t lds = tab > acc ? tab : acc;
+  const dim3 grid(a.n_splits, a.n_kv * A.head_tiles, a.n_seqs);
+  hipError_t e = hipSuccess;
+  auto run = [&](auto kernel) {
+    if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e == hipSuccess) kernel<<<grid, 64 * kWaves, lds, st>>>(A);
+    if (e == hipSuccess) e = hipGetLastError();
+  };
+  if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4>);
+  else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8>);
+  else run(attn_kernel<T, PT, F8, 16>);
+  if (e != hipSuccess || a.n_splits == 1) return e;
+  attn_join_kernel<T><<<dim3(a.n_heads, a.n_seqs), 256, 0, st>>>(a, Mma<PT>::kShift);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention(const AttnArgs& a, aqmb_dtype dtype, bool f8, hipStream_t st) {
+  if (f8) return dtype == AQMB_F16 ? go<AQMB_F16, AQMB_BF16, true>(a, st) : go<AQMB_BF16, AQMB_BF16, true>(a, st);
+  return dtype == AQMB_F16 ? go<AQMB_F16, AQMB_F16, false>(a, st) : go<AQMB_BF16, AQMB_BF16, false>(a, st);
+}
+
+}  // namespace aqmb

@@ -1,0 +1,255 @@
+// Root-mean-square norm with the residual's addition and 16-bit, binary32 or 8-bit output.
+//
+//   h = x + r,  r' = round(h),  v = h * (1 / sqrt(mean(h^2) + eps)) * (w + w0)
+//
+// A row is read once and stays in registers: NT threads own 8 consecutive columns each, NV times
+// over, so the sum of squares, the largest magnitude of a scale group (g / 8 neighbouring lanes) and
+// the output need no second pass over memory. Bound by HBM for many rows, by latency (load, two
+// reductions, store) for few.
+#include "device.h"
+#include "ops.h"
+
+namespace aqmb {
+
+// 8 consecutive 16-bit elements, of which the first n exist (n <= 0: none). Rows may start at any
+// element: the 16-byte access needs no alignment beyond the element's on gfx950.
+struct __attribute__((packed, aligned(2))) Raw8 { uint32_t w[4]; };
+
+__device__ __forceinline__ Raw8 load8(const uint16_t* p, int n) {
+  Raw8 r = {{0, 0, 0, 0}};
+  if (n >= 8) {
+    r = *(const Raw8*)p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) r.w[i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
+  }
+  return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void widen8(const Raw8& r, float* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = DT == AQMB_F16 ? f16lo(r.w[i]) : bf16lo(r.w[i]);
+    f[2 * i + 1] = DT == AQMB_F16 ? f16hi(r.w[i]) : bf16hi(r.w[i]);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void store8_16(uint16_t* p, const float* f, int n) {
+  Raw8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r.w[i] = DT == AQMB_F16 ? pack_f16x2(f[2 * i], f[2 * i + 1]) : pack_bf16x2(f[2 * i], f[2 * i + 1]);
+  if (n >= 8) {
+    *(Raw8*)p = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint16_t)(r.w[i / 2] >> (16 * (i % 2)));
+  }
+}
+
+struct __attribute__((packed, aligned(4))) F4 { float f[4]; };
+struct __attribute__((packed, aligned(1))) B8 { uint32_t w[2]; };
+
+template <int NT>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  if constexpr (NT > 64) {
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v += lds[i];
+  }
+  return v;
+}
+
+// Largest of the magnitudes as bits: above every finite value come infinity and then the NaNs, so one
+// integer maximum also says whether a value is not finite.
+template <int NT>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  if constexpr (NT > 64) {
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v = max(v, lds[i]);
+  }
+  return v;
+}
+
+constexpr float kScaleFloor = 7.888609052210118e-31f;  // 2^-100: keeps L / a and a / L normal numbers
+
+// NT threads per row (64: one wave, four rows per workgroup; else the whole workgroup).
+template <int DT, int NT, int NV>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_kernel(NormArgs a) {
+  __shared__ float lds_sum[16];
+  __shared__ uint32_t lds_max[16];
+  const int t = NT == 64 ? threadIdx.x % 64 : threadIdx.x;
+  const int64_t row = NT == 64 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
+  if (NT == 64 && row >= a.rows) return;      // whole waves, and no barrier below for NT = 64
+  const uint16_t* x = (const uint16_t*)a.x + row * a.x_stride;
+  const uint16_t* r = a.residual ? (const uint16_t*)a.residual + row * a.residual_stride : nullptr;
+
+  float h[NV][8];
+  Raw8 w[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * NT + t) * 8;
+    widen8<DT>(load8(x + c, a.cols - c), h[i]);
+  }
+  if (r) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * NT + t) * 8;
+      float f[8];
+      widen8<DT>(load8(r + c, a.cols - c), f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[i][j] += f[j];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * NT + t) * 8;
+    w[i] = load8((const uint16_t*)a.weight + c, a.cols - c);
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * NT + t) * 8;
+    if (r) store8_16<DT>((uint16_t*)a.residual_out + row * a.residual_stride + c, h[i], a.cols - c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss += h[i][j] * h[i][j];
+  }
+  ss = row_sum<NT>(ss, lds_sum);
+  const float inv = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float f[8];
+    widen8<DT>(w[i], f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[i][j] = h[i][j] * inv * (f[j] + a.weight_offset);
+    // Columns past the end hold h = 0; an infinite offset or inv would make them NaN.
+    const int c = (i * NT + t) * 8;
+    if (a.cols - c < 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j >= a.cols) h[i][j] = 0.f;
+    }
+  }
+
+  if (a.y_dtype == AQMB_F16 || a.y_dtype == AQMB_BF16) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * NT + t) * 8;
+      uint16_t* y = (uint16_t*)a.y + row * a.y_stride + c;
+      if (a.y_dtype == AQMB_F16) store8_16<AQMB_F16>(y, h[i], a.cols - c);
+      else store8_16<AQMB_BF16>(y, h[i], a.cols - c);
+    }
+    return;
+  }
+  if (a.y_dtype == AQMB_F32) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * NT + t) * 8, n = a.cols - c;
+      float* y = (float*)a.y + row * a.y_stride + c;
+      if (n >= 8) {
+        ((F4*)y)[0] = F4{{h[i][0], h[i][1], h[i][2], h[i][3]}};
+        ((F4*)y)[1] = F4{{h[i][4], h[i][5], h[i][6], h[i][7]}};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < n) y[j] = h[i][j];
+      }
+    }
+    return;
+  }
+
+  // 8 bits. The group's largest magnitude: g / 8 neighbouring lanes, or the whole row.
+  const int g = a.scale_group;
+  const float top = a.y_dtype == AQMB_F8 ? 448.f : 127.f;
+  uint32_t m[NV];
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    m[i] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m[i] = max(m[i], __builtin_bit_cast(uint32_t, h[i][j]) & 0x7FFFFFFFu);
+    all = max(all, m[i]);
+  }
+  if (g == 0) {
+    all = row_max<NT>(all, lds_max);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) m[i] = all;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      for (int d = g / 16; d >= 1; d >>= 1) m[i] = max(m[i], (uint32_t)__shfl_xor((int)m[i], d));
+  }
+  const int n_groups = g ? (a.cols + g - 1) / g : 1;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * NT + t) * 8, n = a.cols - c;
+    if (n <= 0) continue;
+    const bool finite = m[i] < 0x7F800000u;
+    const float big = fmaxf(__builtin_bit_cast(float, m[i]), kScaleFloor);
+    const float mul = top / big;
+    const float scale = finite ? big / top : __builtin_nanf("");
+    if (g ? c % g == 0 : c == 0) a.scales[row * n_groups + (g ? c / g : 0)] = scale;
+    B8 b;
+    if (a.y_dtype == AQMB_F8) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        int w8 = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * k] * mul, h[i][4 * k + 1] * mul, 0, false);
+        b.w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * k + 2] * mul, h[i][4 * k + 3] * mul, w8, true);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        b.w[k] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b.w[k] |= ((uint32_t)__float2int_rn(h[i][4 * k + j] * mul) & 0xFFu) << (8 * j);
+      }
+    }
+    if (!finite) b.w[0] = b.w[1] = 0;
+    uint8_t* y = (uint8_t*)a.y + row * a.y_stride + c;
+    if (n >= 8) {
+      *(B8*)y = b;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) y[j] = (uint8_t)(b.w[j / 4] >> (8 * (j % 4)));
+    }
+  }
+}
+
+template <int DT, int NT, int NV>
+static hipError_t go(const NormArgs& a, hipStream_t st) {
+  const int blocks = NT == 64 ? (a.rows + 3) / 4 : a.rows;
+  norm_kernel<DT, NT, NV><<<blocks, NT == 64 ? 256 : NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <int DT>
+static hipError_t choose(const NormArgs& a, hipStream_t st) {
+  const int v = (a.cols + 7) / 8;
+  if (v <= 64) return go<DT, 64, 1>(a, st);
+  if (v <= 128) return go<DT, 64, 2>(a, st);
+  if (v <= 256) return go<DT, 256, 1>(a, st);
+  if (v <= 512) return go<DT, 256, 2>(a, st);
+  if (v <= 1024) return go<DT, 256, 4>(a, st);
+  if (v <= 2048) return go<DT, 1024, 2>(a, st);
+  return go<DT, 1024, 4>(a, st);
+}
+
+hipError_t launch_rms_norm(const NormArgs& a, aqmb_dtype dtype, hipStream_t st) {
+  return dtype == AQMB_F16 ? choose<AQMB_F16>(a, st) : choose<AQMB_BF16>(a, st);
+}
+
+}  // namespace aqmb

@@ -18,7 +18,11 @@ aqmb_status fail(aqmb_status s, const char* fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_last_error = buf;
+  try {  // no exception may leave a C entry point, not even for want of memory for the message
+    g_last_error = buf;
+  } catch (...) {
+    g_last_error.clear();
+  }
   return s;
 }
 
