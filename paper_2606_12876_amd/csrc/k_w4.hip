@@ -44,12 +44,14 @@ __global__ void w4_pack_kernel(const uint8_t* w, uint32_t* tiles, int d_out, int
   tiles[i] = v;
 }
 
-// Scales and zero points, one thread per (row tile, group, row).
+// Scales and zero points of a tile, [row / 4][group][row % 4]: a lane's share is one piece.
 __global__ void w4_pack_scales_kernel(const uint16_t* s, const uint8_t* z, uint16_t* so, uint8_t* zo, int d_out,
-                                      int groups, int padded, size_t n) {
+                                      int groups, int n_kt, int per, size_t n) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n) return;
-  const int row = (int)(i / 16 / padded) * kW4Rows + i % 16, g = (int)(i / 16 % padded);
+  const size_t tile = i / (16 * per);
+  const int e = (int)(i % (16 * per));
+  const int row = (int)(tile / n_kt) * kW4Rows + e / (4 * per) * 4 + e % 4, g = (int)(tile % n_kt) * per + e / 4 % per;
   const bool in = row < d_out && g < groups;
   so[i] = in ? s[(size_t)row * groups + g] : 0;
   if (zo) zo[i] = in ? z[(size_t)row * groups + g] : 0;
@@ -57,31 +59,70 @@ __global__ void w4_pack_scales_kernel(const uint16_t* s, const uint8_t* z, uint1
 
 hipError_t launch_w4_pack(const W4& L, const uint8_t* weights, const uint16_t* scales, const uint8_t* zeros,
                           hipStream_t st) {
-  const int g = L.d.group_size, groups = (L.d.d_in + g - 1) / g, padded = L.n_kt * (kW4Cols / g);
-  const size_t n = (size_t)L.n_rt * L.n_kt * 256, ns = (size_t)L.n_rt * padded * 16;
+  const int g = L.d.group_size, groups = (L.d.d_in - 1) / g + 1, per = kW4Cols / g;
+  const size_t n = (size_t)L.n_rt * L.n_kt * 256, ns = (size_t)L.n_rt * L.n_kt * per * 16;
   w4_pack_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(weights, (uint32_t*)L.tiles, L.d.d_out, L.d.d_in, L.n_kt, n);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   w4_pack_scales_kernel<<<(unsigned)((ns + 255) / 256), 256, 0, st>>>(scales, zeros, L.scales, L.zeros, L.d.d_out,
-                                                                     groups, padded, ns);
+                                                                     groups, L.n_kt, per, ns);
   return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ product
 struct W4Args {
-  const uint4* tiles;
+  const u32x4_t* tiles;
   const uint16_t* scales;
   const uint8_t* zeros;
   const void* x;
   const float* x_scales;
   void* y;
   int64_t x_stride, y_stride;
-  int d_out, d_in, n_kt, batch, x_groups;   // x_groups: 0 for one scale per row, else scales per row
+  int d_out, d_in, n_kt, batch;
+  int x_groups;            // 0 for one scale per row, else scales per row
+  int y_dtype;
 };
+
+// x[k .. k + 7] of a row: rows start at any element, which 8- and 16-byte loads allow on gfx950.
+struct __attribute__((packed, aligned(2))) X16 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(1))) X8 { uint32_t w[2]; };
+
+struct Load16 {
+  typedef X16 X;
+  static __device__ __forceinline__ X load(const void* row, int k) { return *(const X16*)((const uint16_t*)row + k); }
+  // The same at the end of a row: zeros from d_in on.
+  static __device__ __forceinline__ X load_end(const void* row, int k, int d_in) {
+    if (k + 8 <= d_in) return load(row, k);
+    X16 r = {{0, 0, 0, 0}};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < d_in) r.w[i / 2] |= (uint32_t)((const uint16_t*)row)[k + i] << (16 * (i % 2));
+    return r;
+  }
+};
+struct Load8 {
+  typedef X8 X;
+  static __device__ __forceinline__ X load(const void* row, int k) { return *(const X8*)((const uint8_t*)row + k); }
+  static __device__ __forceinline__ X load_end(const void* row, int k, int d_in) {
+    if (k + 8 <= d_in) return load(row, k);
+    X8 r = {{0, 0}};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < d_in) r.w[i / 4] |= (uint32_t)((const uint8_t*)row)[k + i] << (8 * (i % 4));
+    return r;
+  }
+};
+
+// Four e4m3 values as fp16.
+__device__ __forceinline__ uint2 widen_f8(uint32_t w) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(b.x, b.y));
+}
 
 // How each type of x meets the nibbles.
 template <int XT> struct Op;
-template <> struct Op<AQMB_F16> {
+struct F16Form {
   typedef f16x8_t V;
   typedef f32x4_t C;
   static constexpr float kZero = 16.f;
@@ -94,7 +135,7 @@ template <> struct Op<AQMB_F16> {
   }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
-template <> struct Op<AQMB_BF16> {
+template <> struct Op<AQMB_BF16> : Load16 {
   typedef bf16x8_t V;
   typedef f32x4_t C;
   static constexpr float kZero = 16.f;
@@ -105,10 +146,19 @@ template <> struct Op<AQMB_BF16> {
   static __device__ __forceinline__ V ones() {
     return __builtin_bit_cast(V, u32x4_t{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
   }
+  static __device__ __forceinline__ V operand(X x) { return __builtin_bit_cast(V, x); }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
-template <> struct Op<AQMB_F8> : Op<AQMB_F16> {};
-template <> struct Op<AQMB_I8> {
+template <> struct Op<AQMB_F16> : F16Form, Load16 {
+  static __device__ __forceinline__ V operand(X x) { return __builtin_bit_cast(V, x); }
+};
+template <> struct Op<AQMB_F8> : F16Form, Load8 {
+  static __device__ __forceinline__ V operand(X x) {
+    const uint2 a = widen_f8(x.w[0]), b = widen_f8(x.w[1]);
+    return __builtin_bit_cast(V, u32x4_t{a.x, a.y, b.x, b.y});
+  }
+};
+template <> struct Op<AQMB_I8> : Load8 {
   typedef long V;
   typedef i32x4_t C;
   static __device__ __forceinline__ V weights(uint32_t w) {
@@ -116,170 +166,160 @@ template <> struct Op<AQMB_I8> {
     return (long)((uint64_t)((w >> 4) & m) << 32 | (w & m));
   }
   static __device__ __forceinline__ V ones() { return 0x0101010101010101l; }
+  // The masks leave weights 0, 4, 1, 5 and 2, 6, 3, 7; x has to follow.
+  static __device__ __forceinline__ V operand(X x) {
+    const uint32_t lo = __builtin_amdgcn_perm(x.w[1], x.w[0], 0x05010400u);
+    const uint32_t hi = __builtin_amdgcn_perm(x.w[1], x.w[0], 0x07030602u);
+    return (long)((uint64_t)hi << 32 | lo);
+  }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0); }
 };
 
-struct __attribute__((packed, aligned(2))) X16 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(1))) X8 { uint32_t w[2]; };
+// The scales (fp16) and zero points (uint8) that a lane needs of a tile: 4 rows of every group.
+template <int N> struct Piece;
+template <> struct Piece<4> { uint2 s; uint32_t z; };
+template <> struct Piece<8> { u32x4_t s; uint2 z; };
+template <> struct Piece<16> { u32x4_t s, s2; u32x4_t z; };
 
-// Four e4m3 values as fp16.
-__device__ __forceinline__ uint2 widen_f8(uint32_t w) {
-  typedef float f32x2_t __attribute__((ext_vector_type(2)));
-  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  return make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(b.x, b.y));
-}
-
-// x[k .. k + 7] of one row as an operand, zeros from d_in on. x of 16 bits (and e4m3, widened) is used
-// in its own order: the nibbles were laid out for it. The int8 masks leave bytes 0, 4, 1, 5 and 2, 6, 3, 7.
-template <int XT>
-__device__ __forceinline__ typename Op<XT>::V load_x(const void* row, int k, int d_in) {
-  typedef typename Op<XT>::V V;
-  if constexpr (XT == AQMB_F16 || XT == AQMB_BF16) {
-    const uint16_t* p = (const uint16_t*)row + k;
-    X16 r = {{0, 0, 0, 0}};
-    if (k + 8 <= d_in) {
-      r = *(const X16*)p;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < d_in) r.w[i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
-    }
-    return __builtin_bit_cast(V, r);
-  } else {
-    const uint8_t* p = (const uint8_t*)row + k;
-    X8 r = {{0, 0}};
-    if (k + 8 <= d_in) {
-      r = *(const X8*)p;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < d_in) r.w[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
-    }
-    if constexpr (XT == AQMB_F8) {
-      const uint2 a = widen_f8(r.w[0]), b = widen_f8(r.w[1]);
-      return __builtin_bit_cast(V, u32x4_t{a.x, a.y, b.x, b.y});
-    } else {
-      const uint32_t lo = __builtin_amdgcn_perm(r.w[1], r.w[0], 0x05010400u);
-      const uint32_t hi = __builtin_amdgcn_perm(r.w[1], r.w[0], 0x07030602u);
-      return (V)((uint64_t)hi << 32 | lo);
-    }
-  }
-}
-
-// A workgroup of W waves takes R tiles of 16 rows; wave w takes the input tiles w, w + W, ... and the
-// waves' sums meet in LDS. G: the group size.
-template <int XT, int YT, int G, int R, int W>
+// A workgroup of W waves takes one tile of 16 rows; wave w takes the input tiles w, w + W, ... and the
+// waves' sums meet in LDS. kAhead tiles (weights, scales and x) are under way at any time: a row tile
+// is read by few waves, so the bytes in flight come from depth. G: the group size.
+template <int XT, int G, int W>
 __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   typedef Op<XT> O;
   typedef typename O::C C;
-  constexpr int kSteps = G / 32, kGroups = kW4Cols / G;
-  __shared__ float part[W][R][16][17];
+  constexpr bool kWide = XT == AQMB_F16 || XT == AQMB_BF16;
+  constexpr int kSteps = G / 32, kGroups = kW4Cols / G, kAhead = W == 16 || G == 32 ? 2 : 4;
+  __shared__ float part[W][16][17];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int n = lane % 16, q = lane / 16;
   const int col = n < a.batch ? n : a.batch - 1;     // the columns past the batch repeat its last row
-  const char* xr = (const char*)a.x + (int64_t)col * a.x_stride * (XT == AQMB_F16 || XT == AQMB_BF16 ? 2 : 1);
+  const char* xr = (const char*)a.x + (int64_t)col * a.x_stride * (kWide ? 2 : 1);
   const float* xs = a.x_scales && a.x_groups ? a.x_scales + (int64_t)col * a.x_groups : nullptr;
-  const int n_rt = (a.d_out + kW4Rows - 1) / kW4Rows;
-  const int rt0 = blockIdx.x * R;
-  const size_t tile_pitch = (size_t)a.n_kt * 64;
+  const size_t tile0 = (size_t)blockIdx.x * a.n_kt;
 
-  float tot[R][4];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) tot[r][i] = 0.f;
-
-  for (int kt = wave; kt < a.n_kt; kt += W) {
-    uint4 w[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int rt = rt0 + r < n_rt ? rt0 + r : n_rt - 1;
-      w[r] = load_stream16(a.tiles + rt * tile_pitch + (size_t)kt * 64 + lane);
+  u32x4_t w[kAhead];
+  typename O::X x[kAhead][4];
+  Piece<4 * kGroups> sz[kAhead];
+  float sx[kAhead][kGroups];
+  auto fetch = [&](int u, int kt) {
+    const size_t tile = tile0 + kt;
+    w[u] = __builtin_nontemporal_load((const u32x4_t*)a.tiles + tile * 64 + lane);
+    const size_t at = tile * (16 * kGroups) + 4 * kGroups * q;
+    if constexpr (kGroups == 1) {
+      sz[u].s = *(const uint2*)(a.scales + at);
+      sz[u].z = a.zeros ? *(const uint32_t*)(a.zeros + at) : 0x08080808u;
+    } else if constexpr (kGroups == 2) {
+      sz[u].s = *(const u32x4_t*)(a.scales + at);
+      sz[u].z = a.zeros ? *(const uint2*)(a.zeros + at) : make_uint2(0x08080808u, 0x08080808u);
+    } else {
+      sz[u].s = *(const u32x4_t*)(a.scales + at);
+      sz[u].s2 = *(const u32x4_t*)(a.scales + at + 8);
+      sz[u].z = a.zeros ? *(const u32x4_t*)(a.zeros + at) : u32x4_t{0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u};
     }
+    const int k = kt * kW4Cols + 8 * q;
+    if (kt * kW4Cols + kW4Cols <= a.d_in) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x[u][d] = O::load(xr, k + 32 * d);
+    } else {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x[u][d] = O::load_end(xr, k + 32 * d, a.d_in);
+    }
+    // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      C acc[R], ax;
+      sx[u][g] = 1.f;
+      if constexpr (!kWide)
+        if (xs) sx[u][g] = xs[min(kt * kGroups + g, a.x_groups - 1)];
+    }
+  };
+
+  float tot[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ax[i] = 0;
+  for (int u = 0; u < kAhead; ++u)
+    if (wave + u * W < a.n_kt) fetch(u, wave + u * W);
+  for (int kt0 = wave; kt0 < a.n_kt; kt0 += kAhead * W) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) acc[r] = ax;
+    for (int u = 0; u < kAhead; ++u) {
+      const int kt = kt0 + u * W;
+      if (kt >= a.n_kt) break;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int d = g * kSteps + s;
-        const typename O::V x = load_x<XT>(xr, kt * kW4Cols + 32 * d + 8 * q, a.d_in);
-        ax = O::mul(O::ones(), x, ax);
+      for (int g = 0; g < kGroups; ++g) {
+        C acc, ax;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const uint32_t dw = d == 0 ? w[r].x : d == 1 ? w[r].y : d == 2 ? w[r].z : w[r].w;
-          acc[r] = O::mul(O::weights(dw), x, acc[r]);
+        for (int i = 0; i < 4; ++i) acc[i] = ax[i] = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const typename O::V v = O::operand(x[u][g * kSteps + s]);
+          ax = O::mul(O::ones(), v, ax);
+          acc = O::mul(O::weights(w[u][g * kSteps + s]), v, acc);
         }
-      }
-      // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
-      const int gi = kt * kGroups + g;
-      const float sx = xs && gi < a.x_groups ? xs[gi] : 1.f;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int rt = rt0 + r < n_rt ? rt0 + r : n_rt - 1;
-        const size_t at = ((size_t)rt * a.n_kt * kGroups + gi) * 16 + 4 * q;
-        const uint2 sw = *(const uint2*)(a.scales + at);
-        const uint32_t zw = a.zeros ? *(const uint32_t*)(a.zeros + at) : 0x08080808u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float s = f16_to_f32((i < 2 ? sw.x : sw.y) >> (16 * (i % 2)) & 0xFFFFu);
-          if constexpr (XT == AQMB_I8) {
-            const int z = (int)((zw >> (8 * i)) & 0xFFu);
-            tot[r][i] += (s * sx) * (float)(acc[r][i] - z * ax[i]);
+          const int e = 4 * g + i;                     // of the lane's piece
+          uint32_t sw, zw;
+          if constexpr (kGroups == 1) {
+            sw = e < 2 ? sz[u].s.x : sz[u].s.y;
+            zw = sz[u].z;
+          } else if constexpr (kGroups == 2) {
+            sw = sz[u].s[e / 2];
+            zw = e < 4 ? sz[u].z.x : sz[u].z.y;
           } else {
-            const float z = (float)((zw >> (8 * i)) & 0xFFu) + O::kZero;
-            tot[r][i] += (s * sx) * (acc[r][i] - z * ax[i]);
+            sw = e < 8 ? sz[u].s[e / 2] : sz[u].s2[e / 2 - 4];
+            zw = sz[u].z[e / 4];
           }
+          float s = e % 2 ? f16hi(sw) : f16lo(sw);
+          if constexpr (!kWide) s *= sx[u][g];
+          const int z = (int)((zw >> (8 * i)) & 0xFFu);
+          if constexpr (XT == AQMB_I8) tot[i] += s * (float)(acc[i] - z * ax[i]);
+          else tot[i] += s * (acc[i] - ((float)z + O::kZero) * ax[i]);
         }
       }
+      if (kt + kAhead * W < a.n_kt) fetch(u, kt + kAhead * W);
     }
   }
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][r][4 * q + i][n] = tot[r][i];
+  for (int i = 0; i < 4; ++i) part[wave][4 * q + i][n] = tot[i];
   __syncthreads();
-  for (int e = threadIdx.x; e < R * 256; e += 64 * W) {
-    const int row = e % 16, b = e / 16 % 16, r = e / 256;
-    const int out = (rt0 + r) * kW4Rows + row;
+  for (int e = threadIdx.x; e < 256; e += 64 * W) {
+    const int row = e % 16, b = e / 16, out = blockIdx.x * kW4Rows + row;
     if (b >= a.batch || out >= a.d_out) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) v += part[k][r][row][b];
+    for (int k = 0; k < W; ++k) v += part[k][row][b];
     if (a.x_scales && !a.x_groups) v *= a.x_scales[b];
-    OutT<YT>::store(a.y, (size_t)b * a.y_stride + out, v);
+    const size_t at = (size_t)b * a.y_stride + out;
+    if (a.y_dtype == AQMB_F16) OutT<AQMB_F16>::store(a.y, at, v);
+    else if (a.y_dtype == AQMB_BF16) OutT<AQMB_BF16>::store(a.y, at, v);
+    else OutT<AQMB_F32>::store(a.y, at, v);
   }
 }
 
-template <int XT, int YT, int G>
-static hipError_t go(const W4Args& a, hipStream_t st) {
-  const int n_rt = (a.d_out + kW4Rows - 1) / kW4Rows;
-  w4_kernel<XT, YT, G, 1, 4><<<n_rt, 256, 0, st>>>(a);
+template <int XT, int G>
+static hipError_t go(const W4Args& a, int n_cu, hipStream_t st) {
+  const int n_rt = (a.d_out - 1) / kW4Rows + 1;
+  // Waves per row tile: enough for 16 waves on every compute unit, never more than input tiles.
+  const int want = (16 * n_cu + n_rt - 1) / n_rt;
+  if (want > 8 && a.n_kt > 8) w4_kernel<XT, G, 16><<<n_rt, 1024, 0, st>>>(a);
+  else if (want > 4 && a.n_kt > 4) w4_kernel<XT, G, 8><<<n_rt, 512, 0, st>>>(a);
+  else w4_kernel<XT, G, 4><<<n_rt, 256, 0, st>>>(a);
   return hipGetLastError();
 }
-template <int XT, int YT>
-static hipError_t by_group(const W4Args& a, int g, hipStream_t st) {
-  return g == 32 ? go<XT, YT, 32>(a, st) : g == 64 ? go<XT, YT, 64>(a, st) : go<XT, YT, 128>(a, st);
-}
 template <int XT>
-static hipError_t by_out(const W4Args& a, int g, aqmb_dtype yt, hipStream_t st) {
-  return yt == AQMB_F16 ? by_group<XT, AQMB_F16>(a, g, st) : yt == AQMB_BF16 ? by_group<XT, AQMB_BF16>(a, g, st)
-                                                                            : by_group<XT, AQMB_F32>(a, g, st);
+static hipError_t by_group(const W4Args& a, int g, int n_cu, hipStream_t st) {
+  return g == 32 ? go<XT, 32>(a, n_cu, st) : g == 64 ? go<XT, 64>(a, n_cu, st) : go<XT, 128>(a, n_cu, st);
 }
 
 hipError_t launch_w4_gemv(const W4& L, const void* x, aqmb_dtype x_dtype, int64_t x_stride, const float* x_scales,
                           int x_scale_group, int batch, void* y, aqmb_dtype y_dtype, int64_t y_stride, hipStream_t st) {
   const int g = L.d.group_size;
-  W4Args a = {(const uint4*)L.tiles, L.scales, L.zeros, x, x_scales, y, x_stride, y_stride,
-              L.d.d_out, L.d.d_in, L.n_kt, batch, x_scale_group ? (L.d.d_in + g - 1) / g : 0};
+  W4Args a = {(const u32x4_t*)L.tiles, L.scales, L.zeros, x, x_scales, y, x_stride, y_stride,
+              L.d.d_out, L.d.d_in, L.n_kt, batch, x_scale_group ? (L.d.d_in - 1) / g + 1 : 0, (int)y_dtype};
   switch (x_dtype) {
-    case AQMB_F16: return by_out<AQMB_F16>(a, g, y_dtype, st);
-    case AQMB_BF16: return by_out<AQMB_BF16>(a, g, y_dtype, st);
-    case AQMB_F8: return by_out<AQMB_F8>(a, g, y_dtype, st);
-    default: return by_out<AQMB_I8>(a, g, y_dtype, st);
+    case AQMB_F16: return by_group<AQMB_F16>(a, g, L.n_cu, st);
+    case AQMB_BF16: return by_group<AQMB_BF16>(a, g, L.n_cu, st);
+    case AQMB_F8: return by_group<AQMB_F8>(a, g, L.n_cu, st);
+    default: return by_group<AQMB_I8>(a, g, L.n_cu, st);
   }
 }
 

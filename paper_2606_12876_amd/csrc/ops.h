@@ -30,7 +30,7 @@ struct W4 {
   int device, n_cu;
   int n_rt, n_kt;          // row tiles, input tiles
   unsigned char* tiles;    // [n_rt][n_kt][1024]
-  uint16_t* scales;        // [n_rt][n_kt * 128 / g][16] fp16, 0 in the padding
+  uint16_t* scales;        // [n_rt][n_kt][4 rows / 4][128 / g][4] fp16, 0 in the padding
   unsigned char* zeros;    // the same shape, or null (8 everywhere)
 };
 constexpr uint32_t kW4Magic = 0x41513457u;
