@@ -15,6 +15,8 @@
 // bits (measured: 1.1e-4 of the result at 4096 x 4096).
 // so a dword of eight weights costs 3 (int8) or 8 vector instructions. sum x is a second product with a row
 // of ones: it arrives in every lane that needs it, with the same grouping and order of sums.
+#include <type_traits>
+
 #include "device.h"
 #include "ops.h"
 
@@ -83,35 +85,33 @@ struct W4Args {
   int y_dtype;
 };
 
-// x[k .. k + 7] of a row: rows start at any element, which 8- and 16-byte loads allow on gfx950.
-struct __attribute__((packed, aligned(2))) X16 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(1))) X8 { uint32_t w[2]; };
+// 16 bytes of a row of x from element k on: rows start at any element, which 16-byte loads allow on gfx950.
+struct __attribute__((packed, aligned(1))) Bytes16 { uint64_t lo, hi; };
 
-struct Load16 {
-  typedef X16 X;
-  static __device__ __forceinline__ X load(const void* row, int k) { return *(const X16*)((const uint16_t*)row + k); }
-  // The same at the end of a row: zeros from d_in on.
-  static __device__ __forceinline__ X load_end(const void* row, int k, int d_in) {
-    if (k + 8 <= d_in) return load(row, k);
-    X16 r = {{0, 0, 0, 0}};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k + i < d_in) r.w[i / 2] |= (uint32_t)((const uint16_t*)row)[k + i] << (16 * (i % 2));
-    return r;
+// The same at the end of a row, zeros from element d_in on: the row's last 16 bytes, moved down by
+// those that lie before k.
+template <typename E>
+__device__ __forceinline__ Bytes16 load_end(const E* row, int k, int d_in) {
+  constexpr int kN = 16 / sizeof(E);
+  Bytes16 v = {0, 0};
+  if (k >= d_in) return v;
+  if (d_in < kN) {                                    // k = 0: the whole row
+#pragma unroll 1
+    for (int i = 0; i < d_in; ++i) {
+      const uint64_t e = row[i];
+      const int s = 8 * (int)sizeof(E) * i;
+      if (s < 64) v.lo |= e << s;
+      else v.hi |= e << (s - 64);
+    }
+    return v;
   }
-};
-struct Load8 {
-  typedef X8 X;
-  static __device__ __forceinline__ X load(const void* row, int k) { return *(const X8*)((const uint8_t*)row + k); }
-  static __device__ __forceinline__ X load_end(const void* row, int k, int d_in) {
-    if (k + 8 <= d_in) return load(row, k);
-    X8 r = {{0, 0}};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k + i < d_in) r.w[i / 4] |= (uint32_t)((const uint8_t*)row)[k + i] << (8 * (i % 4));
-    return r;
-  }
-};
+  const int past = max(k - (d_in - kN), 0) * (int)sizeof(E);      // 0..15 bytes
+  v = *(const Bytes16*)(row + min(k, d_in - kN));
+  const int s = 8 * (past % 8);
+  if (past >= 8) v = {v.hi, 0};
+  if (s) v = {v.lo >> s | v.hi << (64 - s), v.hi >> s};
+  return v;
+}
 
 // Four e4m3 values as fp16.
 __device__ __forceinline__ uint2 widen_f8(uint32_t w) {
@@ -120,12 +120,12 @@ __device__ __forceinline__ uint2 widen_f8(uint32_t w) {
   return make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(b.x, b.y));
 }
 
-// How each type of x meets the nibbles.
+// How each type of x meets the nibbles. X: 8 neighbouring inputs of one row.
 template <int XT> struct Op;
 struct F16Form {
   typedef f16x8_t V;
   typedef f32x4_t C;
-  static constexpr float kZero = 16.f;
+  static constexpr int kZero = 16;
   static __device__ __forceinline__ V weights(uint32_t w) {
     const uint32_t m = 0x03C003C0u, o = 0x4C004C00u;
     return __builtin_bit_cast(V, u32x4_t{((w << 6) & m) | o, ((w << 2) & m) | o, ((w >> 2) & m) | o, ((w >> 6) & m) | o});
@@ -135,10 +135,22 @@ struct F16Form {
   }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
-template <> struct Op<AQMB_BF16> : Load16 {
+template <> struct Op<AQMB_F16> : F16Form {
+  typedef u32x4_t X;
+  static __device__ __forceinline__ V operand(X x) { return __builtin_bit_cast(V, x); }
+};
+template <> struct Op<AQMB_F8> : F16Form {
+  typedef uint2 X;
+  static __device__ __forceinline__ V operand(X x) {
+    const uint2 a = widen_f8(x.x), b = widen_f8(x.y);
+    return __builtin_bit_cast(V, u32x4_t{a.x, a.y, b.x, b.y});
+  }
+};
+template <> struct Op<AQMB_BF16> {
+  typedef u32x4_t X;
   typedef bf16x8_t V;
   typedef f32x4_t C;
-  static constexpr float kZero = 16.f;
+  static constexpr int kZero = 16;
   static __device__ __forceinline__ V weights(uint32_t w) {
     const uint32_t m = 0x00780078u, o = 0x41804180u;
     return __builtin_bit_cast(V, u32x4_t{((w << 3) & m) | o, ((w >> 1) & m) | o, ((w >> 5) & m) | o, ((w >> 9) & m) | o});
@@ -149,18 +161,11 @@ template <> struct Op<AQMB_BF16> : Load16 {
   static __device__ __forceinline__ V operand(X x) { return __builtin_bit_cast(V, x); }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
-template <> struct Op<AQMB_F16> : F16Form, Load16 {
-  static __device__ __forceinline__ V operand(X x) { return __builtin_bit_cast(V, x); }
-};
-template <> struct Op<AQMB_F8> : F16Form, Load8 {
-  static __device__ __forceinline__ V operand(X x) {
-    const uint2 a = widen_f8(x.w[0]), b = widen_f8(x.w[1]);
-    return __builtin_bit_cast(V, u32x4_t{a.x, a.y, b.x, b.y});
-  }
-};
-template <> struct Op<AQMB_I8> : Load8 {
+template <> struct Op<AQMB_I8> {
+  typedef uint2 X;
   typedef long V;
   typedef i32x4_t C;
+  static constexpr int kZero = 0;
   static __device__ __forceinline__ V weights(uint32_t w) {
     const uint32_t m = 0x0F0F0F0Fu;
     return (long)((uint64_t)((w >> 4) & m) << 32 | (w & m));
@@ -168,8 +173,8 @@ template <> struct Op<AQMB_I8> : Load8 {
   static __device__ __forceinline__ V ones() { return 0x0101010101010101l; }
   // The masks leave weights 0, 4, 1, 5 and 2, 6, 3, 7; x has to follow.
   static __device__ __forceinline__ V operand(X x) {
-    const uint32_t lo = __builtin_amdgcn_perm(x.w[1], x.w[0], 0x05010400u);
-    const uint32_t hi = __builtin_amdgcn_perm(x.w[1], x.w[0], 0x07030602u);
+    const uint32_t lo = __builtin_amdgcn_perm(x.y, x.x, 0x05010400u);
+    const uint32_t hi = __builtin_amdgcn_perm(x.y, x.x, 0x07030602u);
     return (long)((uint64_t)hi << 32 | lo);
   }
   static __device__ __forceinline__ C mul(V a, V b, C c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0); }
@@ -177,107 +182,132 @@ template <> struct Op<AQMB_I8> : Load8 {
 
 // The scales (fp16) and zero points (uint8) that a lane needs of a tile: 4 rows of every group.
 template <int N> struct Piece;
-template <> struct Piece<4> { uint2 s; uint32_t z; };
-template <> struct Piece<8> { u32x4_t s; uint2 z; };
-template <> struct Piece<16> { u32x4_t s, s2; u32x4_t z; };
+template <> struct Piece<4> {
+  uint2 s; uint32_t z;
+  __device__ __forceinline__ uint32_t scale(int e) const { return e < 2 ? s.x : s.y; }
+  __device__ __forceinline__ uint32_t zero(int) const { return z; }
+};
+template <> struct Piece<8> {
+  u32x4_t s; uint2 z;
+  __device__ __forceinline__ uint32_t scale(int e) const { return s[e / 2]; }
+  __device__ __forceinline__ uint32_t zero(int e) const { return e < 4 ? z.x : z.y; }
+};
+template <> struct Piece<16> {
+  u32x4_t s, s2; u32x4_t z;
+  __device__ __forceinline__ uint32_t scale(int e) const { return e < 8 ? s[e / 2] : s2[e / 2 - 4]; }
+  __device__ __forceinline__ uint32_t zero(int e) const { return z[e / 4]; }
+};
 
-// A workgroup of W waves takes one tile of 16 rows; wave w takes the input tiles w, w + W, ... and the
-// waves' sums meet in LDS. kAhead tiles (weights, scales and x) are under way at any time: a row tile
-// is read by few waves, so the bytes in flight come from depth. G: the group size.
+// A workgroup of W waves takes one tile of 16 rows; wave w takes the input tiles w, w + W, ..., the next
+// one under way while it works on one, and the waves' sums meet in LDS. G: the group size.
+//
+// x is read by rows (16 bytes a lane, neighbouring lanes neighbouring bytes) and brought into operand
+// order through LDS: loads in operand order would have every lane on a row of its own, which costs the
+// address unit a cycle a lane (4096 x 11008 at 16 rows of int8: 15 us so, of which the loads of x were 5).
+// The 16-byte chunks of a row are stored at their number xor the row's, so that reads of 16 rows at
+// one chunk spread over all banks. The code is one small loop: a launch runs it once or a few times per
+// wave, and its first pass is fetched cold.
 template <int XT, int G, int W>
 __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   typedef Op<XT> O;
   typedef typename O::C C;
-  constexpr bool kWide = XT == AQMB_F16 || XT == AQMB_BF16;
-  constexpr int kSteps = G / 32, kGroups = kW4Cols / G, kAhead = W == 16 || G == 32 ? 2 : 4;
-  __shared__ float part[W][16][17];
+  typedef typename std::conditional<XT == AQMB_F16 || XT == AQMB_BF16, uint16_t, uint8_t>::type E;
+  constexpr bool kWide = sizeof(E) == 2;
+  constexpr int kSteps = G / 32, kGroups = kW4Cols / G;
+  constexpr int kChunks = kW4Cols * (int)sizeof(E) / 16, kRows = 64 / kChunks, kLoads = 16 / kRows;
+  constexpr int kSlab = 16 * kChunks * 16;              // bytes of x a wave holds in LDS
+  constexpr int kPart = 16 * 17 * 4;                    // bytes of its sums, in the same place afterwards
+  __shared__ __attribute__((aligned(16))) unsigned char lds[W * (kSlab > kPart ? kSlab : kPart)];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int n = lane % 16, q = lane / 16;
-  const int col = n < a.batch ? n : a.batch - 1;     // the columns past the batch repeat its last row
-  const char* xr = (const char*)a.x + (int64_t)col * a.x_stride * (kWide ? 2 : 1);
-  const float* xs = a.x_scales && a.x_groups ? a.x_scales + (int64_t)col * a.x_groups : nullptr;
+  unsigned char* slab = lds + wave * kSlab;
+  const float* xs = a.x_scales && a.x_groups ? a.x_scales + (int64_t)min(n, a.batch - 1) * a.x_groups : nullptr;
   const size_t tile0 = (size_t)blockIdx.x * a.n_kt;
 
-  u32x4_t w[kAhead];
-  typename O::X x[kAhead][4];
-  Piece<4 * kGroups> sz[kAhead];
-  float sx[kAhead][kGroups];
-  auto fetch = [&](int u, int kt) {
-    const size_t tile = tile0 + kt;
-    w[u] = __builtin_nontemporal_load((const u32x4_t*)a.tiles + tile * 64 + lane);
-    const size_t at = tile * (16 * kGroups) + 4 * kGroups * q;
-    if constexpr (kGroups == 1) {
-      sz[u].s = *(const uint2*)(a.scales + at);
-      sz[u].z = a.zeros ? *(const uint32_t*)(a.zeros + at) : 0x08080808u;
-    } else if constexpr (kGroups == 2) {
-      sz[u].s = *(const u32x4_t*)(a.scales + at);
-      sz[u].z = a.zeros ? *(const uint2*)(a.zeros + at) : make_uint2(0x08080808u, 0x08080808u);
-    } else {
-      sz[u].s = *(const u32x4_t*)(a.scales + at);
-      sz[u].s2 = *(const u32x4_t*)(a.scales + at + 8);
-      sz[u].z = a.zeros ? *(const u32x4_t*)(a.zeros + at) : u32x4_t{0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u};
-    }
-    const int k = kt * kW4Cols + 8 * q;
-    if (kt * kW4Cols + kW4Cols <= a.d_in) {
+  // This lane's part of the loads of x: row lane / kChunks (+ kRows per load), chunk lane % kChunks.
+  Bytes16 x[kLoads];
+  auto load_x = [&](int kt) {
+    const int k = kt * kW4Cols + lane % kChunks * (16 / (int)sizeof(E));
 #pragma unroll
-      for (int d = 0; d < 4; ++d) x[u][d] = O::load(xr, k + 32 * d);
-    } else {
-#pragma unroll
-      for (int d = 0; d < 4; ++d) x[u][d] = O::load_end(xr, k + 32 * d, a.d_in);
+    for (int i = 0; i < kLoads; ++i) {
+      if (i * kRows >= a.batch) continue;
+      const E* row = (const E*)a.x + (int64_t)min(i * kRows + lane / kChunks, a.batch - 1) * a.x_stride;
+      x[i] = (kt + 1) * kW4Cols <= a.d_in ? *(const Bytes16*)(row + k) : load_end(row, k, a.d_in);
     }
-    // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      sx[u][g] = 1.f;
-      if constexpr (!kWide)
-        if (xs) sx[u][g] = xs[min(kt * kGroups + g, a.x_groups - 1)];
-    }
+  };
+  auto load_piece = [&](int kt) {
+    Piece<4 * kGroups> p;
+    const size_t at = (tile0 + kt) * (16 * kGroups) + 4 * kGroups * q;
+    typedef decltype(p.z) Z;
+    p.s = *(const decltype(p.s)*)(a.scales + at);
+    if constexpr (kGroups == 4) p.s2 = *(const u32x4_t*)(a.scales + at + 8);
+    if (a.zeros) p.z = *(const Z*)(a.zeros + at);
+    else __builtin_memset(&p.z, 8, sizeof p.z);
+    return p;
   };
 
   float tot[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u)
-    if (wave + u * W < a.n_kt) fetch(u, wave + u * W);
-  for (int kt0 = wave; kt0 < a.n_kt; kt0 += kAhead * W) {
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int kt = kt0 + u * W;
-      if (kt >= a.n_kt) break;
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        C acc, ax;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = ax[i] = 0;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const typename O::V v = O::operand(x[u][g * kSteps + s]);
-          ax = O::mul(O::ones(), v, ax);
-          acc = O::mul(O::weights(w[u][g * kSteps + s]), v, acc);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 4 * g + i;                     // of the lane's piece
-          uint32_t sw, zw;
-          if constexpr (kGroups == 1) {
-            sw = e < 2 ? sz[u].s.x : sz[u].s.y;
-            zw = sz[u].z;
-          } else if constexpr (kGroups == 2) {
-            sw = sz[u].s[e / 2];
-            zw = e < 4 ? sz[u].z.x : sz[u].z.y;
-          } else {
-            sw = e < 8 ? sz[u].s[e / 2] : sz[u].s2[e / 2 - 4];
-            zw = sz[u].z[e / 4];
-          }
-          float s = e % 2 ? f16hi(sw) : f16lo(sw);
-          if constexpr (!kWide) s *= sx[u][g];
-          const int z = (int)((zw >> (8 * i)) & 0xFFu);
-          if constexpr (XT == AQMB_I8) tot[i] += s * (float)(acc[i] - z * ax[i]);
-          else tot[i] += s * (acc[i] - ((float)z + O::kZero) * ax[i]);
-        }
-      }
-      if (kt + kAhead * W < a.n_kt) fetch(u, kt + kAhead * W);
-    }
+  u32x4_t w = {0, 0, 0, 0};
+  Piece<4 * kGroups> piece;
+  if (wave < a.n_kt) {
+    w = __builtin_nontemporal_load(a.tiles + (tile0 + wave) * 64 + lane);
+    load_x(wave);
+    piece = load_piece(wave);
   }
+#pragma unroll 1
+  for (int kt = wave; kt < a.n_kt; kt += W) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (i * kRows >= a.batch) continue;
+      const int row = i * kRows + lane / kChunks;
+      *(u32x4_t*)(slab + (row * kChunks + (lane % kChunks ^ row % kChunks)) * 16) = __builtin_bit_cast(u32x4_t, x[i]);
+    }
+    // Lanes read what others of the wave wrote; LDS serves a wave's accesses in order.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const bool more = kt + W < a.n_kt;
+    u32x4_t w2 = w;
+    Piece<4 * kGroups> piece2 = piece;
+    if (more) {
+      w2 = __builtin_nontemporal_load(a.tiles + (tile0 + kt + W) * 64 + lane);
+      load_x(kt + W);
+      piece2 = load_piece(kt + W);
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      // Rows of the slab past the batch hold anything: columns of the product that nobody reads.
+      typename O::V v[kSteps];
+      C ax = {0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int byte = (32 * (g * kSteps + s) + 8 * q) * (int)sizeof(E);
+        v[s] = O::operand(*(const typename O::X*)(slab + (n * kChunks + (byte / 16 ^ n % kChunks)) * 16 + byte % 16));
+        ax = O::mul(O::ones(), v[s], ax);
+      }
+      C acc = ax * -O::kZero;                            // the operands' offset, off before the products come
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) acc = O::mul(O::weights(w[g * kSteps + s]), v[s], acc);
+      // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
+      float sx = 1.f;
+      if constexpr (!kWide)
+        if (xs) sx = xs[min(kt * kGroups + g, a.x_groups - 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = 4 * g + i;                         // of the lane's piece
+        const float s = e % 2 ? f16hi(piece.scale(e)) : f16lo(piece.scale(e));
+        const uint32_t z = (piece.zero(e) >> (8 * i)) & 0xFFu;
+        float p;
+        if constexpr (XT == AQMB_I8) p = (float)(acc[i] - (int)z * ax[i]);
+        else p = acc[i] - (float)z * ax[i];
+        if constexpr (!kWide) p *= sx;
+        tot[i] += s * p;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    w = w2;
+    piece = piece2;
+  }
+  __syncthreads();                                       // the slabs become the waves' sums
+  float (*part)[16][17] = (float (*)[16][17])lds;
 #pragma unroll
   for (int i = 0; i < 4; ++i) part[wave][4 * q + i][n] = tot[i];
   __syncthreads();
