@@ -56,7 +56,8 @@ __global__ void w4_pack_scales_kernel(const uint16_t* s, const uint8_t* z, uint1
   const int row = (int)(tile / n_kt) * kW4Rows + e / (4 * per) * 4 + e % 4, g = (int)(tile % n_kt) * per + e / 4 % per;
   const bool in = row < d_out && g < groups;
   so[i] = in ? s[(size_t)row * groups + g] : 0;
-  if (zo) zo[i] = in ? z[(size_t)row * groups + g] : 0;
+  if (z) zo[i] = in ? z[(size_t)row * groups + g] : 0;
+  else if (i < 16 * per) zo[i] = 8;                    // one tile's
 }
 
 hipError_t launch_w4_pack(const W4& L, const uint8_t* weights, const uint16_t* scales, const uint8_t* zeros,
@@ -76,12 +77,13 @@ struct W4Args {
   const u32x4_t* tiles;
   const uint16_t* scales;
   const uint8_t* zeros;
+  size_t zero_pitch;       // from tile to tile; 0 where all are 8
   const void* x;
   const float* x_scales;
   void* y;
   int64_t x_stride, y_stride;
   int d_out, d_in, n_kt, batch;
-  int x_groups;            // 0 for one scale per row, else scales per row
+  int x_groups;            // scales of a row of x
   int y_dtype;
 };
 
@@ -198,79 +200,105 @@ template <> struct Piece<16> {
   __device__ __forceinline__ uint32_t zero(int e) const { return z[e / 4]; }
 };
 
-// A workgroup of W waves takes one tile of 16 rows; wave w takes the input tiles w, w + W, ..., the next
-// one under way while it works on one, and the waves' sums meet in LDS. G: the group size.
+// A workgroup of W waves takes R tiles of 16 rows, which share x and its sums; wave w takes the input
+// tiles w, w + W, ..., the next one under way while it works on one, and the waves' sums meet in LDS.
+// G: the group size.
 //
 // x is read by rows (16 bytes a lane, neighbouring lanes neighbouring bytes) and brought into operand
 // order through LDS: loads in operand order would have every lane on a row of its own, which costs the
 // address unit a cycle a lane (4096 x 11008 at 16 rows of int8: 15 us so, of which the loads of x were 5).
 // The 16-byte chunks of a row are stored at their number xor the row's, so that reads of 16 rows at
-// one chunk spread over all banks. The code is one small loop: a launch runs it once or a few times per
-// wave, and its first pass is fetched cold.
-template <int XT, int G, int W>
+// one chunk spread over all banks. What bounds the kernel is instructions more than bytes, most of all
+// those that a wave spends before its few turns of the loop: tile numbers are scalar, addresses of x
+// advance by one addition, the ragged last tile has code of its own.
+//
+// Loads of the next tile are straight code (a choice between two values of a register would have to wait
+// for both): the number of row loads NL is a parameter, symmetric layers have a piece of eights for zero
+// points, one scale per row is one group.
+template <int XT, int G, int R, int W, int NL>
 __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   typedef Op<XT> O;
   typedef typename O::C C;
   typedef typename std::conditional<XT == AQMB_F16 || XT == AQMB_BF16, uint16_t, uint8_t>::type E;
   constexpr bool kWide = sizeof(E) == 2;
   constexpr int kSteps = G / 32, kGroups = kW4Cols / G;
-  constexpr int kChunks = kW4Cols * (int)sizeof(E) / 16, kRows = 64 / kChunks, kLoads = 16 / kRows;
+  constexpr int kChunks = kW4Cols * (int)sizeof(E) / 16, kRows = 64 / kChunks;
   constexpr int kSlab = 16 * kChunks * 16;              // bytes of x a wave holds in LDS
-  constexpr int kPart = 16 * 17 * 4;                    // bytes of its sums, in the same place afterwards
+  constexpr int kPart = R * 16 * 17 * 4;                // bytes of its sums, in the same place afterwards
   __shared__ __attribute__((aligned(16))) unsigned char lds[W * (kSlab > kPart ? kSlab : kPart)];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int n = lane % 16, q = lane / 16;
   unsigned char* slab = lds + wave * kSlab;
-  const float* xs = a.x_scales && a.x_groups ? a.x_scales + (int64_t)min(n, a.batch - 1) * a.x_groups : nullptr;
-  const size_t tile0 = (size_t)blockIdx.x * a.n_kt;
+  const int rt0 = blockIdx.x * R, n_rt = (a.d_out - 1) / kW4Rows + 1;
+  size_t tile0[R];                                      // of the strip's row tiles; the last may repeat
+#pragma unroll
+  for (int r = 0; r < R; ++r) tile0[r] = (size_t)min(rt0 + r, n_rt - 1) * a.n_kt;
 
   // This lane's part of the loads of x: row lane / kChunks (+ kRows per load), chunk lane % kChunks.
-  Bytes16 x[kLoads];
-  auto load_x = [&](int kt) {
-    const int k = kt * kW4Cols + lane % kChunks * (16 / (int)sizeof(E));
+  const int k_lane = lane % kChunks * (16 / (int)sizeof(E));
+  const E* xp[NL];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      if (i * kRows >= a.batch) continue;
-      const E* row = (const E*)a.x + (int64_t)min(i * kRows + lane / kChunks, a.batch - 1) * a.x_stride;
-      x[i] = (kt + 1) * kW4Cols <= a.d_in ? *(const Bytes16*)(row + k) : load_end(row, k, a.d_in);
+  for (int i = 0; i < NL; ++i)
+    xp[i] = (const E*)a.x + (int64_t)min(i * kRows + lane / kChunks, a.batch - 1) * a.x_stride;
+  Bytes16 x[NL];
+  auto load_x = [&](int kt) {
+    if ((kt + 1) * kW4Cols <= a.d_in) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) x[i] = *(const Bytes16*)(xp[i] + (kt * kW4Cols + k_lane));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) x[i] = load_end(xp[i], kt * kW4Cols + k_lane, a.d_in);
     }
   };
-  auto load_piece = [&](int kt) {
+  const float* xs = kWide ? nullptr : a.x_scales + (int64_t)min(n, a.batch - 1) * a.x_groups;
+  struct Tile {
+    u32x4_t w;
     Piece<4 * kGroups> p;
-    const size_t at = (tile0 + kt) * (16 * kGroups) + 4 * kGroups * q;
-    typedef decltype(p.z) Z;
-    p.s = *(const decltype(p.s)*)(a.scales + at);
-    if constexpr (kGroups == 4) p.s2 = *(const u32x4_t*)(a.scales + at + 8);
-    if (a.zeros) p.z = *(const Z*)(a.zeros + at);
-    else __builtin_memset(&p.z, 8, sizeof p.z);
-    return p;
+  };
+  auto load_tile = [&](size_t tile) {
+    Tile t;
+    t.w = __builtin_nontemporal_load(a.tiles + tile * 64 + lane);
+    const uint16_t* s = a.scales + tile * (16 * kGroups);
+    t.p.s = *(const decltype(t.p.s)*)(s + 4 * kGroups * q);
+    if constexpr (kGroups == 4) t.p.s2 = *(const u32x4_t*)(s + 4 * kGroups * q + 8);
+    t.p.z = *(const decltype(t.p.z)*)(a.zeros + tile * a.zero_pitch + 4 * kGroups * q);
+    return t;
+  };
+  // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
+  float sx[kGroups], sx2[kGroups];
+  auto load_sx = [&](float* to, int kt) {
+    if constexpr (!kWide)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) to[g] = xs[min(kt * kGroups + g, a.x_groups - 1)];
   };
 
-  float tot[4] = {0.f, 0.f, 0.f, 0.f};
-  u32x4_t w = {0, 0, 0, 0};
-  Piece<4 * kGroups> piece;
+  float tot[R][4];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tot[r][i] = 0.f;
+  Tile cur[R];
   if (wave < a.n_kt) {
-    w = __builtin_nontemporal_load(a.tiles + (tile0 + wave) * 64 + lane);
+#pragma unroll
+    for (int r = 0; r < R; ++r) cur[r] = load_tile(tile0[r] + wave);
+    load_sx(sx, wave);
     load_x(wave);
-    piece = load_piece(wave);
   }
 #pragma unroll 1
   for (int kt = wave; kt < a.n_kt; kt += W) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      if (i * kRows >= a.batch) continue;
+    for (int i = 0; i < NL; ++i) {
       const int row = i * kRows + lane / kChunks;
       *(u32x4_t*)(slab + (row * kChunks + (lane % kChunks ^ row % kChunks)) * 16) = __builtin_bit_cast(u32x4_t, x[i]);
     }
     // Lanes read what others of the wave wrote; LDS serves a wave's accesses in order.
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const bool more = kt + W < a.n_kt;
-    u32x4_t w2 = w;
-    Piece<4 * kGroups> piece2 = piece;
-    if (more) {
-      w2 = __builtin_nontemporal_load(a.tiles + (tile0 + kt + W) * 64 + lane);
+    Tile next[R];
+    if (kt + W < a.n_kt) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) next[r] = load_tile(tile0[r] + kt + W);
+      load_sx(sx2, kt + W);
       load_x(kt + W);
-      piece2 = load_piece(kt + W);
     }
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
@@ -283,41 +311,44 @@ __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
         v[s] = O::operand(*(const typename O::X*)(slab + (n * kChunks + (byte / 16 ^ n % kChunks)) * 16 + byte % 16));
         ax = O::mul(O::ones(), v[s], ax);
       }
-      C acc = ax * -O::kZero;                            // the operands' offset, off before the products come
+      const C off = ax * -O::kZero;                      // the operands' offset, off before the products come
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) acc = O::mul(O::weights(w[g * kSteps + s]), v[s], acc);
-      // Groups from the last of d_in on have scale 0 and x 0; an x scale there does not exist.
-      float sx = 1.f;
-      if constexpr (!kWide)
-        if (xs) sx = xs[min(kt * kGroups + g, a.x_groups - 1)];
+      for (int r = 0; r < R; ++r) {
+        C acc = off;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int e = 4 * g + i;                         // of the lane's piece
-        const float s = e % 2 ? f16hi(piece.scale(e)) : f16lo(piece.scale(e));
-        const uint32_t z = (piece.zero(e) >> (8 * i)) & 0xFFu;
-        float p;
-        if constexpr (XT == AQMB_I8) p = (float)(acc[i] - (int)z * ax[i]);
-        else p = acc[i] - (float)z * ax[i];
-        if constexpr (!kWide) p *= sx;
-        tot[i] += s * p;
+        for (int s = 0; s < kSteps; ++s) acc = O::mul(O::weights(cur[r].w[g * kSteps + s]), v[s], acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 4 * g + i;                       // of the lane's piece
+          const float s = e % 2 ? f16hi(cur[r].p.scale(e)) : f16lo(cur[r].p.scale(e));
+          const uint32_t z = (cur[r].p.zero(e) >> (8 * i)) & 0xFFu;
+          float p;
+          if constexpr (XT == AQMB_I8) p = (float)(acc[i] - (int)z * ax[i]);
+          else p = acc[i] - (float)z * ax[i];
+          if constexpr (!kWide) p *= sx[g];
+          tot[r][i] += s * p;
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    w = w2;
-    piece = piece2;
+#pragma unroll
+    for (int r = 0; r < R; ++r) cur[r] = next[r];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) sx[g] = sx2[g];
   }
   __syncthreads();                                       // the slabs become the waves' sums
-  float (*part)[16][17] = (float (*)[16][17])lds;
+  float (*part)[R][16][17] = (float (*)[R][16][17])lds;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) part[wave][4 * q + i][n] = tot[i];
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][r][4 * q + i][n] = tot[r][i];
   __syncthreads();
-  for (int e = threadIdx.x; e < 256; e += 64 * W) {
-    const int row = e % 16, b = e / 16, out = blockIdx.x * kW4Rows + row;
+  for (int e = threadIdx.x; e < R * 256; e += 64 * W) {
+    const int row = e % 16, b = e / 16 % 16, r = e / 256, out = (rt0 + r) * kW4Rows + row;
     if (b >= a.batch || out >= a.d_out) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) v += part[k][row][b];
-    if (a.x_scales && !a.x_groups) v *= a.x_scales[b];
+    for (int k = 0; k < W; ++k) v += part[k][r][row][b];
     const size_t at = (size_t)b * a.y_stride + out;
     if (a.y_dtype == AQMB_F16) OutT<AQMB_F16>::store(a.y, at, v);
     else if (a.y_dtype == AQMB_BF16) OutT<AQMB_BF16>::store(a.y, at, v);
@@ -325,15 +356,24 @@ __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   }
 }
 
+#ifndef RW_R
+#define RW_R 1
+#define RW_W 8
+#endif
+template <int XT, int G, int R, int W>
+static hipError_t by_batch(const W4Args& a, hipStream_t st) {
+  constexpr bool kWide = XT == AQMB_F16 || XT == AQMB_BF16;
+  const int blocks = ((a.d_out - 1) / kW4Rows + R) / R;
+  if (a.batch <= (kWide ? 4 : 8)) w4_kernel<XT, G, R, W, 1><<<blocks, 64 * W, 0, st>>>(a);
+  else if (!kWide || a.batch <= 8) w4_kernel<XT, G, R, W, 2><<<blocks, 64 * W, 0, st>>>(a);
+  else if constexpr (kWide) w4_kernel<XT, G, R, W, 4><<<blocks, 64 * W, 0, st>>>(a);
+  return hipGetLastError();
+}
 template <int XT, int G>
 static hipError_t go(const W4Args& a, int n_cu, hipStream_t st) {
   const int n_rt = (a.d_out - 1) / kW4Rows + 1;
-  // Waves per row tile: enough for 16 waves on every compute unit, never more than input tiles.
-  const int want = (16 * n_cu + n_rt - 1) / n_rt;
-  if (want > 8 && a.n_kt > 8) w4_kernel<XT, G, 16><<<n_rt, 1024, 0, st>>>(a);
-  else if (want > 4 && a.n_kt > 4) w4_kernel<XT, G, 8><<<n_rt, 512, 0, st>>>(a);
-  else w4_kernel<XT, G, 4><<<n_rt, 256, 0, st>>>(a);
-  return hipGetLastError();
+  if (n_rt <= n_cu) return a.n_kt > 8 ? by_batch<XT, G, 1, 16>(a, st) : by_batch<XT, G, 1, 8>(a, st);
+  return by_batch<XT, G, RW_R, RW_W>(a, st);
 }
 template <int XT>
 static hipError_t by_group(const W4Args& a, int g, int n_cu, hipStream_t st) {
@@ -343,8 +383,8 @@ static hipError_t by_group(const W4Args& a, int g, int n_cu, hipStream_t st) {
 hipError_t launch_w4_gemv(const W4& L, const void* x, aqmb_dtype x_dtype, int64_t x_stride, const float* x_scales,
                           int x_scale_group, int batch, void* y, aqmb_dtype y_dtype, int64_t y_stride, hipStream_t st) {
   const int g = L.d.group_size;
-  W4Args a = {(const u32x4_t*)L.tiles, L.scales, L.zeros, x, x_scales, y, x_stride, y_stride,
-              L.d.d_out, L.d.d_in, L.n_kt, batch, x_scale_group ? (L.d.d_in - 1) / g + 1 : 0, (int)y_dtype};
+  W4Args a = {(const u32x4_t*)L.tiles, L.scales, L.zeros, L.asymmetric ? (size_t)(kW4Rows * kW4Cols / g) : 0, x, x_scales, y, x_stride, y_stride,
+              L.d.d_out, L.d.d_in, L.n_kt, batch, x_scale_group ? (L.d.d_in - 1) / g + 1 : 1, (int)y_dtype};
   switch (x_dtype) {
     case AQMB_F16: return by_group<AQMB_F16>(a, g, L.n_cu, st);
     case AQMB_BF16: return by_group<AQMB_BF16>(a, g, L.n_cu, st);

@@ -31,7 +31,8 @@ struct W4 {
   int n_rt, n_kt;          // row tiles, input tiles
   unsigned char* tiles;    // [n_rt][n_kt][1024]
   uint16_t* scales;        // [n_rt][n_kt][4 rows / 4][128 / g][4] fp16, 0 in the padding
-  unsigned char* zeros;    // the same shape, or null (8 everywhere)
+  unsigned char* zeros;    // the same shape, or one tile's (all 8) if not asymmetric
+  bool asymmetric;
 };
 constexpr uint32_t kW4Magic = 0x41513457u;
 hipError_t launch_w4_pack(const W4& L, const uint8_t* weights, const uint16_t* scales, const uint8_t* zeros,

@@ -161,10 +161,10 @@ aqmb_status aqmb_w4_create(aqmb_w4_t* out, const aqmb_w4_desc* desc, const uint8
   L->n_rt = (desc->d_out - 1) / kW4Rows + 1;
   L->n_kt = (desc->d_in - 1) / kW4Cols + 1;
   const size_t tiles = (size_t)L->n_rt * L->n_kt, n_scales = tiles * (kW4Cols / desc->group_size) * kW4Rows;
+  L->asymmetric = zeros != nullptr;
   struct { void** p; size_t n; } allocs[] = {{(void**)&L->tiles, tiles * 1024}, {(void**)&L->scales, n_scales * 2},
-                                             {(void**)&L->zeros, zeros ? n_scales : 0}};
+                                             {(void**)&L->zeros, zeros ? n_scales : n_scales / tiles}};
   for (auto& a : allocs) {
-    if (a.n == 0) continue;
     e = hipMalloc(a.p, a.n);
     if (e != hipSuccess) {
       *a.p = nullptr;
