@@ -102,9 +102,13 @@ struct AttnDev {
   int group, head_tiles;
 };
 
+// 16 bytes at a multiple of 8.
+struct __attribute__((packed, aligned(8))) Half16 { uint32_t w[4]; };
+
 // T: type of q and of the products with K; PT: type of the products with V. DC: values of V per lane
-// and position, head_dim <= 16 DC.
-template <int T, int PT, bool F8, int DC>
+// and position, head_dim <= 16 DC. P8: page_size is a multiple of 8, so that the 8 positions a lane
+// serves (they start at a multiple of 8) lie in one page: 2 look-ups per tile instead of 11.
+template <int T, int PT, bool F8, int DC, bool P8>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const AttnArgs& a = A.a;
   constexpr int kS = DC / 2;             // steps of 32 along head_dim for S
@@ -113,6 +117,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   constexpr size_t E = F8 ? 1 : 2;
   extern __shared__ int pages[];         // the chunk's page numbers, -1 where there is none
   __shared__ float s_ml[kWaves][2][16], s_join[2][16];
+  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][64];   // of a tile's keys, then values
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int r = lane % 16, q = lane / 16;
@@ -138,13 +143,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     pages[i] = p >= 0 && p < a.n_pages ? p : -1;
   }
 
-  // Q^T as the second operand: lane (r, q) holds q[head r][32 s + 8 q ..].
+  // Q^T as the second operand: lane (r, q) holds 8 values of head r for each step s of the product. Which
+  // ones is free as long as K does the same: 32 s + 8 q .., or with an 8-bit cache, where a lane loads 16
+  // values at a time, 64 (s / 2) + 16 q + 8 (s % 2) ...
+  auto dim_of = [&](int s) { return F8 ? 64 * (s / 2) + 16 * q + 8 * (s % 2) : 32 * s + 8 * q; };
   u32x4_t qf[kS];
   {
     const uint16_t* qr = (const uint16_t*)a.q + seq * a.q_stride + (int64_t)(h0 + min(r, nh - 1)) * a.head_dim;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const int d = 32 * s + 8 * q;
+      const int d = dim_of(s);
       qf[s] = d < a.head_dim ? *(const u32x4_t*)(qr + d) : u32x4_t{0, 0, 0, 0};
     }
   }
@@ -168,48 +176,98 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   float m = -__builtin_inff(), l = 0.f;
 
   for (int t0 = c0 + kTile * wave; t0 < c1; t0 += kTile * kWaves) {
-    // Keys of two positions, values of eight. Positions outside are read at the nearest one inside.
-    typename Raw<F8, 8>::T kr[2][kS];
+    // Keys of two positions, values of eight. Positions outside are read at one inside (P8: in the page
+    // of one inside, where there may be anything) and take no part.
+    u32x4_t kr[2][F8 ? kS / 2 : kS];
     typename Raw<F8, VN>::T vr[8][VL];
     uint32_t vmask = 0;                                         // bit j: position 8 q + j takes part
-    float ks[8], vs[8];
+    auto load_key = [&](u32x4_t* to, const char* p) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int pos = t0 + 8 * (r / 4) + r % 4 + 4 * b;
-      int page, slot;
-      locate(max(lo, min(pos, c1 - 1)), page, slot);
-      const char* p = kb + ((int64_t)max(page, 0) * a.page_stride + (int64_t)slot * a.slot_stride) * E;
-#pragma unroll
-      for (int s = 0; s < kS; ++s) {
-        const int d = 32 * s + 8 * q;
-        kr[b][s] = *(const typename Raw<F8, 8>::T*)(p + (d < a.head_dim ? d : 0) * E);
+      for (int s = 0; s < (F8 ? kS / 2 : kS); ++s) {
+        const int d = dim_of(F8 ? 2 * s : s);
+        if constexpr (!F8) {
+          to[s] = *(const u32x4_t*)(p + (d < a.head_dim ? d : 0) * E);
+        } else if (a.head_dim % 16 == 0) {
+          to[s] = __builtin_bit_cast(u32x4_t, *(const Half16*)(p + (d < a.head_dim ? d : 0)));
+        } else {
+          const uint2 x = *(const uint2*)(p + (d < a.head_dim ? d : 0)), y = *(const uint2*)(p + (d + 8 < a.head_dim ? d + 8 : 0));
+          to[s] = u32x4_t{x.x, x.y, y.x, y.y};
+        }
       }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int pos = t0 + 8 * q + j;
-      int page, slot;
-      locate(max(lo, min(pos, c1 - 1)), page, slot);
-      if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
-      const int64_t pg = max(page, 0);
-      const char* p = vb + (pg * a.page_stride + (int64_t)slot * a.slot_stride) * E;
+    };
+    auto load_value = [&](int j, const char* p) {
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
         const int d = r * DC + i * VN;
         vr[j][i] = *(const typename Raw<F8, VN>::T*)(p + (d < a.head_dim ? d : 0) * E);
       }
-      if constexpr (F8) {
-        const int64_t sc = pg * a.sc_page + (int64_t)kvh * a.sc_head + (int64_t)slot * a.sc_slot;
-        ks[j] = a.k_scale[sc];
-        vs[j] = a.v_scale[sc];
+    };
+    auto scale_at = [&](int page, int slot) {
+      return (int64_t)max(page, 0) * a.sc_page + (int64_t)kvh * a.sc_head + (int64_t)slot * a.sc_slot;
+    };
+    auto row_at = [&](int page, int slot) {
+      return ((int64_t)max(page, 0) * a.page_stride + (int64_t)slot * a.slot_stride) * (int64_t)E;
+    };
+    int page, slot;
+    if constexpr (P8) {
+      const int last = (c1 - 1) & ~7;
+      locate(min(t0 + 8 * (r / 4), last), page, slot);
+      const char* p = kb + row_at(page, slot + r % 4);
+      load_key(kr[0], p);
+      load_key(kr[1], p + 4 * a.slot_stride * (int64_t)E);
+      locate(min(t0 + 8 * q, last), page, slot);
+      p = vb + row_at(page, slot);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        load_value(j, p + j * a.slot_stride * (int64_t)E);
+        const int pos = t0 + 8 * q + j;
+        if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
       }
+    } else {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        locate(max(lo, min(t0 + 8 * (r / 4) + r % 4 + 4 * b, c1 - 1)), page, slot);
+        load_key(kr[b], kb + row_at(page, slot));
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int pos = t0 + 8 * q + j;
+        locate(max(lo, min(pos, c1 - 1)), page, slot);
+        load_value(j, vb + row_at(page, slot));
+        if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
+      }
+    }
+    // Scales: a lane loads one (keys in the lower half of the wave) and LDS hands them round.
+    float ks[8], vs[8];
+    if constexpr (F8) {
+      locate(max(lo, min(t0 + lane % 32, c1 - 1)), page, slot);
+      s_scale[wave][lane] = (lane < 32 ? a.k_scale : a.v_scale)[scale_at(page, slot)];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4_t x = *(const f32x4_t*)&s_scale[wave][8 * q + 4 * h], y = *(const f32x4_t*)&s_scale[wave][32 + 8 * q + 4 * h];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ks[4 * h + e] = x[e];
+          vs[4 * h + e] = y[e];
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
     f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      u32x4_t ka = as16<T, F8>(kr[0][s]), kc = as16<T, F8>(kr[1][s]);
-      if (32 * s + 8 * q >= a.head_dim) ka = kc = u32x4_t{0, 0, 0, 0};
+      u32x4_t ka, kc;
+      if constexpr (F8) {
+        const int h = 2 * (s % 2);
+        ka = as16<T, true>(make_uint2(kr[0][s / 2][h], kr[0][s / 2][h + 1]));
+        kc = as16<T, true>(make_uint2(kr[1][s / 2][h], kr[1][s / 2][h + 1]));
+      } else {
+        ka = kr[0][s];
+        kc = kr[1][s];
+      }
+      if (dim_of(s) >= a.head_dim) ka = kc = u32x4_t{0, 0, 0, 0};
       sa = Mma<T>::mul(ka, qf[s], sa);
       sb = Mma<T>::mul(kc, qf[s], sb);
     }
@@ -340,43 +398,52 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   }
 }
 
-// Joins the chunks of one (sequence, head): one workgroup, its waves take turns at the chunks.
+// Joins the chunks of one (sequence, head). head_dim / 4 lanes read a chunk's sum, so a workgroup has
+// several chunks under way, each group of lanes with a running maximum of its own; they meet in LDS.
+constexpr int kJoin = 512;
 template <int T>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, float shift) {
-  __shared__ float so[4][256];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+__global__ __launch_bounds__(kJoin) void attn_join_kernel(AttnArgs a, float shift) {
+  __shared__ float so[kJoin][4], sm[kJoin], sl[kJoin];
   const int64_t at = (int64_t)blockIdx.y * a.n_heads + blockIdx.x;
   const int seq = blockIdx.y;
   const int len = max(0, min(a.lengths[seq], a.max_length));
   const int lo = a.window > 0 ? max(0, len - a.window) : 0;
   const int n = len > 0 ? (len - (lo & ~7) + a.chunk - 1) / a.chunk : 0;
   const float* ml = a.part + (int64_t)a.n_seqs * a.n_heads * a.n_splits * a.head_dim + at * a.n_splits * 2;
-  float M = -__builtin_inff();
-  for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * i]);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-  const float Mu = M == -__builtin_inff() ? 0.f : M;
-  float L = 0.f;
-  for (int i = lane; i < n; i += 64) L += ml[2 * i + 1] * __builtin_amdgcn_exp2f(ml[2 * i] - Mu);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) L += __shfl_xor(L, d);
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
   const float* part = a.part + at * a.n_splits * a.head_dim;
-  for (int i = wave; i < n; i += 4) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * i] - Mu);
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (c * 64 + lane < a.head_dim) v[c] += f * part[(int64_t)i * a.head_dim + c * 64 + lane];
+  const int quads = a.head_dim / 4, groups = kJoin / quads, g = threadIdx.x / quads, d = threadIdx.x % quads * 4;
+  float M = -__builtin_inff(), L = 0.f;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (g < groups) {
+#pragma unroll 4
+    for (int i = g; i < n; i += groups) {
+      const float m = ml[2 * i], l = ml[2 * i + 1];
+      const f32x4_t x = *(const f32x4_t*)(part + (int64_t)i * a.head_dim + d);
+      const float m2 = fmaxf(M, m), mu = m2 == -__builtin_inff() ? 0.f : m2;
+      const float f = __builtin_amdgcn_exp2f(M - mu), e = __builtin_amdgcn_exp2f(m - mu);
+      L = L * f + l * e;
+      v = v * f + x * e;
+      M = m2;
+    }
   }
-#pragma unroll
-  for (int c = 0; c < 4; ++c) so[wave][c * 64 + lane] = v[c];
+  sm[threadIdx.x] = M;
+  sl[threadIdx.x] = L;
+  *(f32x4_t*)so[threadIdx.x] = v;
   __syncthreads();
   if (threadIdx.x < a.head_dim) {
-    const float s = so[0][threadIdx.x] + so[1][threadIdx.x] + so[2][threadIdx.x] + so[3][threadIdx.x];
-    OutT<T>::store(a.out, seq * a.out_stride + (int64_t)blockIdx.x * a.head_dim + threadIdx.x, L > 0.f ? s / L : s);
+    const int q = threadIdx.x / 4;
+    float top = -__builtin_inff(), sum = 0.f, out = 0.f;
+    for (int k = 0; k < groups; ++k) top = fmaxf(top, sm[k * quads + q]);
+    const float mu = top == -__builtin_inff() ? 0.f : top;
+    for (int k = 0; k < groups; ++k) {
+      const float e = __builtin_amdgcn_exp2f(sm[k * quads + q] - mu);
+      sum += sl[k * quads + q] * e;
+      out += so[k * quads + q][threadIdx.x % 4] * e;
+    }
+    OutT<T>::store(a.out, seq * a.out_stride + (int64_t)blockIdx.x * a.head_dim + threadIdx.x, sum > 0.f ? out / sum : out);
+    if (a.lse && threadIdx.x == 0)
+      a.lse[at] = sum > 0.f ? (top - shift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -__builtin_inff();
   }
-  if (a.lse && threadIdx.x == 0)
-    a.lse[at] = L > 0.f ? (M - shift + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -__builtin_inff();
 }
 
 AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu) {
@@ -414,11 +481,17 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
     if (e == hipSuccess) kernel<<<grid, 64 * kWaves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };
-  if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4>);
-  else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8>);
-  else run(attn_kernel<T, PT, F8, 16>);
+  if (a.page_size % 8 == 0) {
+    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, true>);
+    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, true>);
+    else run(attn_kernel<T, PT, F8, 16, true>);
+  } else {
+    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, false>);
+    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, false>);
+    else run(attn_kernel<T, PT, F8, 16, false>);
+  }
   if (e != hipSuccess || a.n_splits == 1) return e;
-  attn_join_kernel<T><<<dim3(a.n_heads, a.n_seqs), 256, 0, st>>>(a, Mma<PT>::kShift);
+  attn_join_kernel<T><<<dim3(a.n_heads, a.n_seqs), kJoin, 0, st>>>(a, Mma<PT>::kShift);
   return hipGetLastError();
 }
 
