@@ -486,10 +486,11 @@ typedef struct {
  *   q, out      [n_seqs][n_heads][head_dim] F16 or BF16 (`dtype`; the cache's own type, or any of
  *               the two with an F8 cache), stride between sequences q_stride / out_stride, each a
  *               multiple of 8; 16-byte aligned
- *   page_table  int32, row s at s * table_stride; only the entries that positions < lengths[s]
- *               need are read. A page outside [0, n_pages) is skipped: its positions do not exist.
+ *   page_table  int32, row s at s * table_stride, of ceil(max_length / page_size) entries; those that
+ *               no position < lengths[s] needs may hold anything. A page outside [0, n_pages) is
+ *               skipped: its positions do not exist.
  *   lengths     int32 [n_seqs], device memory; values outside [0, max_length] are clamped
- *   max_length  an upper bound of the lengths, <= table_stride * page_size: fixes how the work is
+ *   max_length  an upper bound of the lengths, <= table_stride * page_size and <= 2^28: fixes how the work is
  *               split, so results do not depend on other sequences' lengths
  * Slots that hold no token may hold anything (NaN included). Scores and softmax are binary32; the
  * probabilities enter the matrix cores as two 16-bit parts. One rounding to `dtype`.

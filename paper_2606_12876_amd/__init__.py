@@ -795,7 +795,7 @@ class KVCache:
             _dense(lse, torch.float32, n * heads, "lse", where)
         per = page_table.shape[1]
         if max_length is None:
-            max_length = min(per * self.page_size, 1 << 30)
+            max_length = min(per * self.page_size, 1 << 28)
         elif max_length > per * self.page_size:
             _refuse(where, f"max_length = {max_length} needs more pages than the table's {per}")
         row = heads * dim

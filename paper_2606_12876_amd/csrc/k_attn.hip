@@ -121,27 +121,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int r = lane % 16, q = lane / 16;
-  const int split = blockIdx.x, kvh = blockIdx.y / A.head_tiles, ht = blockIdx.y % A.head_tiles, seq = blockIdx.z;
+  // Workgroups go to the XCDs in turn by their x: heads there, so that each XCD has a share of every
+  // sequence. Chunks come last: the first ones, which every sequence has, run first, and an XCD is not
+  // left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which half was that).
+  const int kvh = blockIdx.x / A.head_tiles, ht = blockIdx.x % A.head_tiles, seq = blockIdx.y, split = blockIdx.z;
   const int h0 = kvh * A.group + ht * 16;                       // first query head
   const int nh = min(16, A.group - ht * 16);
+  // Without a window the chunk's place does not depend on the length: pages, length and q are asked for
+  // together, and pages past the length (there may be any number in the table) are not looked at later.
   const int len = max(0, min(a.lengths[seq], a.max_length));
   const int lo = a.window > 0 ? max(0, len - a.window) : 0;
   const int c0 = (lo & ~7) + split * a.chunk, c1 = min(len, c0 + a.chunk);
-  if (c0 >= len) {                                              // no positions here
-    if (split == 0 && a.n_splits == 1) {
-      for (int e = threadIdx.x; e < nh * a.head_dim; e += 64 * kWaves) {
-        const int h = h0 + e / a.head_dim;
-        ((uint16_t*)a.out)[seq * a.out_stride + (int64_t)h * a.head_dim + e % a.head_dim] = 0;
-      }
-      if (a.lse && threadIdx.x < nh) a.lse[(int64_t)seq * a.n_heads + h0 + threadIdx.x] = -__builtin_inff();
+  const int p0 = c0 / a.page_size;
+  const int np = (min(a.max_length, c0 + a.chunk) - 1) / a.page_size - p0 + 1;
+  if (c0 < a.max_length)
+    for (int i = threadIdx.x; i < np; i += 64 * kWaves) {
+      const int p = a.table[seq * a.table_stride + p0 + i];
+      pages[i] = p >= 0 && p < a.n_pages ? p : -1;
     }
-    return;
-  }
-  const int p0 = c0 / a.page_size, np = (c1 - 1) / a.page_size - p0 + 1;
-  for (int i = threadIdx.x; i < np; i += 64 * kWaves) {
-    const int p = a.table[seq * a.table_stride + p0 + i];
-    pages[i] = p >= 0 && p < a.n_pages ? p : -1;
-  }
 
   // Q^T as the second operand: lane (r, q) holds 8 values of head r for each step s of the product. Which
   // ones is free as long as K does the same: 32 s + 8 q .., or with an 8-bit cache, where a lane loads 16
@@ -155,6 +152,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       const int d = dim_of(s);
       qf[s] = d < a.head_dim ? *(const u32x4_t*)(qr + d) : u32x4_t{0, 0, 0, 0};
     }
+  }
+  if (c0 >= len) {                                              // no positions here
+    if (split == 0 && a.n_splits == 1) {
+      for (int e = threadIdx.x; e < nh * a.head_dim; e += 64 * kWaves) {
+        const int h = h0 + e / a.head_dim;
+        ((uint16_t*)a.out)[seq * a.out_stride + (int64_t)h * a.head_dim + e % a.head_dim] = 0;
+      }
+      if (a.lse && threadIdx.x < nh) a.lse[(int64_t)seq * a.n_heads + h0 + threadIdx.x] = -__builtin_inff();
+    }
+    return;
   }
   __syncthreads();
 
@@ -357,14 +364,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) L += s_ml[w][1][r] * __builtin_amdgcn_exp2f(s_ml[w][0][r] - Mu);
   const float mine = __builtin_amdgcn_exp2f(m - Mu);            // 0 for a wave without positions
-  float* so = (float*)pages;              // [kWaves][nh][head_dim]
+  // The waves' sums, [kWaves][nh][head_dim + 4]: 4 values at a time, the pad turns a column of heads
+  // over all banks.
+  const int pitch = a.head_dim + 4;
+  float* so = (float*)pages;
   if (r < nh) {
 #pragma unroll
-    for (int e = 0; e < DC; ++e)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int e = 0; e < DC; e += 4) {
         const int d = (4 * q + i) * DC + e;
-        if (d < a.head_dim) so[(wave * nh + r) * a.head_dim + d] = o[e][i] * mine;
+        if (d < a.head_dim)
+          *(f32x4_t*)(so + (wave * nh + r) * pitch + d) =
+              f32x4_t{o[e][i] * mine, o[e + 1][i] * mine, o[e + 2][i] * mine, o[e + 3][i] * mine};
       }
   }
   if (wave == 0 && q == 0) {              // the joined statistics, for the lines below
@@ -373,16 +385,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   }
   __syncthreads();
   const bool one = a.n_splits == 1;
-  for (int e = threadIdx.x; e < nh * a.head_dim; e += 64 * kWaves) {
-    const int h = e / a.head_dim, d = e % a.head_dim;
-    float v = 0.f;
+  const int quads = a.head_dim / 4;
+  for (int e = threadIdx.x; e < nh * quads; e += 64 * kWaves) {
+    const int h = e / quads, d = e % quads * 4;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += so[(w * nh + h) * a.head_dim + d];
+    for (int w = 0; w < kWaves; ++w) v += *(const f32x4_t*)(so + (w * nh + h) * pitch + d);
     if (one) {
       const float sum = s_join[1][h];
-      OutT<T>::store(a.out, seq * a.out_stride + (int64_t)(h0 + h) * a.head_dim + d, sum > 0.f ? v / sum : v);
+      if (sum > 0.f) v /= sum;
+      uint16_t* out = (uint16_t*)a.out + seq * a.out_stride + (int64_t)(h0 + h) * a.head_dim + d;
+      *(uint2*)out = make_uint2(Mma<T>::pack(v[0], v[1]), Mma<T>::pack(v[2], v[3]));
     } else {
-      a.part[(((int64_t)seq * a.n_heads + h0 + h) * a.n_splits + split) * a.head_dim + d] = v;
+      *(f32x4_t*)(a.part + (((int64_t)seq * a.n_heads + h0 + h) * a.n_splits + split) * a.head_dim + d) = v;
     }
   }
   if (threadIdx.x < nh) {
@@ -450,7 +465,10 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   // A window reaches from the 8 positions that its first one is in.
   const int64_t span = window > 0 && window < max_length ? (int64_t)window + 7 : max_length;
   const int64_t groups = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
-  const int64_t want = (2 * (int64_t)n_cu + groups - 1) / groups;           // workgroups along a sequence
+  
+  // Workgroups along a sequence: two on every unit, four where several sequences (whose lengths differ)
+  // need to be levelled out. 64 ragged streams: 131 us with two, 127 with four; one of 131072: 97 and 104.
+  const int64_t want = ((n_seqs > 1 ? 4 : 2) * (int64_t)n_cu + groups - 1) / groups;
   int64_t chunk = (span + want - 1) / want;
   const int64_t unit = kTile * kWaves;
   chunk = (chunk + unit - 1) / unit * unit;
@@ -472,9 +490,9 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   A.head_tiles = (A.group + 15) / 16;
   const int nh = A.group < 16 ? A.group : 16;
   const size_t tab = (size_t)(a.chunk / a.page_size + 2) * sizeof(int);
-  const size_t acc = (size_t)kWaves * nh * a.head_dim * sizeof(float);
+  const size_t acc = (size_t)kWaves * nh * (a.head_dim + 4) * sizeof(float);
   const size_t lds = tab > acc ? tab : acc;
-  const dim3 grid(a.n_splits, a.n_kv * A.head_tiles, a.n_seqs);
+  const dim3 grid(a.n_kv * A.head_tiles, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
