@@ -548,9 +548,12 @@ def _dt8(t, what: str, where: str) -> int:
     return d
 
 
+_current_device = _get_device if _get_device is not None else torch.cuda.current_device
+
+
 def _here(where: str, **tensors) -> None:
     """Every tensor lives on the current device."""
-    dev = _get_device() if _get_device is not None else torch.cuda.current_device()
+    dev = _current_device()
     for what, t in tensors.items():
         if t is not None and t.get_device() != dev:
             _refuse(where, f"{what} is on {t.device}, device {dev} is current")
@@ -577,28 +580,42 @@ def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=N
     [rows][cols] fp16 or bf16; y is a tensor of the same shape: fp16, bf16, fp32, or (with scales
     [rows][ceil(cols / scale_group)] fp32; scale_group 0 is the whole row) float8_e4m3fn or int8.
     With a residual, x + residual is rounded into residual_out."""
+    # Decode steps call this per layer, so the usual case (dense tensors) is checked with as few calls as it takes.
     where = "aqmb_rms_norm"
     if x.dim() != 2:
         _refuse(where, f"x is {tuple(x.shape)}, not (rows, cols)")
-    rows, cols = x.shape
-    xs = _rows(x, rows, cols, "x", where)
-    ys = _rows(y, rows, cols, "y", where)
-    dt, rs = _dt8(x, "x", where), 0
-    _here(where, x=x, weight=weight, y=y, residual=residual, residual_out=residual_out, scales=scales)
-    _dense(weight, x.dtype, cols, "weight", where)
+    shape, dtype, dev = x.shape, x.dtype, _current_device()
+    rows, cols = shape
+    if x.get_device() != dev or weight.get_device() != dev or y.get_device() != dev:
+        _here(where, x=x, weight=weight, y=y)
+    xs = cols if x.is_contiguous() else _rows(x, rows, cols, "x", where)
+    ys = cols if y.shape == shape and y.is_contiguous() else _rows(y, rows, cols, "y", where)
+    if weight.dtype != dtype or weight.numel() != cols or not weight.is_contiguous():
+        _dense(weight, dtype, cols, "weight", where)
+    rs, rp, ro, sp = 0, None, None, None
     if residual is not None:
-        if residual_out is None or residual.dtype != x.dtype or residual_out.dtype != x.dtype:
+        if residual_out is None or residual.dtype != dtype or residual_out.dtype != dtype:
             _refuse(where, "residual and residual_out go together, in the type of x")
-        rs = _rows(residual, rows, cols, "residual", where)
-        if _rows(residual_out, rows, cols, "residual_out", where) != rs:
-            _refuse(where, "residual and residual_out have different row strides")
+        if residual.get_device() != dev or residual_out.get_device() != dev:
+            _here(where, residual=residual, residual_out=residual_out)
+        if residual.shape == shape == residual_out.shape and residual.is_contiguous() and residual_out.is_contiguous():
+            rs = cols
+        else:
+            rs = _rows(residual, rows, cols, "residual", where)
+            if _rows(residual_out, rows, cols, "residual_out", where) != rs:
+                _refuse(where, "residual and residual_out have different row strides")
+        rp, ro = residual.data_ptr(), residual_out.data_ptr()
+    elif residual_out is not None:
+        _refuse(where, "residual and residual_out go together, in the type of x")
     if scales is not None:
         if scale_group < 0:
             _refuse(where, f"scale_group = {scale_group}")
+        _here(where, scales=scales)
         _dense(scales, torch.float32, rows * (-(-cols // scale_group) if scale_group else 1), "scales", where)
-    st = lib.aqmb_rms_norm(x.data_ptr(), dt, xs, _ptr(residual), _ptr(residual_out), rs, weight.data_ptr(),
-                           weight_offset, eps, rows, cols, y.data_ptr(), _dt8(y, "y", where), ys, _ptr(scales),
-                           scale_group, _stream(stream))
+        sp = scales.data_ptr()
+    st = lib.aqmb_rms_norm(x.data_ptr(), _dt8(x, "x", where), xs, rp, ro, rs, weight.data_ptr(), weight_offset, eps,
+                           rows, cols, y.data_ptr(), _dt8(y, "y", where), ys, sp, scale_group,
+                           _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
     if st:
         _check(st, where)
 
@@ -636,18 +653,23 @@ def _w4_gemv(layer: int, d_out: int, d_in: int, group_size: int, x, y, x_scales,
     where = "aqmb_w4_gemv"
     if x.dim() != 2:
         _refuse(where, f"x is {tuple(x.shape)}, not (batch, d_in)")
-    batch, group = x.shape[0], 0
-    xs = _rows(x, batch, d_in, "x", where)
-    ys = _rows(y, batch, d_out, "y", where)
-    _here(where, x=x, y=y, x_scales=x_scales)
+    batch, cols = x.shape
+    dev, group, sp = _current_device(), 0, None
+    if x.get_device() != dev or y.get_device() != dev:
+        _here(where, x=x, y=y)
+    xs = cols if cols == d_in and x.is_contiguous() else _rows(x, batch, d_in, "x", where)
+    ys = d_out if y.dim() == 2 and y.shape[0] == batch and y.shape[1] == d_out and y.is_contiguous() \
+        else _rows(y, batch, d_out, "y", where)
     if x_scales is not None:
-        groups = -(-d_in // group_size)
         # One scale per row, or one per group (the same thing where a row is one group).
         if x_scales.numel() != batch:
             group = group_size
-        _dense(x_scales, torch.float32, batch * (groups if group else 1), "x_scales", where)
-    st = lib.aqmb_w4_gemv(layer, x.data_ptr(), _dt8(x, "x", where), xs, _ptr(x_scales), group, batch, y.data_ptr(),
-                          _dt8(y, "y", where), ys, _stream(stream))
+        _here(where, x_scales=x_scales)
+        _dense(x_scales, torch.float32, batch * (-(-d_in // group_size) if group else 1), "x_scales", where)
+        sp = x_scales.data_ptr()
+    st = lib.aqmb_w4_gemv(layer, x.data_ptr(), _dt8(x, "x", where), xs, sp, group, batch, y.data_ptr(),
+                          _dt8(y, "y", where), ys,
+                          _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
     if st:
         _check(st, where)
 
@@ -753,7 +775,7 @@ class KVCache:
         return cls(k, v, ks, vs, layout=layout)
 
     def _current(self, where: str) -> None:
-        dev = _get_device() if _get_device is not None else torch.cuda.current_device()
+        dev = _current_device()
         if dev != self.device_index:
             _refuse(where, f"the cache is on device {self.device_index}, device {dev} is current")
 
@@ -777,61 +799,82 @@ class KVCache:
         (default: what the table holds). Without a workspace one is taken from PyTorch's allocator on the
         call's stream."""
         where = "aqmb_paged_attention"
-        self._current(where)
-        _here(where, q=q, page_table=page_table, lengths=lengths, out=out, lse=lse, workspace=workspace)
+        dev = _current_device()
+        if dev != self.device_index:
+            self._current(where)
+        if q.get_device() != dev or page_table.get_device() != dev or lengths.get_device() != dev \
+                or out.get_device() != dev:
+            _here(where, q=q, page_table=page_table, lengths=lengths, out=out)
         if q.dim() != 3 or q.shape[2] != self.head_dim:
             _refuse(where, f"q is {tuple(q.shape)}, not (n_seqs, n_heads, {self.head_dim})")
-        n, heads, dim = q.shape
-        for what, t in (("q", q), ("out", out)):
-            if t.shape != q.shape or t.dtype != q.dtype:
-                _refuse(where, f"{what} is {tuple(t.shape)} of {t.dtype}, not {tuple(q.shape)} of {q.dtype}")
-            if t.numel() and ((t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and heads != 1)):
-                _refuse(where, f"{what}: the heads of a sequence must be dense")
+        shape, dtype = q.shape, q.dtype
+        n, heads, dim = shape
+        row = heads * dim
+        if out.shape != shape or out.dtype != dtype:
+            _refuse(where, f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(shape)} of {dtype}")
+        qs = row if q.is_contiguous() else self._stride(q, n, row, "q", where)
+        os_ = row if out.is_contiguous() else self._stride(out, n, row, "out", where)
         if page_table.dim() != 2 or page_table.shape[0] != n or page_table.dtype != torch.int32 \
-                or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+                or (not page_table.is_contiguous() and page_table.shape[1] > 1 and page_table.stride(1) != 1):
             _refuse(where, f"page_table must be int32 [{n}][pages] with dense rows")
-        _dense(lengths, torch.int32, n, "lengths", where)
+        if lengths.dtype != torch.int32 or lengths.numel() != n or not lengths.is_contiguous():
+            _dense(lengths, torch.int32, n, "lengths", where)
+        lp = None
         if lse is not None:
+            _here(where, lse=lse)
             _dense(lse, torch.float32, n * heads, "lse", where)
+            lp = lse.data_ptr()
         per = page_table.shape[1]
         if max_length is None:
             max_length = min(per * self.page_size, 1 << 28)
         elif max_length > per * self.page_size:
             _refuse(where, f"max_length = {max_length} needs more pages than the table's {per}")
-        row = heads * dim
-        dt = _dt8(q, "q", where)
         need = self.workspace_bytes(heads, n, max_length, window)
-        if workspace is None and need:
+        wp, wb = None, 0
+        if workspace is not None:
+            _here(where, workspace=workspace)
+            wp, wb = workspace.data_ptr(), _nbytes(workspace)
+        elif need:
             if stream is None:
                 workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
             else:   # the allocator ties memory to the stream that is current
                 s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)
                 with torch.cuda.stream(s):
                     workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
-        st = lib.aqmb_paged_attention(self._ref, q.data_ptr(), dt, q.stride(0) if n > 1 else row, heads,
-                                      page_table.data_ptr(), page_table.stride(0) if n > 1 else per, lengths.data_ptr(),
-                                      n, max_length, scale, window, out.data_ptr(), out.stride(0) if n > 1 else row,
-                                      _ptr(lse), _ptr(workspace), _nbytes(workspace) or 0 if workspace is not None else 0,
-                                      _stream(stream))
+            wp, wb = workspace.data_ptr(), need
+        st = lib.aqmb_paged_attention(self._ref, q.data_ptr(), _dt8(q, "q", where), qs, heads, page_table.data_ptr(),
+                                      page_table.stride(0) if n > 1 else per, lengths.data_ptr(), n, max_length, scale,
+                                      window, out.data_ptr(), os_, lp, wp, wb,
+                                      _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
         if st:
             _check(st, where)
+
+    @staticmethod
+    def _stride(t, n: int, row: int, what: str, where: str) -> int:
+        """The stride between the rows [heads][head_dim] of a 3-dimensional tensor, which must be dense."""
+        if t.numel() and ((t.stride(2) != 1 and t.shape[2] != 1) or (t.stride(1) != t.shape[2] and t.shape[1] != 1)):
+            _refuse(where, f"{what}: the heads of a row must be dense")
+        return t.stride(0) if n > 1 else row
 
     def append(self, k, v, slots, stream=None) -> None:
         """aqmb_kv_append: write k, v [n_tokens][n_kv_heads][head_dim] (fp16 or bf16) into slots int64
         [n_tokens] on the GPU (page * page_size + offset; outside the cache: skipped)."""
         where = "aqmb_kv_append"
-        self._current(where)
-        _here(where, k=k, v=v, slots=slots)
+        dev = _current_device()
+        if dev != self.device_index:
+            self._current(where)
+        if k.get_device() != dev or v.get_device() != dev or slots.get_device() != dev:
+            _here(where, k=k, v=v, slots=slots)
         n, dim, heads = slots.numel(), self.head_dim, self.n_kv_heads
-        _dense(slots, torch.int64, n, "slots", where)
-        for what, t in (("k", k), ("v", v)):
-            if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != dim or t.dtype != k.dtype:
-                _refuse(where, f"{what} is {tuple(t.shape)} of {t.dtype}, not ({n}, {heads}, {dim}) of {k.dtype}")
-            if n and ((t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and heads != 1)):
-                _refuse(where, f"{what}: the heads of a token must be dense")
-        row = heads * dim
-        st = lib.aqmb_kv_append(self._ref, k.data_ptr(), k.stride(0) if n > 1 else row, v.data_ptr(),
-                                v.stride(0) if n > 1 else row, _dt8(k, "k", where), slots.data_ptr(), n, _stream(stream))
+        if slots.dtype != torch.int64 or not slots.is_contiguous():
+            _dense(slots, torch.int64, n, "slots", where)
+        shape, dtype, row = k.shape, k.dtype, heads * dim
+        if shape != (n, heads, dim) or v.shape != shape or v.dtype != dtype:
+            _refuse(where, f"k is {tuple(shape)} of {dtype} and v {tuple(v.shape)} of {v.dtype}, not ({n}, {heads}, {dim})")
+        ks = row if k.is_contiguous() else self._stride(k, n, row, "k", where)
+        vs = row if v.is_contiguous() else self._stride(v, n, row, "v", where)
+        st = lib.aqmb_kv_append(self._ref, k.data_ptr(), ks, v.data_ptr(), vs, _dt8(k, "k", where), slots.data_ptr(), n,
+                                _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
         if st:
             _check(st, where)
 
