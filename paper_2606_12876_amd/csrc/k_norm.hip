@@ -4,8 +4,9 @@
 //
 // A row is read once and stays in registers: NT threads own 8 consecutive columns each, NV times
 // over, so the sum of squares, the largest magnitude of a scale group (g / 8 neighbouring lanes) and
-// the output need no second pass over memory. Bound by HBM for many rows, by latency (load, two
-// reductions, store) for few.
+// the output need no second pass over memory. Bound by HBM for many rows (8192 x 4096 bf16 with a
+// residual to e4m3: 49 us, 4.8 TB/s, a large copy's rate), by latency (load, two reductions, store) for
+// few (one row of 4096: 2.9 us).
 #include "device.h"
 #include "ops.h"
 
@@ -57,7 +58,7 @@ struct __attribute__((packed, aligned(1))) B8 { uint32_t w[2]; };
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  for (int d = NT < 64 ? NT / 2 : 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
   if constexpr (NT > 64) {
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
@@ -73,7 +74,7 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
 template <int NT>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  for (int d = NT < 64 ? NT / 2 : 32; d >= 1; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
   if constexpr (NT > 64) {
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
@@ -86,14 +87,14 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
 
 constexpr float kScaleFloor = 7.888609052210118e-31f;  // 2^-100: keeps L / a and a / L normal numbers
 
-// NT threads per row (64: one wave, four rows per workgroup; else the whole workgroup).
+// NT threads per row: up to 64, part of a wave or a wave (256 / NT rows per workgroup); else the workgroup.
 template <int DT, int NT, int NV>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
   __shared__ float lds_sum[16];
   __shared__ uint32_t lds_max[16];
-  const int t = NT == 64 ? threadIdx.x % 64 : threadIdx.x;
-  const int64_t row = NT == 64 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
-  if (NT == 64 && row >= a.rows) return;      // whole waves, and no barrier below for NT = 64
+  const int t = NT <= 64 ? threadIdx.x % NT : threadIdx.x;
+  const int64_t row = NT <= 64 ? (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT : blockIdx.x;
+  if (NT <= 64 && row >= a.rows) return;      // all lanes of the row, and no barrier below for NT <= 64
   const uint16_t* x = (const uint16_t*)a.x + row * a.x_stride;
   const uint16_t* r = a.residual ? (const uint16_t*)a.residual + row * a.residual_stride : nullptr;
 
@@ -231,19 +232,29 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_kernel(NormArgs a) {
 
 template <int DT, int NT, int NV>
 static hipError_t go(const NormArgs& a, hipStream_t st) {
-  const int blocks = NT == 64 ? (a.rows + 3) / 4 : a.rows;
-  norm_kernel<DT, NT, NV><<<blocks, NT == 64 ? 256 : NT, 0, st>>>(a);
+  const int blocks = NT <= 64 ? (a.rows - 1) / (256 / NT) + 1 : a.rows;
+  norm_kernel<DT, NT, NV><<<blocks, NT <= 64 ? 256 : NT, 0, st>>>(a);
   return hipGetLastError();
 }
 
+// Threads for a row: one 8-column piece each as far as that goes (a launch of few rows is bound by its
+// chain of loads, reductions and cold code: 4096 columns, 1 row: 512 threads x 1 piece 2.9 us, 256 x 2 3.1,
+// 128 x 4 3.7, 1024 x 1 3.5; 8192 rows 49.6, 52.3, 51.5 and 62.9 us) and no more threads than pieces. 128
+// columns, 65536 rows: 16 threads 15.9 us, 32 21.4. From 257 columns a wave's lanes are half idle and many rows
+// gain by two pieces (512 columns, 16384 rows: 13.5 against 16.3 us; 64 rows: 3.2 against 2.9).
 template <int DT>
 static hipError_t choose(const NormArgs& a, hipStream_t st) {
   const int v = (a.cols + 7) / 8;
-  if (v <= 64) return go<DT, 64, 1>(a, st);
-  if (v <= 128) return go<DT, 64, 2>(a, st);
+  if (v <= 16) return go<DT, 16, 1>(a, st);
+  if (v <= 32) return go<DT, 32, 1>(a, st);
+  if (v <= 64) return a.rows >= 4096 ? go<DT, 32, 2>(a, st) : go<DT, 64, 1>(a, st);
+  if (v <= 128) return go<DT, 128, 1>(a, st);
   if (v <= 256) return go<DT, 256, 1>(a, st);
-  if (v <= 512) return go<DT, 256, 2>(a, st);
-  if (v <= 1024) return go<DT, 256, 4>(a, st);
+  if (v <= 384) return go<DT, 384, 1>(a, st);
+  if (v <= 512) return go<DT, 512, 1>(a, st);
+  if (v <= 768) return go<DT, 768, 1>(a, st);
+  if (v <= 1024) return go<DT, 1024, 1>(a, st);
+  if (v <= 1536) return go<DT, 768, 2>(a, st);
   if (v <= 2048) return go<DT, 1024, 2>(a, st);
   return go<DT, 1024, 4>(a, st);
 }
