@@ -106,9 +106,8 @@ struct AttnDev {
 struct __attribute__((packed, aligned(8))) Half16 { uint32_t w[4]; };
 
 // T: type of q and of the products with K; PT: type of the products with V. DC: values of V per lane
-// and position, head_dim <= 16 DC. P8: page_size is a multiple of 8, so that the 8 positions a lane
-// serves (they start at a multiple of 8) lie in one page: 2 look-ups per tile instead of 11.
-template <int T, int PT, bool F8, int DC, bool P8>
+// and position, head_dim <= 16 DC.
+template <int T, int PT, bool F8, int DC>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const AttnArgs& a = A.a;
   constexpr int kS = DC / 2;             // steps of 32 along head_dim for S
@@ -117,7 +116,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   constexpr size_t E = F8 ? 1 : 2;
   extern __shared__ int pages[];         // the chunk's page numbers, -1 where there is none
   __shared__ float s_ml[kWaves][2][16], s_join[2][16];
-  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][64];   // of a tile's keys, then values
+  __shared__ __attribute__((aligned(16))) int64_t s_row[kWaves][32];      // byte offsets of a tile's positions
+  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][64];      // scales of its keys, then values
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int r = lane % 16, q = lane / 16;
@@ -165,14 +165,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   }
   __syncthreads();
 
-  // Position -> page (LDS index) and slot; positions are relative to the chunk's first page.
-  const int base = p0 * a.page_size;
-  auto locate = [&](int pos, int& page, int& slot) {
-    const uint32_t rel = (uint32_t)(pos - base);
-    const uint32_t i = a.page_size == 1 ? rel : __umulhi(rel, A.page_magic);
-    page = pages[i];
-    slot = (int)(rel - i * (uint32_t)a.page_size);
-  };
+  const int base = p0 * a.page_size;                            // position of the chunk's first page
   const char* kb = (const char*)a.k + (int64_t)kvh * a.head_stride * E;
   const char* vb = (const char*)a.v + (int64_t)kvh * a.head_stride * E;
   const float scale2 = a.scale * 1.4426950408889634f;           // scores in units of log 2
@@ -183,73 +176,50 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   float m = -__builtin_inff(), l = 0.f;
 
   for (int t0 = c0 + kTile * wave; t0 < c1; t0 += kTile * kWaves) {
-    // Keys of two positions, values of eight. Positions outside are read at one inside (P8: in the page
-    // of one inside, where there may be anything) and take no part.
+    // One look-up for each position of the tile, by lane % 32; LDS hands the offsets (and scales) round.
+    // Positions outside are read at one inside and take no part (mask).
+    const int pos = t0 + lane % 32;
+    const uint32_t rel = (uint32_t)(max(lo, min(pos, c1 - 1)) - base);
+    const uint32_t pi = a.page_size == 1 ? rel : __umulhi(rel, A.page_magic);
+    const int page = pages[pi], slot = (int)(rel - pi * (uint32_t)a.page_size);
+    const uint32_t mask = (uint32_t)__ballot(pos >= lo && pos < c1 && page >= 0);
+    const int64_t pg = max(page, 0);
+    s_row[wave][lane % 32] = (pg * a.page_stride + (int64_t)slot * a.slot_stride) * (int64_t)E;
+    if constexpr (F8)
+      s_scale[wave][lane] = (lane < 32 ? a.k_scale : a.v_scale)[pg * a.sc_page + (int64_t)kvh * a.sc_head + (int64_t)slot * a.sc_slot];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint32_t vmask = mask >> (8 * q) & 0xFFu;             // bit j: position 8 q + j takes part
+
+    // Keys of two positions, values of eight.
     u32x4_t kr[2][F8 ? kS / 2 : kS];
     typename Raw<F8, VN>::T vr[8][VL];
-    uint32_t vmask = 0;                                         // bit j: position 8 q + j takes part
-    auto load_key = [&](u32x4_t* to, const char* p) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const char* p = kb + s_row[wave][8 * (r / 4) + r % 4 + 4 * b];
 #pragma unroll
       for (int s = 0; s < (F8 ? kS / 2 : kS); ++s) {
         const int d = dim_of(F8 ? 2 * s : s);
         if constexpr (!F8) {
-          to[s] = *(const u32x4_t*)(p + (d < a.head_dim ? d : 0) * E);
+          kr[b][s] = *(const u32x4_t*)(p + (d < a.head_dim ? d : 0) * E);
         } else if (a.head_dim % 16 == 0) {
-          to[s] = __builtin_bit_cast(u32x4_t, *(const Half16*)(p + (d < a.head_dim ? d : 0)));
+          kr[b][s] = __builtin_bit_cast(u32x4_t, *(const Half16*)(p + (d < a.head_dim ? d : 0)));
         } else {
           const uint2 x = *(const uint2*)(p + (d < a.head_dim ? d : 0)), y = *(const uint2*)(p + (d + 8 < a.head_dim ? d + 8 : 0));
-          to[s] = u32x4_t{x.x, x.y, y.x, y.y};
+          kr[b][s] = u32x4_t{x.x, x.y, y.x, y.y};
         }
       }
-    };
-    auto load_value = [&](int j, const char* p) {
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* p = vb + s_row[wave][8 * q + j];
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
         const int d = r * DC + i * VN;
         vr[j][i] = *(const typename Raw<F8, VN>::T*)(p + (d < a.head_dim ? d : 0) * E);
       }
-    };
-    auto scale_at = [&](int page, int slot) {
-      return (int64_t)max(page, 0) * a.sc_page + (int64_t)kvh * a.sc_head + (int64_t)slot * a.sc_slot;
-    };
-    auto row_at = [&](int page, int slot) {
-      return ((int64_t)max(page, 0) * a.page_stride + (int64_t)slot * a.slot_stride) * (int64_t)E;
-    };
-    int page, slot;
-    if constexpr (P8) {
-      const int last = (c1 - 1) & ~7;
-      locate(min(t0 + 8 * (r / 4), last), page, slot);
-      const char* p = kb + row_at(page, slot + r % 4);
-      load_key(kr[0], p);
-      load_key(kr[1], p + 4 * a.slot_stride * (int64_t)E);
-      locate(min(t0 + 8 * q, last), page, slot);
-      p = vb + row_at(page, slot);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        load_value(j, p + j * a.slot_stride * (int64_t)E);
-        const int pos = t0 + 8 * q + j;
-        if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
-      }
-    } else {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        locate(max(lo, min(t0 + 8 * (r / 4) + r % 4 + 4 * b, c1 - 1)), page, slot);
-        load_key(kr[b], kb + row_at(page, slot));
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int pos = t0 + 8 * q + j;
-        locate(max(lo, min(pos, c1 - 1)), page, slot);
-        load_value(j, vb + row_at(page, slot));
-        if (pos >= lo && pos < c1 && page >= 0) vmask |= 1u << j;
-      }
     }
-    // Scales: a lane loads one (keys in the lower half of the wave) and LDS hands them round.
     float ks[8], vs[8];
     if constexpr (F8) {
-      locate(max(lo, min(t0 + lane % 32, c1 - 1)), page, slot);
-      s_scale[wave][lane] = (lane < 32 ? a.k_scale : a.v_scale)[scale_at(page, slot)];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const f32x4_t x = *(const f32x4_t*)&s_scale[wave][8 * q + 4 * h], y = *(const f32x4_t*)&s_scale[wave][32 + 8 * q + 4 * h];
@@ -259,8 +229,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
           vs[4 * h + e] = y[e];
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
     f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
 #pragma unroll
@@ -311,8 +281,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     }
     const u32x4_t pho = {ph[0], ph[1], ph[2], ph[3]}, plo = {pl[0], pl[1], pl[2], pl[3]};
 
-    // V^T: values of 8 positions, transposed. A value that takes no part must be 0, not garbage.
-    const bool clean = __all(vmask == 0xFFu);
+    // V^T: values of 8 positions, transposed. A position that takes no part must be 0, not garbage; rows of
+    // V^T past head_dim may be anything, they are rows of a result that nobody reads.
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
       uint32_t v[8][VN / 2];
@@ -328,14 +298,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
           v[j][1] = w.y;
         }
       }
-      const bool in = r * DC + i * VN < a.head_dim;
-      if (!clean || 16 * DC != a.head_dim) {
+      if (mask != 0xFFFFFFFFu) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool keep = in && (vmask >> j & 1);
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int e = 0; e < VN / 2; ++e) v[j][e] = keep ? v[j][e] : 0;
-        }
+          for (int e = 0; e < VN / 2; ++e) v[j][e] = vmask >> j & 1 ? v[j][e] : 0;
       }
 #pragma unroll
       for (int e = 0; e < VN; ++e) {
@@ -527,15 +494,9 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
     if (e == hipSuccess) kernel<<<grid, 64 * kWaves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };
-  if (a.page_size % 8 == 0) {
-    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, true>);
-    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, true>);
-    else run(attn_kernel<T, PT, F8, 16, true>);
-  } else {
-    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, false>);
-    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, false>);
-    else run(attn_kernel<T, PT, F8, 16, false>);
-  }
+  if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4>);
+  else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8>);
+  else run(attn_kernel<T, PT, F8, 16>);
   if (e != hipSuccess || a.n_splits == 1) return e;
   if (a.n_splits <= kFewChunks) {
     const int heads = kJoinFew / (a.head_dim / 4);
