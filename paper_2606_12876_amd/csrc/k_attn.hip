@@ -29,7 +29,7 @@ namespace aqmb {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 32, kWaves = 4, kChunkMax = 4096;
+constexpr int kTile = 32, kWaves = 4, kChunkMax = 4096, kXcds = 8;
 
 // The binary32 number next below a positive one; 0 for 0.
 __device__ __forceinline__ float below(float x) {
@@ -99,7 +99,8 @@ __device__ __forceinline__ uint32_t hi_halves(uint32_t a, uint32_t b) { return _
 struct AttnDev {
   AttnArgs a;
   uint32_t page_magic;     // 2^32 / page_size + 1 (page_size > 1)
-  int group, head_tiles;
+  int group, head_tiles, heads;   // query heads per key-value head, in tiles of 16; tiles in all
+  bool by_unit;
 };
 
 // 16 bytes at a multiple of 8.
@@ -121,10 +122,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int r = lane % 16, q = lane / 16;
-  // Workgroups go to the XCDs in turn by their x: heads there, so that each XCD has a share of every
-  // sequence. Chunks come last: the first ones, which every sequence has, run first, and an XCD is not
-  // left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which half was that).
-  const int kvh = blockIdx.x / A.head_tiles, ht = blockIdx.x % A.head_tiles, seq = blockIdx.y, split = blockIdx.z;
+  // Workgroups go to the XCDs in turn. Either heads do (every XCD has a share of every sequence), or, where
+  // heads share cache lines or keys, all heads of a (sequence, chunk) follow each other on one XCD, so
+  // that its L2 serves all but the first; sequences are turned by one per chunk, so that an XCD does not
+  // keep the same ones. Chunks come last in both: the first ones, which every sequence has, run first, and no
+  // XCD is left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which 30 were that).
+  int head, unit;
+  if (A.by_unit) {
+    const int k = blockIdx.x / kXcds;
+    head = k % A.heads;
+    unit = k / A.heads * kXcds + blockIdx.x % kXcds;
+    if (unit >= a.n_seqs * a.n_splits) return;
+  } else {
+    head = blockIdx.x % A.heads;
+    unit = blockIdx.x / A.heads;
+  }
+  const int split = unit / a.n_seqs, seq = (unit + (A.by_unit ? split : 0)) % a.n_seqs;
+  const int kvh = head / A.head_tiles, ht = head % A.head_tiles;
   const int h0 = kvh * A.group + ht * 16;                       // first query head
   const int nh = min(16, A.group - ht * 16);
   // Without a window the chunk's place does not depend on the length: pages, length and q are asked for
@@ -487,11 +501,18 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   const size_t tab = (size_t)(a.chunk / a.page_size + 2) * sizeof(int);
   const size_t acc = (size_t)kWaves * nh * (a.head_dim + 4) * sizeof(float);
   const size_t lds = tab > acc ? tab : acc;
-  const dim3 grid(a.n_kv * A.head_tiles, a.n_seqs, a.n_splits);
+  A.heads = a.n_kv * A.head_tiles;
+  const int64_t units = (int64_t)a.n_seqs * a.n_splits;
+  // Heads share cache lines (128 bytes) where tokens are outermost in a page and a head does not fill
+  // whole lines: 16 ragged streams, heads of 80 on an e4m3 cache: 32 us by heads, 25 by units. Tiles of heads
+  // share the keys and values themselves.
+  A.by_unit = A.head_tiles > 1 || (a.sc_head == 1 && a.n_kv > 1 && a.head_dim * (F8 ? 1 : 2) % 128 != 0);
+  const int64_t grid = (A.by_unit ? (units + kXcds - 1) / kXcds * kXcds : units) * A.heads;
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e == hipSuccess) kernel<<<grid, 64 * kWaves, lds, st>>>(A);
+    if (e == hipSuccess) kernel<<<(unsigned)grid, 64 * kWaves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };
   if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4>);
