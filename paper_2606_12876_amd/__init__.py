@@ -582,10 +582,13 @@ def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=N
     With a residual, x + residual is rounded into residual_out."""
     # Decode steps call this per layer, so the usual case (dense tensors) is checked with as few calls as it takes.
     where = "aqmb_rms_norm"
-    if x.dim() != 2:
-        _refuse(where, f"x is {tuple(x.shape)}, not (rows, cols)")
     shape, dtype, dev = x.shape, x.dtype, _current_device()
+    if len(shape) != 2:
+        _refuse(where, f"x is {tuple(shape)}, not (rows, cols)")
     rows, cols = shape
+    dt, ydt = _TORCH_DT8.get(dtype), _TORCH_DT8.get(y.dtype)
+    if dt is None or ydt is None:
+        _refuse(where, f"x of {dtype}, y of {y.dtype}", Status.EUNSUPPORTED)
     if x.get_device() != dev or weight.get_device() != dev or y.get_device() != dev:
         _here(where, x=x, weight=weight, y=y)
     xs = cols if x.is_contiguous() else _rows(x, rows, cols, "x", where)
@@ -610,11 +613,12 @@ def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=N
     if scales is not None:
         if scale_group < 0:
             _refuse(where, f"scale_group = {scale_group}")
-        _here(where, scales=scales)
+        if scales.get_device() != dev:
+            _here(where, scales=scales)
         _dense(scales, torch.float32, rows * (-(-cols // scale_group) if scale_group else 1), "scales", where)
         sp = scales.data_ptr()
-    st = lib.aqmb_rms_norm(x.data_ptr(), _dt8(x, "x", where), xs, rp, ro, rs, weight.data_ptr(), weight_offset, eps,
-                           rows, cols, y.data_ptr(), _dt8(y, "y", where), ys, sp, scale_group,
+    st = lib.aqmb_rms_norm(x.data_ptr(), dt, xs, rp, ro, rs, weight.data_ptr(), weight_offset, eps, rows, cols,
+                           y.data_ptr(), ydt, ys, sp, scale_group,
                            _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
     if st:
         _check(st, where)
@@ -651,24 +655,27 @@ def w4_get_desc(layer: int) -> W4Desc:
 
 def _w4_gemv(layer: int, d_out: int, d_in: int, group_size: int, x, y, x_scales, stream) -> None:
     where = "aqmb_w4_gemv"
-    if x.dim() != 2:
-        _refuse(where, f"x is {tuple(x.shape)}, not (batch, d_in)")
-    batch, cols = x.shape
+    shape, yshape = x.shape, y.shape
+    if len(shape) != 2:
+        _refuse(where, f"x is {tuple(shape)}, not (batch, d_in)")
+    batch, cols = shape
+    dt, ydt = _TORCH_DT8.get(x.dtype), _TORCH_DT8.get(y.dtype)
+    if dt is None or ydt is None:
+        _refuse(where, f"x of {x.dtype}, y of {y.dtype}", Status.EUNSUPPORTED)
     dev, group, sp = _current_device(), 0, None
     if x.get_device() != dev or y.get_device() != dev:
         _here(where, x=x, y=y)
     xs = cols if cols == d_in and x.is_contiguous() else _rows(x, batch, d_in, "x", where)
-    ys = d_out if y.dim() == 2 and y.shape[0] == batch and y.shape[1] == d_out and y.is_contiguous() \
-        else _rows(y, batch, d_out, "y", where)
+    ys = d_out if yshape == (batch, d_out) and y.is_contiguous() else _rows(y, batch, d_out, "y", where)
     if x_scales is not None:
         # One scale per row, or one per group (the same thing where a row is one group).
         if x_scales.numel() != batch:
             group = group_size
-        _here(where, x_scales=x_scales)
+        if x_scales.get_device() != dev:
+            _here(where, x_scales=x_scales)
         _dense(x_scales, torch.float32, batch * (-(-d_in // group_size) if group else 1), "x_scales", where)
         sp = x_scales.data_ptr()
-    st = lib.aqmb_w4_gemv(layer, x.data_ptr(), _dt8(x, "x", where), xs, sp, group, batch, y.data_ptr(),
-                          _dt8(y, "y", where), ys,
+    st = lib.aqmb_w4_gemv(layer, x.data_ptr(), dt, xs, sp, group, batch, y.data_ptr(), ydt, ys,
                           _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream))
     if st:
         _check(st, where)
@@ -805,26 +812,27 @@ class KVCache:
         if q.get_device() != dev or page_table.get_device() != dev or lengths.get_device() != dev \
                 or out.get_device() != dev:
             _here(where, q=q, page_table=page_table, lengths=lengths, out=out)
-        if q.dim() != 3 or q.shape[2] != self.head_dim:
-            _refuse(where, f"q is {tuple(q.shape)}, not (n_seqs, n_heads, {self.head_dim})")
-        shape, dtype = q.shape, q.dtype
+        shape, dtype, tshape = q.shape, q.dtype, page_table.shape
+        if len(shape) != 3 or shape[2] != self.head_dim:
+            _refuse(where, f"q is {tuple(shape)}, not (n_seqs, n_heads, {self.head_dim})")
         n, heads, dim = shape
         row = heads * dim
         if out.shape != shape or out.dtype != dtype:
             _refuse(where, f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(shape)} of {dtype}")
         qs = row if q.is_contiguous() else self._stride(q, n, row, "q", where)
         os_ = row if out.is_contiguous() else self._stride(out, n, row, "out", where)
-        if page_table.dim() != 2 or page_table.shape[0] != n or page_table.dtype != torch.int32 \
-                or (not page_table.is_contiguous() and page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        if len(tshape) != 2 or tshape[0] != n or page_table.dtype != torch.int32 \
+                or (not page_table.is_contiguous() and tshape[1] > 1 and page_table.stride(1) != 1):
             _refuse(where, f"page_table must be int32 [{n}][pages] with dense rows")
         if lengths.dtype != torch.int32 or lengths.numel() != n or not lengths.is_contiguous():
             _dense(lengths, torch.int32, n, "lengths", where)
         lp = None
         if lse is not None:
-            _here(where, lse=lse)
+            if lse.get_device() != dev:
+                _here(where, lse=lse)
             _dense(lse, torch.float32, n * heads, "lse", where)
             lp = lse.data_ptr()
-        per = page_table.shape[1]
+        per = tshape[1]
         if max_length is None:
             max_length = min(per * self.page_size, 1 << 28)
         elif max_length > per * self.page_size:
