@@ -29,7 +29,8 @@ namespace aqmb {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 32, kWaves = 4, kChunkMax = 4096, kXcds = 8;
+constexpr int kTile = 32, kChunkMax = 4096, kXcds = 8;
+constexpr int kWavesSplit = 4, kWavesWhole = 8;   // per workgroup, where sequences are split and where not
 
 // The binary32 number next below a positive one; 0 for 0.
 __device__ __forceinline__ float below(float x) {
@@ -96,6 +97,18 @@ __device__ __forceinline__ uint2 as16h(typename Raw<F8, 4>::T r) {
 __device__ __forceinline__ uint32_t lo_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t hi_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
+// f over the four quarters of a wave, in every lane. Swapping rows of a register with rows of its own copy
+// leaves the pairs side by side, without a trip through LDS.
+template <class F>
+__device__ __forceinline__ float quarters(float x, F f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float y = f(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const uint32_t v = __builtin_bit_cast(uint32_t, y);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 struct AttnDev {
   AttnArgs a;
   uint32_t page_magic;     // 2^32 / page_size + 1 (page_size > 1)
@@ -108,7 +121,7 @@ struct __attribute__((packed, aligned(8))) Half16 { uint32_t w[4]; };
 
 // T: type of q and of the products with K; PT: type of the products with V. DC: values of V per lane
 // and position, head_dim <= 16 DC.
-template <int T, int PT, bool F8, int DC>
+template <int T, int PT, bool F8, int DC, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const AttnArgs& a = A.a;
   constexpr int kS = DC / 2;             // steps of 32 along head_dim for S
@@ -247,6 +260,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
     f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+    const bool ragged = a.head_dim % (F8 ? 64 : 32) != 0;       // steps that reach past head_dim
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       u32x4_t ka, kc;
@@ -258,7 +272,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
         ka = kr[0][s];
         kc = kr[1][s];
       }
-      if (dim_of(s) >= a.head_dim) ka = kc = u32x4_t{0, 0, 0, 0};
+      if (ragged && dim_of(s) >= a.head_dim) ka = kc = u32x4_t{0, 0, 0, 0};
       sa = Mma<T>::mul(ka, qf[s], sa);
       sb = Mma<T>::mul(kc, qf[s], sb);
     }
@@ -271,8 +285,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       if (!(vmask >> j & 1)) p[j] = -__builtin_inff();
       top = fmaxf(top, p[j]);
     }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = quarters(top, [](float x, float y) { return fmaxf(x, y); });
     const float m2 = fmaxf(m, top);
     const float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
     if (__any(m2 > m)) {
@@ -331,8 +344,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   }
 
   // The quarters' sums of one head, then the waves.
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  l = quarters(l, [](float x, float y) { return x + y; });
   if (q == 0) {
     s_ml[wave][0][r] = m;
     s_ml[wave][1][r] = l;
@@ -470,6 +482,7 @@ __global__ __launch_bounds__(kJoin) void attn_join_kernel(AttnArgs a, float shif
   store_joined<T>(a, at, seq, d, v, M, L, shift);
 }
 
+
 AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu) {
   // A window reaches from the 8 positions that its first one is in.
   const int64_t span = window > 0 && window < max_length ? (int64_t)window + 7 : max_length;
@@ -479,11 +492,16 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   // need to be levelled out. 64 ragged streams: 131 us with two, 127 with four; one of 131072: 97 and 104.
   const int64_t want = ((n_seqs > 1 ? 4 : 2) * (int64_t)n_cu + groups - 1) / groups;
   int64_t chunk = (span + want - 1) / want;
-  const int64_t unit = kTile * kWaves;
+  const int64_t unit = kTile * kWavesSplit;
   chunk = (chunk + unit - 1) / unit * unit;
   chunk = chunk < unit ? unit : chunk > kChunkMax ? kChunkMax : chunk;
-  const int64_t n = span > 0 ? (span + chunk - 1) / chunk : 1;
   AttnPlan p;
+  p.waves = kWavesSplit;
+  if (span <= (groups < n_cu / 2 ? 256 : 512) && span > chunk) {
+    p.waves = kWavesWhole;
+    chunk = (span + kTile - 1) / kTile * kTile;
+  }
+  const int64_t n = span > 0 ? (span + chunk - 1) / chunk : 1;
   p.chunk = (int)chunk;
   p.n_splits = (int)n;
   p.bytes = n == 1 ? 0 : (size_t)n_seqs * n_heads * n * (head_dim + 2) * sizeof(float);
@@ -499,7 +517,7 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   A.head_tiles = (A.group + 15) / 16;
   const int nh = A.group < 16 ? A.group : 16;
   const size_t tab = (size_t)(a.chunk / a.page_size + 2) * sizeof(int);
-  const size_t acc = (size_t)kWaves * nh * (a.head_dim + 4) * sizeof(float);
+  const size_t acc = (size_t)a.waves * nh * (a.head_dim + 4) * sizeof(float);
   const size_t lds = tab > acc ? tab : acc;
   A.heads = a.n_kv * A.head_tiles;
   const int64_t units = (int64_t)a.n_seqs * a.n_splits;
@@ -512,12 +530,18 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e == hipSuccess) kernel<<<(unsigned)grid, 64 * kWaves, lds, st>>>(A);
+    if (e == hipSuccess) kernel<<<(unsigned)grid, 64 * a.waves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };
-  if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4>);
-  else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8>);
-  else run(attn_kernel<T, PT, F8, 16>);
+  if (a.waves == kWavesSplit) {
+    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, kWavesSplit>);
+    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, kWavesSplit>);
+    else run(attn_kernel<T, PT, F8, 16, kWavesSplit>);
+  } else {
+    if (a.head_dim <= 64) run(attn_kernel<T, PT, F8, 4, kWavesWhole>);
+    else if (a.head_dim <= 128) run(attn_kernel<T, PT, F8, 8, kWavesWhole>);
+    else run(attn_kernel<T, PT, F8, 16, kWavesWhole>);
+  }
   if (e != hipSuccess || a.n_splits == 1) return e;
   if (a.n_splits <= kFewChunks) {
     const int heads = kJoinFew / (a.head_dim / 4);

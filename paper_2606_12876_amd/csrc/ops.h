@@ -60,10 +60,11 @@ struct AttnArgs {
   float* lse;
   int n_heads, n_kv, head_dim;
   int chunk, n_splits;     // positions per workgroup, workgroups along a sequence
+  int waves;               // per workgroup
   float* part;             // n_splits > 1: partial sums and (max, sum) pairs
 };
 // How attention splits a sequence of up to max_length positions (window: as the call).
-struct AttnPlan { int chunk, n_splits; size_t bytes; };
+struct AttnPlan { int chunk, n_splits, waves; size_t bytes; };
 AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu);
 hipError_t launch_attention(const AttnArgs& a, aqmb_dtype dtype, bool f8, hipStream_t st);
 

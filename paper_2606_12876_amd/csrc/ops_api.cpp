@@ -311,6 +311,7 @@ aqmb_status aqmb_paged_attention(const aqmb_kv_cache* cache, const void* q, aqmb
   a.head_dim = c.head_dim;
   a.chunk = plan.chunk;
   a.n_splits = plan.n_splits;
+  a.waves = plan.waves;
   a.part = (float*)workspace;
   return hip_status(launch_attention(a, dtype, c.dtype == AQMB_F8, (hipStream_t)stream), "paged_attention: launch");
 }

@@ -265,7 +265,7 @@ def test_offsets_beyond_32_bits():
 
 def test_workspace_is_checked_and_used():
     g = gen(85)
-    c, table, lens = build(g, [900], 1, 64, 16, torch.float16)
+    c, table, lens = build(g, [900], 1, 64, 16, torch.float16, per=200)      # the bound, not the length, splits
     q = normal(g, 1, 2, 64, dtype=torch.float16)
     want = attend(c, q, table, lens)
     need = c.workspace_bytes(2, 1, table.shape[1] * 16)
