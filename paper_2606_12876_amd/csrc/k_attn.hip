@@ -24,6 +24,7 @@
 // Chunks of a sequence are joined by a second kernel from (max, sum, unnormalised out) in the workspace.
 #include "device.h"
 #include "ops.h"
+#include "wave.h"
 
 namespace aqmb {
 
@@ -97,16 +98,13 @@ __device__ __forceinline__ uint2 as16h(typename Raw<F8, 4>::T r) {
 __device__ __forceinline__ uint32_t lo_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t hi_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// f over the four quarters of a wave, in every lane. Swapping rows of a register with rows of its own copy
-// leaves the pairs side by side, without a trip through LDS.
+// f over the four quarters of a wave.
 template <class F>
 __device__ __forceinline__ float quarters(float x, F f) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const float y = f(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
-  const uint32_t v = __builtin_bit_cast(uint32_t, y);
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return f(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+  return __builtin_bit_cast(float, butterfly<32>(butterfly<16>(__builtin_bit_cast(uint32_t, x), f), f));
+}
+__device__ __forceinline__ uint32_t max_floats(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
 }
 
 struct AttnDev {
@@ -285,7 +283,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       if (!(vmask >> j & 1)) p[j] = -__builtin_inff();
       top = fmaxf(top, p[j]);
     }
-    top = quarters(top, [](float x, float y) { return fmaxf(x, y); });
+    top = quarters(top, max_floats);
     const float m2 = fmaxf(m, top);
     const float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
     if (__any(m2 > m)) {
@@ -344,7 +342,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   }
 
   // The quarters' sums of one head, then the waves.
-  l = quarters(l, [](float x, float y) { return x + y; });
+  l = quarters(l, add_floats);
   if (q == 0) {
     s_ml[wave][0][r] = m;
     s_ml[wave][1][r] = l;

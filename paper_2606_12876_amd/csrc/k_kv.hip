@@ -3,6 +3,7 @@
 // step's few tokens, the launch) bounds both.
 #include "device.h"
 #include "ops.h"
+#include "wave.h"
 
 namespace aqmb {
 
@@ -48,8 +49,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     // The largest magnitude as bits: infinity and NaN come out above every finite value.
 #pragma unroll
     for (int i = 0; i < 8; ++i) big = max(big, __builtin_bit_cast(uint32_t, f[i]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+    big = over_lanes<32>(big, max_bits);
     const bool finite = big < 0x7F800000u;
     const float m = fmaxf(__builtin_bit_cast(float, big), 7.888609052210118e-31f);   // at least 2^-100
     const float mul = 448.f / m;

@@ -9,6 +9,7 @@
 // few (one row of 4096: 2.9 us).
 #include "device.h"
 #include "ops.h"
+#include "wave.h"
 
 namespace aqmb {
 
@@ -57,8 +58,7 @@ struct __attribute__((packed, aligned(1))) B8 { uint32_t w[2]; };
 
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
-#pragma unroll
-  for (int d = NT < 64 ? NT / 2 : 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  v = __builtin_bit_cast(float, over_lanes<(NT < 64 ? NT : 64)>(__builtin_bit_cast(uint32_t, v), add_floats));
   if constexpr (NT > 64) {
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
@@ -73,8 +73,7 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
 // integer maximum also says whether a value is not finite.
 template <int NT>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
-#pragma unroll
-  for (int d = NT < 64 ? NT / 2 : 32; d >= 1; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  v = over_lanes<(NT < 64 ? NT : 64)>(v, max_bits);
   if constexpr (NT > 64) {
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
@@ -190,10 +189,14 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     for (int i = 0; i < NV; ++i) m[i] = all;
   } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      for (int d = g / 16; d >= 1; d >>= 1) m[i] = max(m[i], (uint32_t)__shfl_xor((int)m[i], d));
+    for (int i = 0; i < NV; ++i) {
+      m[i] = over_lanes<4>(m[i], max_bits);
+      if (g >= 64) m[i] = butterfly<4>(m[i], max_bits);
+      if (g >= 128) m[i] = butterfly<8>(m[i], max_bits);
+    }
   }
-  const int n_groups = g ? (a.cols + g - 1) / g : 1;
+  const int shift = g == 0 ? 31 : g == 32 ? 5 : g == 64 ? 6 : 7;      // column -> group
+  const int n_groups = ((a.cols - 1) >> shift) + 1;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * NT + t) * 8, n = a.cols - c;
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     const float big = fmaxf(__builtin_bit_cast(float, m[i]), kScaleFloor);
     const float mul = top / big;
     const float scale = finite ? big / top : __builtin_nanf("");
-    if (g ? c % g == 0 : c == 0) a.scales[row * n_groups + (g ? c / g : 0)] = scale;
+    if ((c & ((1u << shift) - 1)) == 0) a.scales[row * n_groups + (c >> shift)] = scale;
     B8 b;
     if (a.y_dtype == AQMB_F8) {
 #pragma unroll
