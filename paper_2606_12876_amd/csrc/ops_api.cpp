@@ -144,8 +144,8 @@ aqmb_status aqmb_w4_create(aqmb_w4_t* out, const aqmb_w4_desc* desc, const uint8
   if (!desc) return fail(AQMB_EINVAL, "w4_create: descriptor is NULL");
   if (desc->d_out < 1 || desc->d_in < 1)
     return fail(AQMB_EINVAL, "w4_create: d_out = %d and d_in = %d must be >= 1", desc->d_out, desc->d_in);
-  if ((uint64_t)desc->d_out * (uint64_t)desc->d_in >= (1ull << 32))
-    return fail(AQMB_EINVAL, "w4_create: d_out * d_in must be below 2^32");
+  if (desc->d_out > 1 << 30 || desc->d_in > 1 << 30 || (uint64_t)desc->d_out * (uint64_t)desc->d_in >= (1ull << 32))
+    return fail(AQMB_EINVAL, "w4_create: d_out and d_in must be at most 2^30, their product below 2^32");
   if (desc->group_size != 32 && desc->group_size != 64 && desc->group_size != 128)
     return fail(AQMB_EUNSUPPORTED, "w4_create: group_size = %d is not 32, 64 or 128", desc->group_size);
   if (!weights || !scales) return fail(AQMB_EINVAL, "w4_create: weights or scales is NULL");

@@ -163,6 +163,18 @@ def test_long_and_ragged(dtype, cache):
         assert np.all(np.abs(values(one) - ref) <= 2 * half_ulp(ref, dtype) + 1e-4 * np.max(np.abs(ref)))
 
 
+def test_many_short_sequences():
+    g = gen(90)
+    lens_ = [i % 4 for i in range(5000)]
+    c, table, lens = build(g, lens_, 2, 16, 2, torch.bfloat16)
+    q = normal(g, 5000, 4, 16, dtype=torch.bfloat16)
+    out = torch.full_like(q, 9.0)
+    c.attention(q, table, lens, out, scale=0.25)
+    pick = list(range(0, 5000, 61)) + [4999]
+    check(c, q[pick], table[pick], lens[pick], 0.25, 0, out[pick], None)
+    assert (out[torch.tensor(lens_) == 0] == 0).all()
+
+
 def test_split_counts_agree():
     """The same sequence under bounds that split it differently."""
     g = gen(78)

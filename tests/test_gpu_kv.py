@@ -112,6 +112,16 @@ def test_copy_pages(caches, pages, page, kv, dim, pairs, dtype):
         assert torch.equal(bits(t), bits(w))
 
 
+def test_more_pairs_than_one_launch_takes():
+    g = gen(7)
+    n = 40000
+    c = make(g, 2 * n, 1, 1, 8, torch.float16, "head")
+    src = torch.arange(n, dtype=torch.int32, device="cuda")
+    want = c.k[:n].clone()
+    A.kv_copy_pages([c], src, src + n)
+    assert torch.equal(bits(c.k[n:]), bits(want)) and torch.equal(bits(c.k[:n]), bits(want))
+
+
 def test_copy_skips_a_page_onto_itself_and_bad_sources():
     g = gen(2)
     c = make(g, 5, 8, 2, 64, torch.float16, "head")

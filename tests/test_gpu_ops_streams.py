@@ -143,6 +143,27 @@ def test_graph_replays(layer):
     del g
 
 
+def test_graph_of_the_largest_workgroup():
+    """16 heads of 256 on one key-value head: the most LDS the attention takes (over 64 KiB)."""
+    g = gen(9)
+    c = A.KVCache(normal(g, 64, 1, 8, 256, dtype=torch.bfloat16), normal(g, 64, 1, 8, 256, dtype=torch.bfloat16))
+    q = normal(g, 2, 16, 256, dtype=torch.bfloat16)
+    table = torch.arange(64, dtype=torch.int32, device="cuda").view(2, 32)
+    lens = torch.tensor([256, 100], dtype=torch.int32, device="cuda")
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attention(q, table, lens, out, scale=0.06)
+    c.attention(q, table, lens, want, scale=0.06)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del graph
+
+
 def test_results_repeat_bit_for_bit(layer):
     s = Step(5, layer)
     s.run()

@@ -47,7 +47,8 @@ def test_rms_norm_refuses(kw, status):
 
 @pytest.mark.parametrize("d_out,d_in,g,w,s,status", [
     (0, 64, 32, 16, 16, S.EINVAL), (4, 0, 32, 16, 16, S.EINVAL), (4, 64, 16, 16, 16, S.EUNSUPPORTED),
-    (4, 64, 256, 16, 16, S.EUNSUPPORTED), (1 << 17, 1 << 15, 32, 16, 16, S.EINVAL), (4, 64, 32, None, 16, S.EINVAL),
+    (4, 64, 256, 16, 16, S.EUNSUPPORTED), (1 << 17, 1 << 15, 32, 16, 16, S.EINVAL),
+    (1, (1 << 30) + 1, 32, 16, 16, S.EINVAL), ((1 << 30) + 1, 1, 32, 16, 16, S.EINVAL), (4, 64, 32, None, 16, S.EINVAL),
     (4, 64, 32, 16, None, S.EINVAL), (4, 64, 32, 16, 17, S.EINVAL)])
 def test_w4_create_refuses(d_out, d_in, g, w, s, status):
     h, d = ctypes.c_void_p(0x1234), A.W4Desc(d_out, d_in, g)
