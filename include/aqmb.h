@@ -490,7 +490,7 @@ typedef struct {
  *               no position < lengths[s] needs may hold anything. A page outside [0, n_pages) is
  *               skipped: its positions do not exist.
  *   lengths     int32 [n_seqs], device memory; values outside [0, max_length] are clamped
- *   max_length  an upper bound of the lengths, <= table_stride * page_size and <= 2^28: fixes how the work is
+ *   max_length  an upper bound of the lengths, <= table_stride * page_size and <= 2^27: fixes how the work is
  *               split, so results do not depend on other sequences' lengths
  * Slots that hold no token may hold anything (NaN included). Scores and softmax are binary32; the
  * probabilities enter the matrix cores as two 16-bit parts. One rounding to `dtype`.

@@ -834,7 +834,7 @@ class KVCache:
             lp = lse.data_ptr()
         per = tshape[1]
         if max_length is None:
-            max_length = min(per * self.page_size, 1 << 28)
+            max_length = min(per * self.page_size, 1 << 27)
         elif max_length > per * self.page_size:
             _refuse(where, f"max_length = {max_length} needs more pages than the table's {per}")
         need = self.workspace_bytes(heads, n, max_length, window)

@@ -109,7 +109,9 @@ __device__ __forceinline__ uint32_t max_floats(uint32_t a, uint32_t b) {
 
 struct AttnDev {
   AttnArgs a;
-  uint32_t page_magic;     // 2^32 / page_size + 1 (page_size > 1)
+  int page_shift;          // log2 of page_size, -1 if it is no power of two
+  uint32_t page_magic;     // 2^32 / page_size + 1, then
+  uint32_t quad_magic;     // 2^32 / (head_dim / 4) + 1
   int group, head_tiles, heads;   // query heads per key-value head, in tiles of 16; tiles in all
   bool by_unit;
 };
@@ -131,25 +133,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   __shared__ __attribute__((aligned(16))) int64_t s_row[kWaves][32];      // byte offsets of a tile's positions
   __shared__ __attribute__((aligned(16))) float s_scale[kWaves][64];      // scales of its keys, then values
 
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, q = lane / 16;
   // Workgroups go to the XCDs in turn. Either heads do (every XCD has a share of every sequence), or, where
   // heads share cache lines or keys, all heads of a (sequence, chunk) follow each other on one XCD, so
   // that its L2 serves all but the first; sequences are turned by one per chunk, so that an XCD does not
   // keep the same ones. Chunks come last in both: the first ones, which every sequence has, run first, and no
   // XCD is left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which 30 were that).
-  int head, unit;
+  int kvh = blockIdx.x, ht = 0, seq = blockIdx.y, split = blockIdx.z;
   if (A.by_unit) {
-    const int k = blockIdx.x / kXcds;
-    head = k % A.heads;
-    unit = k / A.heads * kXcds + blockIdx.x % kXcds;
+    const int k = blockIdx.x / kXcds, unit = k / A.heads * kXcds + blockIdx.x % kXcds, head = k % A.heads;
     if (unit >= a.n_seqs * a.n_splits) return;
-  } else {
-    head = blockIdx.x % A.heads;
-    unit = blockIdx.x / A.heads;
+    split = unit / a.n_seqs;
+    seq = (unit + split) % a.n_seqs;
+    kvh = head / A.head_tiles;
+    ht = head % A.head_tiles;
   }
-  const int split = unit / a.n_seqs, seq = (unit + (A.by_unit ? split : 0)) % a.n_seqs;
-  const int kvh = head / A.head_tiles, ht = head % A.head_tiles;
   const int h0 = kvh * A.group + ht * 16;                       // first query head
   const int nh = min(16, A.group - ht * 16);
   // Without a window the chunk's place does not depend on the length: pages, length and q are asked for
@@ -157,8 +156,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const int len = max(0, min(a.lengths[seq], a.max_length));
   const int lo = a.window > 0 ? max(0, len - a.window) : 0;
   const int c0 = (lo & ~7) + split * a.chunk, c1 = min(len, c0 + a.chunk);
-  const int p0 = c0 / a.page_size;
-  const int np = (min(a.max_length, c0 + a.chunk) - 1) / a.page_size - p0 + 1;
+  const int reach = max(0, min(a.max_length, c0 + a.chunk) - 1);
+  const int p0 = A.page_shift >= 0 ? c0 >> A.page_shift : c0 / a.page_size;
+  const int np = (A.page_shift >= 0 ? reach >> A.page_shift : reach / a.page_size) - p0 + 1;
   if (c0 < a.max_length)
     for (int i = threadIdx.x; i < np; i += 64 * kWaves) {
       const int p = a.table[seq * a.table_stride + p0 + i];
@@ -200,12 +200,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   for (int e = 0; e < DC; ++e) o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -__builtin_inff(), l = 0.f;
 
-  for (int t0 = c0 + kTile * wave; t0 < c1; t0 += kTile * kWaves) {
+  const int first = c0 + kTile * wave;
+  for (int t0 = first; t0 < c1; t0 += kTile * kWaves) {
     // One look-up for each position of the tile, by lane % 32; LDS hands the offsets (and scales) round.
     // Positions outside are read at one inside and take no part (mask).
     const int pos = t0 + lane % 32;
     const uint32_t rel = (uint32_t)(max(lo, min(pos, c1 - 1)) - base);
-    const uint32_t pi = a.page_size == 1 ? rel : __umulhi(rel, A.page_magic);
+    const uint32_t pi = A.page_shift >= 0 ? rel >> A.page_shift : __umulhi(rel, A.page_magic);
     const int page = pages[pi], slot = (int)(rel - pi * (uint32_t)a.page_size);
     const uint32_t mask = (uint32_t)__ballot(pos >= lo && pos < c1 && page >= 0);
     const int64_t pg = max(page, 0);
@@ -286,13 +287,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     top = quarters(top, max_floats);
     const float m2 = fmaxf(m, top);
     const float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
-    if (__any(m2 > m)) {
-      const float f = __builtin_amdgcn_exp2f(m - m2 == 0.f ? 0.f : (m2 == -__builtin_inff() ? 0.f : m - m2));
+    if (t0 != first && __any(m2 > m)) {
+      const float f = __builtin_amdgcn_exp2f(m2 == -__builtin_inff() ? 0.f : m - m2);
       l *= f;
 #pragma unroll
       for (int e = 0; e < DC; ++e) o[e] *= f;
-      m = m2;
     }
+    m = m2;
     uint32_t ph[4], pl[4];
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const bool one = a.n_splits == 1;
   const int quads = a.head_dim / 4;
   for (int e = threadIdx.x; e < nh * quads; e += 64 * kWaves) {
-    const int h = e / quads, d = e % quads * 4;
+    const int h = (int)__umulhi((uint32_t)e, A.quad_magic), d = (e - h * quads) * 4;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) v += *(const f32x4_t*)(so + (w * nh + h) * pitch + d);
@@ -510,7 +511,11 @@ template <int T, int PT, bool F8>
 static hipError_t go(const AttnArgs& a, hipStream_t st) {
   AttnDev A;
   A.a = a;
+  // Quotients by multiplication: exact while numerator times divisor stays below 2^32 (positions of a chunk
+  // and a page, at most 36896, by 32768; 16 heads by 64).
+  A.page_shift = (a.page_size & (a.page_size - 1)) == 0 ? __builtin_ctz((unsigned)a.page_size) : -1;
   A.page_magic = a.page_size > 1 ? (uint32_t)((1ull << 32) / (uint32_t)a.page_size + 1) : 0;
+  A.quad_magic = (uint32_t)((1ull << 32) / (uint32_t)(a.head_dim / 4) + 1);
   A.group = a.n_heads / a.n_kv;
   A.head_tiles = (A.group + 15) / 16;
   const int nh = A.group < 16 ? A.group : 16;
@@ -523,12 +528,13 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   // whole lines: 16 ragged streams, heads of 80 on an e4m3 cache: 32 us by heads, 25 by units. Tiles of heads
   // share the keys and values themselves.
   A.by_unit = A.head_tiles > 1 || (a.sc_head == 1 && a.n_kv > 1 && a.head_dim * (F8 ? 1 : 2) % 128 != 0);
-  const int64_t grid = (A.by_unit ? (units + kXcds - 1) / kXcds * kXcds : units) * A.heads;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const int64_t ids = (units + kXcds - 1) / kXcds * kXcds * A.heads;
+  if (A.by_unit && ids > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const dim3 grid = A.by_unit ? dim3((unsigned)ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e == hipSuccess) kernel<<<(unsigned)grid, 64 * a.waves, lds, st>>>(A);
+    if (e == hipSuccess) kernel<<<grid, 64 * a.waves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };
   if (a.waves == kWavesSplit) {

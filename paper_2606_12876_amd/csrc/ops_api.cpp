@@ -82,7 +82,7 @@ static aqmb_status check_attention(const aqmb_kv_cache* c, int n_heads, int n_se
     return fail(AQMB_EINVAL, "%s: n_heads = %d is not a multiple of n_kv_heads = %d", where, n_heads, c->n_kv_heads);
   if (n_heads > 65535 || n_seqs > 65535) return fail(AQMB_EUNSUPPORTED, "%s: more than 65535 heads or sequences", where);
   if (n_seqs < 1) return fail(AQMB_EINVAL, "%s: n_seqs = %d must be >= 1", where, n_seqs);
-  if (max_length < 0 || max_length > 1 << 28) return fail(AQMB_EINVAL, "%s: max_length = %d outside [0, 2^28]", where, max_length);
+  if (max_length < 0 || max_length > 1 << 27) return fail(AQMB_EINVAL, "%s: max_length = %d outside [0, 2^27]", where, max_length);
   if (window < 0) return fail(AQMB_EINVAL, "%s: window = %d is negative", where, window);
   return AQMB_OK;
 }
