@@ -244,19 +244,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
         vr[j][i] = *(const typename Raw<F8, VN>::T*)(p + (d < a.head_dim ? d : 0) * E);
       }
     }
-    float ks[8], vs[8];
-    if constexpr (F8) {
+    // The 8 scales of this lane's positions, of keys (which = 0) or values (1); read when they are needed.
+    auto scales = [&](int which, float* to) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const f32x4_t x = *(const f32x4_t*)&s_scale[wave][8 * q + 4 * h], y = *(const f32x4_t*)&s_scale[wave][32 + 8 * q + 4 * h];
+        const f32x4_t x = *(const f32x4_t*)&s_scale[wave][32 * which + 8 * q + 4 * h];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ks[4 * h + e] = x[e];
-          vs[4 * h + e] = y[e];
-        }
+        for (int e = 0; e < 4; ++e) to[4 * h + e] = x[e];
       }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
 
     f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
     const bool ragged = a.head_dim % (F8 ? 64 : 32) != 0;       // steps that reach past head_dim
@@ -275,12 +271,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       sa = Mma<T>::mul(ka, qf[s], sa);
       sb = Mma<T>::mul(kc, qf[s], sb);
     }
-    float p[8];
+    float p[8], sc[8];
+    if constexpr (F8) scales(0, sc);
     float top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       p[j] = (j < 4 ? sa[j] : sb[j - 4]) * scale2;
-      if constexpr (F8) p[j] *= ks[j];
+      if constexpr (F8) p[j] *= sc[j];
       if (!(vmask >> j & 1)) p[j] = -__builtin_inff();
       top = fmaxf(top, p[j]);
     }
@@ -294,14 +291,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       for (int e = 0; e < DC; ++e) o[e] *= f;
     }
     m = m2;
+    if constexpr (F8) scales(1, sc);
     uint32_t ph[4], pl[4];
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
       float x = __builtin_amdgcn_exp2f(p[j] - mu), y = __builtin_amdgcn_exp2f(p[j + 1] - mu);
       l += x + y;
       if constexpr (F8) {
-        x = vmask >> j & 1 ? x * vs[j] : 0.f;
-        y = vmask >> (j + 1) & 1 ? y * vs[j + 1] : 0.f;
+        x = vmask >> j & 1 ? x * sc[j] : 0.f;
+        y = vmask >> (j + 1) & 1 ? y * sc[j + 1] : 0.f;
       }
       Mma<PT>::split(x, y, ph[j / 2], pl[j / 2]);
     }
@@ -310,36 +308,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     // V^T: values of 8 positions, transposed. A position that takes no part must be 0, not garbage; rows of
     // V^T past head_dim may be anything, they are rows of a result that nobody reads.
 #pragma unroll
-    for (int i = 0; i < VL; ++i) {
-      uint32_t v[8][VN / 2];
+    for (int i = 0; i < DC / 4; ++i) {                           // 4 values at a time
+      uint2 v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if constexpr (VN == 8) {
-          const u32x4_t w = as16<PT, F8>(vr[j][i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[j][e] = w[e];
+        if constexpr (VN == 4) {
+          v[j] = as16h<PT, F8>(vr[j][i]);
+        } else if constexpr (F8) {
+          v[j] = widen_f8<PT>(i % 2 ? vr[j][i / 2].y : vr[j][i / 2].x);
         } else {
-          const uint2 w = as16h<PT, F8>(vr[j][i]);
-          v[j][0] = w.x;
-          v[j][1] = w.y;
+          v[j] = make_uint2(vr[j][i / 2][2 * (i % 2)], vr[j][i / 2][2 * (i % 2) + 1]);
         }
       }
       if (mask != 0xFFFFFFFFu) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int e = 0; e < VN / 2; ++e) v[j][e] = vmask >> j & 1 ? v[j][e] : 0;
+        for (int j = 0; j < 8; ++j) v[j] = vmask >> j & 1 ? v[j] : make_uint2(0, 0);
       }
 #pragma unroll
-      for (int e = 0; e < VN; ++e) {
+      for (int e = 0; e < 4; ++e) {
         u32x4_t w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = e % 2 ? hi_halves(v[2 * j][e / 2], v[2 * j + 1][e / 2]) : lo_halves(v[2 * j][e / 2], v[2 * j + 1][e / 2]);
-        o[i * VN + e] = Mma<PT>::mul(w, pho, o[i * VN + e]);
-        o[i * VN + e] = Mma<PT>::mul(w, plo, o[i * VN + e]);
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t x = e < 2 ? v[2 * j].x : v[2 * j].y, y = e < 2 ? v[2 * j + 1].x : v[2 * j + 1].y;
+          w[j] = e % 2 ? hi_halves(x, y) : lo_halves(x, y);
+        }
+        o[4 * i + e] = Mma<PT>::mul(w, pho, o[4 * i + e]);
+        o[4 * i + e] = Mma<PT>::mul(w, plo, o[4 * i + e]);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
   // The quarters' sums of one head, then the waves.
