@@ -257,7 +257,9 @@ __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   };
   auto load_tile = [&](size_t tile) {
     Tile t;
-    t.w = __builtin_nontemporal_load(a.tiles + tile * 64 + lane);
+    // Cached, not streaming: models of up to the Infinity Cache's 256 MB then find their weights there at the
+    // next step (4096 x 11008 int8 at 16 rows: 7.4 against 9.7 us), for 3 to 5 % more where they do not fit.
+    t.w = a.tiles[tile * 64 + lane];
     const uint16_t* s = a.scales + tile * (16 * kGroups);
     t.p.s = *(const decltype(t.p.s)*)(s + 4 * kGroups * q);
     if constexpr (kGroups == 4) t.p.s2 = *(const u32x4_t*)(s + 4 * kGroups * q + 8);
