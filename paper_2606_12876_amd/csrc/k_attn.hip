@@ -483,7 +483,7 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   // A window reaches from the 8 positions that its first one is in.
   const int64_t span = window > 0 && window < max_length ? (int64_t)window + 7 : max_length;
   const int64_t groups = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
-  
+
   // Workgroups along a sequence: two on every unit, four where several sequences (whose lengths differ)
   // need to be levelled out. 64 ragged streams: 131 us with two, 127 with four; one of 131072: 97 and 104.
   const int64_t want = ((n_seqs > 1 ? 4 : 2) * (int64_t)n_cu + groups - 1) / groups;
@@ -493,7 +493,12 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   chunk = chunk < unit ? unit : chunk > kChunkMax ? kChunkMax : chunk;
   AttnPlan p;
   p.waves = kWavesSplit;
-  if (span <= (groups < n_cu / 2 ? 256 : 512) && span > chunk) {
+  // Short sequences stay whole, with twice the waves, which saves the second launch. Per call from the host
+  // whole and split, 8 key-value heads of 128 (queries 4 times as many): one sequence of 300, 6.9 and 10.8 us;
+  // of 500, 8.5 and 10.8 (in a graph 8.4 and 7.3); 700 costs 10.8 either way. Heads of 64 and 1000 positions:
+  // 8.9 and 10.7 us for one sequence (in a graph 8.8 and 7.1), 16.4 and 19.8 for 64. Heads of 256 with 250
+  // positions: 9.3 and 10.9.
+  if (span <= (head_dim <= 64 ? 1024 : head_dim <= 128 ? 512 : 256) && span > chunk) {
     p.waves = kWavesWhole;
     chunk = (span + kTile - 1) / kTile * kTile;
   }
