@@ -163,6 +163,23 @@ def test_long_and_ragged(dtype, cache):
         assert np.all(np.abs(values(one) - ref) <= 2 * half_ulp(ref, dtype) + 1e-4 * np.max(np.abs(ref)))
 
 
+@pytest.mark.parametrize("dtype,cache", [(torch.float16, None), (torch.bfloat16, None), (torch.bfloat16, F8)])
+@pytest.mark.parametrize("layout", ["head", "slot"])
+@pytest.mark.parametrize("dim", [8, 64, 72, 128, 136, 256])
+def test_split_sequences(dim, layout, dtype, cache):
+    """Chunks that are full, partly full and empty, joined: many of them, and two or three of each sequence."""
+    g = gen(dim + 1)
+    lens_ = [1030, 0, 1, 128, 129, 700]
+    c, table, lens = build(g, lens_, 2, dim, 20, dtype, cache, layout)
+    q = normal(g, len(lens_), 6, dim, dtype=dtype, std=2.0)
+    assert c.workspace_bytes(6, len(lens_), 1030) > 0
+    attend(c, q, table, lens, max_length=1030)
+    attend(c, q, table, lens, max_length=1030, window=1028)
+    lens_ = [1100, 0, 1, 384, 512, 513, 1025] + [64] * 25
+    c, table, lens = build(g, lens_, 8, dim, 20, dtype, cache, layout)
+    attend(c, normal(g, len(lens_), 8, dim, dtype=dtype, std=2.0), table, lens)
+
+
 def test_many_short_sequences():
     g = gen(90)
     lens_ = [i % 4 for i in range(5000)]
