@@ -115,11 +115,10 @@ __device__ __forceinline__ Bytes16 load_end(const E* row, int k, int d_in) {
   return v;
 }
 
-// Four e4m3 values as fp16.
+// Four e4m3 values as fp16, exactly.
 __device__ __forceinline__ uint2 widen_f8(uint32_t w) {
-  typedef float f32x2_t __attribute__((ext_vector_type(2)));
-  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  return make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(b.x, b.y));
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true)));
 }
 
 // How each type of x meets the nibbles. X: 8 neighbouring inputs of one row.
