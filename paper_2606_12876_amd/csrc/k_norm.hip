@@ -5,28 +5,48 @@
 // A row is read once and stays in registers: NT threads own 8 consecutive columns each, NV times
 // over, so the sum of squares, the largest magnitude of a scale group (g / 8 neighbouring lanes) and
 // the output need no second pass over memory. Bound by HBM for many rows (8192 x 4096 bf16 with a
-// residual to e4m3: 49 us, 4.8 TB/s, a large copy's rate), by latency (load, two reductions, store) for
-// few (one row of 4096: 2.9 us).
+// residual to e4m3: 43 us, 5.5 TB/s, more than a large copy's rate), by latency (load, two reductions,
+// store) for few (one row of 4096: 2.4 us).
 #include "device.h"
 #include "ops.h"
 #include "wave.h"
 
 namespace aqmb {
 
-// 8 consecutive 16-bit elements, of which the first n exist (n <= 0: none). Rows may start at any
-// element: the 16-byte access needs no alignment beyond the element's on gfx950.
+// 8 consecutive 16-bit elements. Rows may start at any element: the 16-byte access needs no alignment
+// beyond the element's on gfx950.
 struct __attribute__((packed, aligned(2))) Raw8 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(2))) Raw4 { uint32_t w[2]; };
+struct __attribute__((packed, aligned(2))) Raw2 { uint32_t w; };
 
-__device__ __forceinline__ Raw8 load8(const uint16_t* p, int n) {
-  Raw8 r = {{0, 0, 0, 0}};
-  if (n >= 8) {
-    r = *(const Raw8*)p;
-  } else {
+// Columns c .. c + 7 of a row. What reaches over the row's end is its last 8 columns, for shift8 to put right:
+// one load for every lane and no branch around it (element by element, with a wait for each, 4000 rows of 4095
+// took 42 us, not 30). kShort: rows may have fewer than 8 columns, 0 past the end.
+template <bool kShort>
+__device__ __forceinline__ Raw8 load8(const uint16_t* row, int c, int cols) {
+  if (kShort && cols < 8) {
+    Raw8 r = {{0, 0, 0, 0}};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) r.w[i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
+      if (c + i < cols) r.w[i / 2] |= (uint32_t)row[c + i] << (16 * (i % 2));
+    return r;
   }
-  return r;
+  return *(const Raw8*)(row + min(c, cols - 8));
+}
+
+// past elements to the left, 0 from the right.
+__device__ __forceinline__ void shift8(Raw8& r, int past) {
+  uint32_t a = r.w[0], b = r.w[1], c = r.w[2], d = r.w[3];
+  const bool four = past & 4, two = past & 2;
+  const uint32_t odd = 16 * (past & 1);
+  a = four ? c : a, b = four ? d : b, c = four ? 0 : c, d = four ? 0 : d;
+  a = two ? b : a, b = two ? c : b, c = two ? d : c, d = two ? 0 : d;
+  a = __builtin_amdgcn_alignbit(b, a, odd);
+  b = __builtin_amdgcn_alignbit(c, b, odd);
+  c = __builtin_amdgcn_alignbit(d, c, odd);
+  d >>= odd;
+  const bool none = past >= 8;
+  r = Raw8{{none ? 0 : a, none ? 0 : b, none ? 0 : c, none ? 0 : d}};
 }
 
 template <int DT>
@@ -46,15 +66,18 @@ __device__ __forceinline__ void store8_16(uint16_t* p, const float* f, int n) {
     r.w[i] = DT == AQMB_F16 ? pack_f16x2(f[2 * i], f[2 * i + 1]) : pack_bf16x2(f[2 * i], f[2 * i + 1]);
   if (n >= 8) {
     *(Raw8*)p = r;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint16_t)(r.w[i / 2] >> (16 * (i % 2)));
+  } else if (n > 0) {
+    if (n & 4) *(Raw4*)p = Raw4{{r.w[0], r.w[1]}}, p += 4, r.w[0] = r.w[2], r.w[1] = r.w[3];
+    if (n & 2) *(Raw2*)p = Raw2{r.w[0]}, p += 2, r.w[0] = r.w[1];
+    if (n & 1) *p = (uint16_t)r.w[0];
   }
 }
 
 struct __attribute__((packed, aligned(4))) F4 { float f[4]; };
+struct __attribute__((packed, aligned(4))) F2 { float f[2]; };
 struct __attribute__((packed, aligned(1))) B8 { uint32_t w[2]; };
+struct __attribute__((packed, aligned(1))) B4 { uint32_t w; };
+struct __attribute__((packed, aligned(1))) B2 { uint16_t w; };
 
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
@@ -91,33 +114,39 @@ template <int DT, int NT, int NV>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
   __shared__ float lds_sum[16];
   __shared__ uint32_t lds_max[16];
+  constexpr bool kShort = NT == 16;
   const int t = NT <= 64 ? threadIdx.x % NT : threadIdx.x;
   const int64_t row = NT <= 64 ? (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT : blockIdx.x;
   if (NT <= 64 && row >= a.rows) return;      // all lanes of the row, and no barrier below for NT <= 64
   const uint16_t* x = (const uint16_t*)a.x + row * a.x_stride;
   const uint16_t* r = a.residual ? (const uint16_t*)a.residual + row * a.residual_stride : nullptr;
 
+  // All loads first.
   float h[NV][8];
-  Raw8 w[NV];
+  Raw8 hx[NV], hr[NV], w[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * NT + t) * 8;
-    widen8<DT>(load8(x + c, a.cols - c), h[i]);
-  }
+  for (int i = 0; i < NV; ++i) hx[i] = load8<kShort>(x, (i * NT + t) * 8, a.cols);
   if (r) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * NT + t) * 8;
+    for (int i = 0; i < NV; ++i) hr[i] = load8<kShort>(r, (i * NT + t) * 8, a.cols);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) w[i] = load8<kShort>((const uint16_t*)a.weight, (i * NT + t) * 8, a.cols);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int past = (i * NT + t) * 8 - (a.cols - 8);
+    if (past > 0 && !(kShort && a.cols < 8)) {
+      shift8(hx[i], past);
+      if (r) shift8(hr[i], past);
+      shift8(w[i], past);
+    }
+    widen8<DT>(hx[i], h[i]);
+    if (r) {
       float f[8];
-      widen8<DT>(load8(r + c, a.cols - c), f);
+      widen8<DT>(hr[i], f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[i][j] += f[j];
     }
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * NT + t) * 8;
-    w[i] = load8((const uint16_t*)a.weight + c, a.cols - c);
   }
   float ss = 0.f;
 #pragma unroll
@@ -162,10 +191,15 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
       if (n >= 8) {
         ((F4*)y)[0] = F4{{h[i][0], h[i][1], h[i][2], h[i][3]}};
         ((F4*)y)[1] = F4{{h[i][4], h[i][5], h[i][6], h[i][7]}};
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < n) y[j] = h[i][j];
+      } else if (n > 0) {
+        f32x4_t f = {h[i][0], h[i][1], h[i][2], h[i][3]};
+        if (n & 4) {
+          *(F4*)y = F4{{f[0], f[1], f[2], f[3]}};
+          y += 4;
+          f = f32x4_t{h[i][4], h[i][5], h[i][6], 0.f};
+        }
+        if (n & 2) *(F2*)y = F2{{f[0], f[1]}};
+        if (n & 1) y[n & 2] = n & 2 ? f[2] : f[0];
       }
     }
     return;
@@ -226,9 +260,9 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     if (n >= 8) {
       *(B8*)y = b;
     } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < n) y[j] = (uint8_t)(b.w[j / 4] >> (8 * (j % 4)));
+      if (n & 4) *(B4*)y = B4{b.w[0]}, y += 4, b.w[0] = b.w[1];
+      if (n & 2) *(B2*)y = B2{(uint16_t)b.w[0]}, y += 2, b.w[0] >>= 16;
+      if (n & 1) *y = (uint8_t)b.w[0];
     }
   }
 }
@@ -241,10 +275,11 @@ static hipError_t go(const NormArgs& a, hipStream_t st) {
 }
 
 // Threads for a row: one 8-column piece each as far as that goes (a launch of few rows is bound by its
-// chain of loads, reductions and cold code: 4096 columns, 1 row: 512 threads x 1 piece 2.9 us, 256 x 2 3.1,
-// 128 x 4 3.7, 1024 x 1 3.5; 8192 rows 49.6, 52.3, 51.5 and 62.9 us) and no more threads than pieces. 128
-// columns, 65536 rows: 16 threads 15.9 us, 32 21.4. From 257 columns a wave's lanes are half idle and many rows
-// gain by two pieces (512 columns, 16384 rows: 13.5 against 16.3 us; 64 rows: 3.2 against 2.9).
+// chain of loads, reductions and cold code: 4096 columns, 1 row: 512 threads x 1 piece 2.4 us, 256 x 2 2.5,
+// 128 x 4 3.1, 1024 x 1 3.1; 8192 rows 46.0, 45.5, 47.3 and 50.6 us) and no more threads than pieces. 128
+// columns, 65536 rows: 16 threads 15.6 us, 32 19.3. From 257 columns a wave's lanes are half idle and many rows
+// gain by two pieces (512 columns, 16384 rows: 14.6 against 15.1 us; 64 rows: 2.7 against 2.5). Above 768
+// pieces two cost few rows nothing (8192 columns, 1 row: 512 x 2 2.8 us, 1024 x 1 2.9; 4096 rows: 46.2, 48.4).
 template <int DT>
 static hipError_t choose(const NormArgs& a, hipStream_t st) {
   const int v = (a.cols + 7) / 8;
@@ -256,7 +291,7 @@ static hipError_t choose(const NormArgs& a, hipStream_t st) {
   if (v <= 384) return go<DT, 384, 1>(a, st);
   if (v <= 512) return go<DT, 512, 1>(a, st);
   if (v <= 768) return go<DT, 768, 1>(a, st);
-  if (v <= 1024) return go<DT, 1024, 1>(a, st);
+  if (v <= 1024) return go<DT, 512, 2>(a, st);
   if (v <= 1536) return go<DT, 768, 2>(a, st);
   if (v <= 2048) return go<DT, 1024, 2>(a, st);
   return go<DT, 1024, 4>(a, st);
