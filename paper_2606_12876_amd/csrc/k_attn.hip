@@ -117,8 +117,8 @@ struct AttnDev {
   int page_shift;          // log2 of page_size, -1 if it is no power of two
   uint32_t page_magic;     // 2^32 / page_size + 1, then
   uint32_t quad_magic;     // 2^32 / (head_dim / 4) + 1
-  int group, head_tiles, heads;   // query heads per key-value head, in tiles of 16; tiles in all
-  bool by_unit;
+  int group, head_tiles;   // query heads per key-value head, in tiles of 16
+  int block, blocks;       // 0, or the tiles of the heads that share cache lines, and such blocks in all
 };
 
 // 16 bytes at a multiple of 8.
@@ -141,16 +141,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, q = lane / 16;
   // Workgroups go to the XCDs in turn. Either heads do (every XCD has a share of every sequence), or, where
-  // heads share cache lines or keys, all heads of a (sequence, chunk) follow each other on one XCD, so
+  // heads share cache lines or keys, those of a (sequence, chunk) that do follow each other on one XCD, so
   // that its L2 serves all but the first; sequences are turned by one per chunk, so that an XCD does not
   // keep the same ones. Chunks come last in both: the first ones, which every sequence has, run first, and no
   // XCD is left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which 30 were that).
   int kvh = blockIdx.x, ht = 0, seq = blockIdx.y, split = blockIdx.z;
-  if (A.by_unit) {
-    const int k = blockIdx.x / kXcds, unit = k / A.heads * kXcds + blockIdx.x % kXcds, head = k % A.heads;
-    if (unit >= a.n_seqs * a.n_splits) return;
-    split = unit / a.n_seqs;
-    seq = (unit + split) % a.n_seqs;
+  if (A.block) {
+    const int k = blockIdx.x / kXcds, unit = k / A.block * kXcds + blockIdx.x % kXcds, row = a.n_seqs * A.blocks;
+    if (unit >= row * a.n_splits) return;
+    split = unit / row;
+    const int rest = unit - split * row, s = rest / A.blocks, head = (rest - s * A.blocks) * A.block + k % A.block;
+    seq = (s + split) % a.n_seqs;
     kvh = head / A.head_tiles;
     ht = head % A.head_tiles;
   }
@@ -532,15 +533,22 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   const size_t tab = (size_t)(a.chunk / a.page_size + 2) * sizeof(int);
   const size_t acc = (size_t)a.waves * nh * (a.head_dim + 4) * sizeof(float);
   const size_t lds = tab > acc ? tab : acc;
-  A.heads = a.n_kv * A.head_tiles;
-  const int64_t units = (int64_t)a.n_seqs * a.n_splits;
-  // Heads share cache lines (128 bytes) where tokens are outermost in a page and a head does not fill
-  // whole lines: 16 ragged streams, heads of 80 on an e4m3 cache: 32 us by heads, 25 by units. Tiles of heads
-  // share the keys and values themselves.
-  A.by_unit = A.head_tiles > 1 || (a.sc_head == 1 && a.n_kv > 1 && a.head_dim * (F8 ? 1 : 2) % 128 != 0);
-  const int64_t ids = (units + kXcds - 1) / kXcds * kXcds * A.heads;
-  if (A.by_unit && ids > 0x7FFFFFFF) return hipErrorInvalidValue;
-  const dim3 grid = A.by_unit ? dim3((unsigned)ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
+  // Heads share cache lines (128 bytes) where tokens are outermost in a page and a head does not fill whole
+  // lines. Under 192 bytes they are taken in the smallest blocks that do; 25 ragged streams of up to 4557, 8 heads:
+  // of 160 bytes in fours and each by itself, 47.8 us both (64 of up to 2000: 55.6 and 58.6; 4 of up to 20000:
+  // 32 and 42; all 8 heads on one XCD: 58, 62 and 37); of 96, 41.3 and 47.0; of 192, 52.0 and 48.3; of 64, 33.3
+  // and 35.7. Tiles of heads share the keys and values themselves.
+  const int bytes = a.head_dim * (F8 ? 1 : 2);
+  int share = 1;
+  if (a.sc_head == 1 && bytes < 192)
+    while (share < a.n_kv && share * bytes % 128 != 0) share *= 2;
+  if (a.n_kv % share != 0) share = a.n_kv;
+  A.block = share * A.head_tiles > 1 ? share * A.head_tiles : 0;
+  A.blocks = a.n_kv / share;
+  const int64_t units = (int64_t)a.n_seqs * a.n_splits * A.blocks;
+  const int64_t ids = (units + kXcds - 1) / kXcds * kXcds * A.block;
+  if (ids > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const dim3 grid = A.block ? dim3((unsigned)ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

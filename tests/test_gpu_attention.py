@@ -180,6 +180,19 @@ def test_split_sequences(dim, layout, dtype, cache):
     attend(c, normal(g, len(lens_), 8, dim, dtype=dtype, std=2.0), table, lens)
 
 
+@pytest.mark.parametrize("kv,per", [(1, 17), (3, 2), (5, 1), (6, 20), (12, 1), (16, 3)])
+@pytest.mark.parametrize("dim", [8, 24, 64, 80])
+@pytest.mark.parametrize("cache", [None, F8])
+def test_heads_that_share_lines(cache, dim, kv, per):
+    """Every (sequence, head, chunk) is done once where heads lie side by side and do not fill cache lines."""
+    g = gen(100 * kv + dim)
+    lens_ = [1030, 3, 0, 400, 77]
+    c, table, lens = build(g, lens_, kv, dim, 16, torch.float16, cache, "slot")
+    q = normal(g, 5, kv * per, dim, dtype=torch.float16, std=2.0)
+    attend(c, q, table, lens)
+    attend(c, q[1:], table[1:], lens[1:], max_length=400)
+
+
 def test_many_short_sequences():
     g = gen(90)
     lens_ = [i % 4 for i in range(5000)]
