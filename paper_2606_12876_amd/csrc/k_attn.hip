@@ -485,17 +485,17 @@ __global__ __launch_bounds__(kJoin) void attn_join_kernel(AttnArgs a, float shif
 }
 
 
-AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, bool f8, int n_seqs, int max_length, int window, int n_cu) {
+AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu) {
   // A window reaches from the 8 positions that its first one is in.
   const int64_t span = window > 0 && window < max_length ? (int64_t)window + 7 : max_length;
   const int64_t groups = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
 
-  // Workgroups along a sequence: two on every unit, more where several sequences (whose lengths differ) need
-  // to be levelled out: four with a 16-bit cache, of which three run at once, six with an 8-bit one (four).
-  // One sequence of 131072: 97 us with two, 104 with four. 32 ragged streams of up to 6000, 16 bits: 88 us
-  // with four, 94 with six; 64 of up to 8192, 8 bits: 129 with four, 112 with six, 123 with eight.
-  const int per_cu = n_seqs == 1 ? 2 : f8 ? 6 : 4;
-  const int64_t want = (per_cu * (int64_t)n_cu + groups - 1) / groups;
+  // Workgroups along a sequence: two on every unit, five where several sequences (whose lengths differ) need to
+  // be levelled out: three run at once with a 16-bit cache, four with an 8-bit one. One sequence of 131072: 97 us
+  // with two, 104 with four. Ragged streams, over eight sets of lengths, with four, five, six and eight: 32 of up
+  // to 6000, 16 bits, 89, 87, 90, 88 us; 200 of up to 1500 124, 121, 121, 125. 8 bits, with five, six and eight: 64
+  // of up to 8192 122, 121, 131; 8 of up to 16000 44, 50, 48.
+  const int64_t want = ((n_seqs > 1 ? 5 : 2) * (int64_t)n_cu + groups - 1) / groups;
   int64_t chunk = (span + want - 1) / want;
   const int64_t unit = kTile * kWavesSplit;
   chunk = (chunk + unit - 1) / unit * unit;

@@ -65,7 +65,7 @@ struct AttnArgs {
 };
 // How attention splits a sequence of up to max_length positions (window: as the call).
 struct AttnPlan { int chunk, n_splits, waves; size_t bytes; };
-AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, bool f8, int n_seqs, int max_length, int window, int n_cu);
+AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_length, int window, int n_cu);
 hipError_t launch_attention(const AttnArgs& a, aqmb_dtype dtype, bool f8, hipStream_t st);
 
 hipError_t launch_kv_append(const aqmb_kv_cache& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride,

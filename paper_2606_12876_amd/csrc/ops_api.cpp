@@ -250,8 +250,7 @@ aqmb_status aqmb_paged_attention_workspace_bytes(const aqmb_kv_cache* cache, int
   int n_cu = 0;
   const hipError_t e = compute_units(&n_cu);
   if (e != hipSuccess) return hip_status(e, "paged_attention_workspace_bytes");
-  *bytes = attn_plan(n_heads, cache->n_kv_heads, cache->head_dim, cache->dtype == AQMB_F8, n_seqs, max_length, window,
-                     n_cu).bytes;
+  *bytes = attn_plan(n_heads, cache->n_kv_heads, cache->head_dim, n_seqs, max_length, window, n_cu).bytes;
   return AQMB_OK;
 }
 
@@ -277,7 +276,7 @@ aqmb_status aqmb_paged_attention(const aqmb_kv_cache* cache, const void* q, aqmb
   int n_cu = 0;
   hipError_t e = compute_units(&n_cu);
   if (e != hipSuccess) return hip_status(e, where);
-  const AttnPlan plan = attn_plan(n_heads, c.n_kv_heads, c.head_dim, c.dtype == AQMB_F8, n_seqs, max_length, window, n_cu);
+  const AttnPlan plan = attn_plan(n_heads, c.n_kv_heads, c.head_dim, n_seqs, max_length, window, n_cu);
   if (plan.bytes && (!workspace || workspace_bytes < plan.bytes))
     return fail(AQMB_EINVAL, "%s: workspace of %zu bytes, %zu needed", where, workspace ? workspace_bytes : (size_t)0, plan.bytes);
   if (plan.bytes && !aligned(workspace, 16)) return fail(AQMB_EINVAL, "%s: workspace must be 16-byte aligned", where);
