@@ -13,7 +13,7 @@
 // they lose digits: the subnormals 0x000q of fp16 and 0x0q of e4m3 stand for q 2^-24 and q 2^-9, but the
 // matrix cores line products up by their unnormalised exponents, and a sum of them keeps only about 17
 // bits (measured: 1.1e-4 of the result at 4096 x 4096).
-// so a dword of eight weights costs 3 (int8) or 8 vector instructions. sum x is a second product with a row
+// A dword of eight weights costs 3 (int8) or 8 vector instructions. sum x is a second product with a row
 // of ones: it arrives in every lane that needs it, with the same grouping and order of sums.
 #include <type_traits>
 
@@ -368,9 +368,9 @@ static hipError_t by_batch(const W4Args& a, hipStream_t st) {
 }
 // Row tiles per workgroup: as many as give every compute unit one workgroup (or one a round, of at most
 // 4 tiles), so that no round is partly filled and x is read once for all of them. 11008 x 4096 (688 row
-// tiles, 256 units), groups of 64 with zero points, 11 rows: 1 tile 11.3 us, 2 tiles 11.7, 3 tiles 10.2;
-// 14336 x 4096 e4m3, 16 rows: 1 tile 13.5, 2 tiles 12.1, 4 tiles 10.9. One tile takes 16 waves (4096 x 4096 at
-// 16 rows 5.7 us, with 8 waves 6.1), unless there are too few input tiles for them.
+// tiles, 256 units), groups of 64 with zero points, 11 rows: 1 tile 11.6 us, 2 tiles 9.9, 3 tiles 8.9, 4 tiles
+// 10.7; 14336 x 4096 e4m3, 16 rows: 1 tile 14.0, 2 tiles 10.0, 4 tiles 9.7. One tile takes 16 waves (4096 x
+// 11008 int8 at 16 rows 7.3 us, with 8 waves 7.9), unless there are too few input tiles for them.
 template <int XT, int G>
 static hipError_t go(const W4Args& a, int n_cu, hipStream_t st) {
   const int n_rt = (a.d_out - 1) / kW4Rows + 1, rounds = (n_rt - 1) / (4 * n_cu) + 1;
