@@ -162,6 +162,17 @@ lib = _load()
 
 import torch  # noqa: E402  (after the library's own import of it, see _load)
 
+# The operators between the layers take their usual calls past ctypes: _direct checks the tensors, makes the call
+# and returns its status, or None where the functions below have to look.
+try:
+    from . import _direct  # noqa: E402
+except ImportError as e:
+    raise ImportError(f"{os.path.join(os.path.dirname(LIB_PATH), '_direct.so')} is missing or was built for another "
+                      f"PyTorch: build it first (python -m paper_2606_12876_amd.build)") from e
+_direct.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+    "aqmb_rms_norm", "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes",
+    "aqmb_kv_append", "aqmb_kv_copy_pages")))
+
 _TORCH_DT = {torch.float16: int(DType.F16), torch.bfloat16: int(DType.BF16), torch.float32: int(DType.F32)}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _get_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -580,8 +591,11 @@ def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=N
     [rows][cols] fp16 or bf16; y is a tensor of the same shape: fp16, bf16, fp32, or (with scales
     [rows][ceil(cols / scale_group)] fp32; scale_group 0 is the whole row) float8_e4m3fn or int8.
     With a residual, x + residual is rounded into residual_out."""
-    # Decode steps call this per layer, so the usual case (dense tensors) is checked with as few calls as it takes.
     where = "aqmb_rms_norm"
+    if stream is None:
+        st = _direct.rms_norm(x, weight, y, eps, weight_offset, residual, residual_out, scales, scale_group)
+        if st is not None:
+            return _check(st, where) if st else None
     shape, dtype, dev = x.shape, x.dtype, _current_device()
     if len(shape) != 2:
         _refuse(where, f"x is {tuple(shape)}, not (rows, cols)")
@@ -655,6 +669,10 @@ def w4_get_desc(layer: int) -> W4Desc:
 
 def _w4_gemv(layer: int, d_out: int, d_in: int, group_size: int, x, y, x_scales, stream) -> None:
     where = "aqmb_w4_gemv"
+    if stream is None:
+        st = _direct.w4_gemv(layer, d_out, d_in, group_size, x, y, x_scales)
+        if st is not None:
+            return _check(st, where) if st else None
     shape, yshape = x.shape, y.shape
     if len(shape) != 2:
         _refuse(where, f"x is {tuple(shape)}, not (batch, d_in)")
@@ -770,6 +788,7 @@ class KVCache:
                                 k.stride(0) if k.shape[0] > 1 else page, int(dt), int(lay), k.shape[0], size, heads,
                                 k.shape[3])
         self._ref = ctypes.byref(self.desc)
+        self._address = ctypes.addressof(self.desc)
         self._plans = {}
 
     @classmethod
@@ -806,6 +825,11 @@ class KVCache:
         (default: what the table holds). Without a workspace one is taken from PyTorch's allocator on the
         call's stream."""
         where = "aqmb_paged_attention"
+        if stream is None:
+            st = _direct.paged_attention(self._address, self.device_index, q, page_table, lengths, out, scale, max_length,
+                                         window, lse, workspace)
+            if st is not None:
+                return _check(st, where) if st else None
         dev = _current_device()
         if dev != self.device_index:
             self._current(where)
@@ -868,6 +892,10 @@ class KVCache:
         """aqmb_kv_append: write k, v [n_tokens][n_kv_heads][head_dim] (fp16 or bf16) into slots int64
         [n_tokens] on the GPU (page * page_size + offset; outside the cache: skipped)."""
         where = "aqmb_kv_append"
+        if stream is None:
+            st = _direct.kv_append(self._address, self.device_index, k, v, slots)
+            if st is not None:
+                return _check(st, where) if st else None
         dev = _current_device()
         if dev != self.device_index:
             self._current(where)
@@ -904,7 +932,12 @@ def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
 def kv_copy_pages(caches, src, dst, stream=None) -> None:
     """aqmb_kv_copy_pages: page src[i] to page dst[i] (int32, on the GPU) in every KVCache of `caches`."""
     where = "aqmb_kv_copy_pages"
-    caches = list(caches)
+    if not isinstance(caches, (list, tuple)):
+        caches = list(caches)
+    if stream is None:
+        st = _direct.kv_copy_pages(caches, src, dst)
+        if st is not None:
+            return _check(st, where) if st else None
     _here(where, src=src, dst=dst)
     for c in caches:
         c._current(where)

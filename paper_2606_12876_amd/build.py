@@ -3,15 +3,18 @@
 Objects go to ``_build/`` at the repository root; the shared library is written next to
 this file, where the binding loads it. Every HIP source is compiled with packed-fp32
 instruction generation turned off. ``libaqmb_ceilings.so`` (the benchmark's measured-ceiling
-kernels, not part of the layer) is built beside it.
+kernels, not part of the layer) and ``_direct.so`` (the binding's way from tensors to the library
+without ctypes; host code against the headers of Python and of the installed PyTorch) are built beside it.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -19,7 +22,9 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libaqmb.so")
 CEIL_SOURCES = ["ceilings.hip"]
+DIRECT_SOURCES = ["direct.cpp"]
 CEIL_LIB = os.path.join(HERE, "libaqmb_ceilings.so")
+DIRECT_LIB = os.path.join(HERE, "_direct.so")
 
 SOURCES = ["validate.cpp", "api.cpp", "k_dequant.hip", "k_gemv.hip", "k_gemv16.hip", "k_gemv4.hip", "k_gemv_mma.hip", "k_gemm.hip", "k_gemm_small.hip", "k_gemm_mid.hip", "k_distortion.hip", "k_beam.hip", "k_beam_mma.hip", "ops_api.cpp", "pages.cpp",
            "k_norm.hip", "k_w4.hip", "k_attn.hip", "k_kv.hip"]
@@ -37,7 +42,20 @@ def _flags(src: str):
     common = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{os.path.join(ROOT, 'include')}"]
     if src.endswith(".hip"):
         return ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"] + common
+    if src in DIRECT_SOURCES:
+        inc = [sysconfig.get_paths()["include"], os.path.join(_torch(), "include"), os.path.join(_rocm(), "include")]
+        return common + ["-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1"] + \
+            [a for i in inc for a in ("-isystem", i)]
     return common
+
+
+def _rocm() -> str:
+    return os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+
+
+def _torch() -> str:
+    """The installed PyTorch's folder (found, not imported: it would load its HIP runtime)."""
+    return os.path.dirname(importlib.util.find_spec("torch").origin)
 
 
 def _compile(src: str) -> str:
@@ -49,9 +67,9 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _link(objs, lib):
+def _link(objs, lib, more=()):
     tmp = lib + ".tmp"
-    cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
+    cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs + list(more)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"linking failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
@@ -60,14 +78,17 @@ def _link(objs, lib):
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    srcs = SOURCES + CEIL_SOURCES
+    srcs = SOURCES + CEIL_SOURCES + DIRECT_SOURCES
     jobs = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(jobs) as ex:
         objs = dict(zip(srcs, ex.map(_compile, srcs)))
     _link([objs[s] for s in SOURCES], LIB)
     _link([objs[s] for s in CEIL_SOURCES], CEIL_LIB)
+    # PyTorch's libraries are found by name: the package imports torch first.
+    _link([objs[s] for s in DIRECT_SOURCES], DIRECT_LIB,
+          ["-L" + os.path.join(_torch(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])
     if verbose:
-        print(f"built {LIB} and {CEIL_LIB}")
+        print(f"built {LIB}, {CEIL_LIB} and {DIRECT_LIB}")
     return LIB
 
 
