@@ -501,13 +501,14 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   chunk = (chunk + unit - 1) / unit * unit;
   chunk = chunk < unit ? unit : chunk > kChunkMax ? kChunkMax : chunk;
   AttnPlan p;
+  // Short sequences stay whole, with twice the waves, which saves the second launch; where they leave most of the
+  // card idle, a quarter less is short. Calls in sequence, whole and split, 8 key-value heads of 128 (queries 4
+  // times as many): one sequence of 300, 6.8 and 8.5 us; of 400, 7.7 and 7.9; of 500, 8.3 and 7.9; 64 of up to 500,
+  // 16.6 and 18.9. Heads of 64: one of 700, 7.3 and 7.8 us; of 1000, 8.8 and 7.8; 64 of up to 1000, 16.3 and 19.8.
+  // Heads of 256, 2 of 250: 9.2 and 9.9.
+  const int whole = head_dim <= 64 ? 1024 : head_dim <= 128 ? 512 : 256;
   p.waves = kWavesSplit;
-  // Short sequences stay whole, with twice the waves, which saves the second launch. Per call from the host
-  // whole and split, 8 key-value heads of 128 (queries 4 times as many): one sequence of 300, 6.9 and 10.8 us;
-  // of 500, 8.5 and 10.8 (in a graph 8.4 and 7.3); 700 costs 10.8 either way. Heads of 64 and 1000 positions:
-  // 8.9 and 10.7 us for one sequence (in a graph 8.8 and 7.1), 16.4 and 19.8 for 64. Heads of 256 with 250
-  // positions: 9.3 and 10.9.
-  if (span <= (head_dim <= 64 ? 1024 : head_dim <= 128 ? 512 : 256) && span > chunk) {
+  if (span <= (head_dim <= 128 && groups < n_cu / 2 ? whole - whole / 4 : whole) && span > chunk) {
     p.waves = kWavesWhole;
     chunk = (span + kTile - 1) / kTile * kTile;
   }
