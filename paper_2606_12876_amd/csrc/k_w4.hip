@@ -121,14 +121,16 @@ __device__ __forceinline__ uint2 widen_f8(uint32_t w) {
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true)));
 }
 
-// How each type of x meets the nibbles. X: 8 neighbouring inputs of one row.
+// How each type of x meets the nibbles. X: 8 neighbouring inputs of one row. kSixteens comes in a register
+// (o): "and" and "or" are one instruction then, which takes at most one constant.
 template <int XT> struct Op;
 struct F16Form {
   typedef f16x8_t V;
   typedef f32x4_t C;
   static constexpr int kZero = 16;
-  static __device__ __forceinline__ V weights(uint32_t w) {
-    const uint32_t m = 0x03C003C0u, o = 0x4C004C00u;
+  static constexpr uint32_t kSixteens = 0x4C004C00u;
+  static __device__ __forceinline__ V weights(uint32_t w, uint32_t o) {
+    const uint32_t m = 0x03C003C0u;
     return __builtin_bit_cast(V, u32x4_t{((w << 6) & m) | o, ((w << 2) & m) | o, ((w >> 2) & m) | o, ((w >> 6) & m) | o});
   }
   static __device__ __forceinline__ V ones() {
@@ -152,8 +154,9 @@ template <> struct Op<AQMB_BF16> {
   typedef bf16x8_t V;
   typedef f32x4_t C;
   static constexpr int kZero = 16;
-  static __device__ __forceinline__ V weights(uint32_t w) {
-    const uint32_t m = 0x00780078u, o = 0x41804180u;
+  static constexpr uint32_t kSixteens = 0x41804180u;
+  static __device__ __forceinline__ V weights(uint32_t w, uint32_t o) {
+    const uint32_t m = 0x00780078u;
     return __builtin_bit_cast(V, u32x4_t{((w << 3) & m) | o, ((w >> 1) & m) | o, ((w >> 5) & m) | o, ((w >> 9) & m) | o});
   }
   static __device__ __forceinline__ V ones() {
@@ -167,7 +170,8 @@ template <> struct Op<AQMB_I8> {
   typedef long V;
   typedef i32x4_t C;
   static constexpr int kZero = 0;
-  static __device__ __forceinline__ V weights(uint32_t w) {
+  static constexpr uint32_t kSixteens = 0;
+  static __device__ __forceinline__ V weights(uint32_t w, uint32_t) {
     const uint32_t m = 0x0F0F0F0Fu;
     return (long)((uint64_t)((w >> 4) & m) << 32 | (w & m));
   }
@@ -278,6 +282,8 @@ __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < 4; ++i) tot[r][i] = 0.f;
+  uint32_t sixteens = O::kSixteens;
+  if constexpr (O::kSixteens != 0) asm("" : "+v"(sixteens));
   Tile cur[R];
   if (wave < a.n_kt) {
 #pragma unroll
@@ -317,15 +323,13 @@ __global__ __launch_bounds__(64 * W) void w4_kernel(W4Args a) {
       for (int r = 0; r < R; ++r) {
         C acc = off;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) acc = O::mul(O::weights(cur[r].w[g * kSteps + s]), v[s], acc);
+        for (int s = 0; s < kSteps; ++s) acc = O::mul(O::weights(cur[r].w[g * kSteps + s], sixteens), v[s], acc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int e = 4 * g + i;                       // of the lane's piece
           const float s = e % 2 ? f16hi(cur[r].p.scale(e)) : f16lo(cur[r].p.scale(e));
-          const uint32_t z = (cur[r].p.zero(e) >> (8 * i)) & 0xFFu;
-          float p;
-          if constexpr (XT == AQMB_I8) p = (float)(acc[i] - (int)z * ax[i]);
-          else p = acc[i] - (float)z * ax[i];
+          const float z = (float)((cur[r].p.zero(e) >> (8 * i)) & 0xFFu);
+          float p = (float)acc[i] - z * (float)ax[i];     // int8: all of it exact, below 2^18
           if constexpr (!kWide) p *= sx[g];
           tot[r][i] += s * p;
         }
