@@ -104,6 +104,24 @@ def test_random(d_out, d_in, group, xt):
 
 
 @pytest.mark.parametrize("xt", XT)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("d_out,d_in", [(4097, 2200), (4200, 300), (8209, 2100), (8209, 200), (12305, 1111), (16401, 2313)])
+def test_tall_layers(d_out, d_in, group, xt):
+    """Workgroups of one to four row tiles and of 8 to 16 waves, the last of them partly outside: every output
+    is written, some rows are held against the formula."""
+    g = gen(d_out + d_in + group)
+    rows = torch.tensor(sorted(set(range(40)) | set(range(0, d_out, 101)) | set(range(d_out - 70, d_out))), device="cuda")
+    for batch, zeros, out in ((1, True, torch.float32), (3, False, torch.bfloat16), (16, True, torch.float32)):
+        w, s, z = layer(g, d_out, d_in, group, zeros)
+        x, xs = inputs(g, batch, d_in, xt, group)
+        y, bound = reference(x, xs, w[rows], s[rows], z[rows] if zeros else None, d_in, group)
+        got = run(x, xs, w, s, z, d_in, group, out)
+        assert np.isfinite(got).all()
+        got = got[:, rows.cpu().numpy()]
+        assert np.all(np.abs(got - y) <= bound + half_ulp(y, out)), (batch, np.max(np.abs(got - y) / bound))
+
+
+@pytest.mark.parametrize("xt", XT)
 @pytest.mark.parametrize("d_out,d_in,group", [(1, 1, 32), (19, 77, 32), (48, 512, 64), (100, 1111, 128), (33, 2048, 128),
                                               (520, 3001, 64)])
 def test_integers_come_out_exactly(d_out, d_in, group, xt):
