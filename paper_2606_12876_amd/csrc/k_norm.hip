@@ -157,7 +157,9 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     for (int j = 0; j < 8; ++j) ss += h[i][j] * h[i][j];
   }
   ss = row_sum<NT>(ss, lds_sum);
-  const float inv = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+  // Reciprocals and root by the instructions, an ulp each (rsqrtf takes care of subnormals): a launch of few rows
+  // is bound by its waves' instructions, and the exact forms are 60 of them.
+  const float inv = rsqrtf(ss * __builtin_amdgcn_rcpf((float)a.cols) + a.eps);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float f[8];
@@ -237,8 +239,8 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     if (n <= 0) continue;
     const bool finite = m[i] < 0x7F800000u;
     const float big = fmaxf(__builtin_bit_cast(float, m[i]), kScaleFloor);
-    const float mul = top / big;
-    const float scale = finite ? big / top : __builtin_nanf("");
+    const float mul = (top * 0x1p-20f) * __builtin_amdgcn_rcpf(big * 0x1p-20f);    // no step of it is subnormal
+    const float scale = finite ? big * (1.f / top) : __builtin_nanf("");
     if ((c & ((1u << shift) - 1)) == 0) a.scales[row * n_groups + (c >> shift)] = scale;
     B8 b;
     if (a.y_dtype == AQMB_F8) {
@@ -250,9 +252,12 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     } else {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        b.w[k] = 0;
+        // 1.5 2^23 + v rounds v to an integer, whose two's complement is the sum's low bits.
+        uint32_t u[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b.w[k] |= ((uint32_t)__float2int_rn(h[i][4 * k + j] * mul) & 0xFFu) << (8 * j);
+        for (int j = 0; j < 4; ++j) u[j] = __builtin_bit_cast(uint32_t, __builtin_fmaf(h[i][4 * k + j], mul, 12582912.f));
+        b.w[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0C0C0400u),
+                                       __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400u), 0x05040100u);
       }
     }
     if (!finite) b.w[0] = b.w[1] = 0;

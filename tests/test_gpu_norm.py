@@ -113,6 +113,18 @@ def test_values_that_are_not_finite():
         assert np.isnan(sv[2, 0]) and np.all(np.isfinite(sv[2, 1:3])) and np.all(qv[2] == 0)
 
 
+@pytest.mark.parametrize("out", [torch.float8_e4m3fn, torch.int8])
+@pytest.mark.parametrize("size", [3e38, 1e38, 1e-20, 1e-29])
+def test_large_and_small_groups(size, out):
+    """Groups whose largest magnitude has a subnormal reciprocal, or is close to the scales' floor."""
+    g = gen(8)
+    x = torch.where(torch.rand((2, 256), generator=g, device="cuda") < 0.5, -1.0, 1.0).bfloat16()
+    w = (size * torch.rand((256,), generator=g, device="cuda")).bfloat16()
+    y, s = torch.empty((2, 256), dtype=out, device="cuda"), torch.empty((2, 4), device="cuda")
+    A.rms_norm(x, w, y, eps=0.0, scales=s, scale_group=64)
+    check(x, None, w, 0.0, 0.0, y, None, s, 64)
+
+
 @pytest.mark.parametrize("dtype", H16)
 def test_strides_alignment_and_in_place(dtype):
     g = gen(5)
