@@ -375,11 +375,11 @@ static hipError_t by_batch(const W4Args& a, hipStream_t st) {
 // tiles, 256 units), groups of 64 with zero points, 11 rows: 1 tile 11.6 us, 2 tiles 9.9, 3 tiles 8.9, 4 tiles
 // 10.7; 14336 x 4096 e4m3, 16 rows: 1 tile 14.0, 2 tiles 10.0, 4 tiles 9.7.
 //
-// Waves: 8, and more where registers allow and turns are long. One tile, 4096 x 11008 int8 at 16 rows: 7.3 us with
+// Waves: 8, and 16 where registers allow and turns are long. One tile, 4096 x 11008 int8 at 16 rows: 7.3 us with
 // 16, 7.9 with 8. Two tiles, 6000 x 9000, groups of 64, one row of bf16 8.9 and 9.6, 16 rows of e4m3 9.7 and 10.6, but of
-// int8 6.6 and 6.3 at 4200 x 4096; groups of 32 spill. Three, groups of 64: 11008 x 4096, one row of bf16 7.4 with
-// 12 and 7.9, 16 rows 8.1 and 8.4, int8 8.1 and 7.8; groups of 128 6.8 and 6.7. Where there are too few input tiles
-// for them, more waves only cost their start.
+// int8 6.6 and 6.3 at 4200 x 4096; groups of 32 spill. Three with 12, groups of 64, 14 rows of bf16: 13.3 and 14.0 at
+// 11008 x 8000, but 10.4 and 9.4 at 11008 x 4099: left at 8. Where there are too few input tiles for them, more waves only
+// cost their start.
 template <int XT, int G>
 static hipError_t go(const W4Args& a, int n_cu, hipStream_t st) {
   const int n_rt = (a.d_out - 1) / kW4Rows + 1, rounds = (n_rt - 1) / (4 * n_cu) + 1;
@@ -390,7 +390,7 @@ static hipError_t go(const W4Args& a, int n_cu, hipStream_t st) {
         if (a.n_kt > 16) return by_batch<XT, G, 2, 16>(a, st);
       }
       return by_batch<XT, G, 2, 8>(a, st);
-    case 3: return by_batch<XT, G, 3, (XT != AQMB_I8 && G == 64 ? 12 : 8)>(a, st);
+    case 3: return by_batch<XT, G, 3, 8>(a, st);
     default: return by_batch<XT, G, 4, 8>(a, st);
   }
 }
