@@ -21,7 +21,8 @@ struct __attribute__((packed, aligned(2))) Raw2 { uint32_t w; };
 
 // Columns c .. c + 7 of a row. What reaches over the row's end is its last 8 columns, for shift8 to put right:
 // one load for every lane and no branch around it (element by element, with a wait for each, 4000 rows of 4095
-// took 42 us, not 30). kShort: rows may have fewer than 8 columns, 0 past the end.
+// took 42 us, not 30). Those of its columns that belong to another thread, which may be storing to them in
+// place, are among what is shifted out. kShort: rows may have fewer than 8 columns, 0 past the end.
 template <bool kShort>
 __device__ __forceinline__ Raw8 load8(const uint16_t* row, int c, int cols) {
   if (kShort && cols < 8) {
