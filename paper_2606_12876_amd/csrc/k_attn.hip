@@ -379,6 +379,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     s_join[1][r] = L;
   }
   __syncthreads();
+  // A sum is 0 only where no position takes part, NaN where a score is: then out and lse are NaN too.
   const bool one = a.n_splits == 1;
   const int quads = a.head_dim / 4;
   for (int e = threadIdx.x; e < nh * quads; e += 64 * kWaves) {
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       ml[(at * a.n_splits + split) * 2] = mm;
       ml[(at * a.n_splits + split) * 2 + 1] = sum;
     } else if (a.lse) {
-      a.lse[at] = sum > 0.f ? (mm - Mma<PT>::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -__builtin_inff();
+      a.lse[at] = sum == 0.f ? -__builtin_inff() : (mm - Mma<PT>::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
   }
 }
@@ -427,7 +428,7 @@ __device__ __forceinline__ void store_joined(const AttnArgs& a, int64_t at, int 
   uint16_t* out = (uint16_t*)a.out + seq * a.out_stride + (at - (int64_t)seq * a.n_heads) * a.head_dim + d;
   *(uint2*)out = make_uint2(Mma<T>::pack(v[0], v[1]), Mma<T>::pack(v[2], v[3]));
   if (a.lse && d == 0)
-    a.lse[at] = sum > 0.f ? (top - shift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -__builtin_inff();
+    a.lse[at] = sum == 0.f ? -__builtin_inff() : (top - shift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // chunk i's statistics and sum added to a running (M, L, v)

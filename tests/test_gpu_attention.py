@@ -264,6 +264,29 @@ def test_scores_that_are_not_finite():
     assert torch.isnan(out[0]).all() and torch.equal(out[1], want[1])
 
 
+@pytest.mark.parametrize("cache_dtype", [None, F8])
+@pytest.mark.parametrize("length", [40, 900, 40000])      # one workgroup, a few chunks, many
+def test_a_score_that_is_nan_shows_in_the_denominator(length, cache_dtype):
+    g = gen(85)
+    c, table, lens = build(g, [length, length], 1, 128, 16, torch.float16, cache_dtype)
+    q = normal(g, 2, 3, 128, dtype=torch.float16)
+    out, lse = torch.empty_like(q), torch.empty((2, 3), device="cuda")
+    c.attention(q, table, lens, out, scale=128 ** -0.5, lse=lse)
+    assert torch.isfinite(lse).all()
+    want, stats = out.clone(), lse.clone()
+    q[0, 1, 7] = float("nan")                             # one head of sequence 0
+    c.attention(q, table, lens, out, scale=128 ** -0.5, lse=lse)
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(lse[0, 1])
+    q[0, 1, 7] = 0.0
+    if cache_dtype is None:                               # and one key, for every head
+        c.k[table[0, 2], 0, 0, 0] = float("nan")
+    else:
+        c.k_scale[table[0, 2], 0, 0] = float("nan")
+    c.attention(q, table, lens, out, scale=128 ** -0.5, lse=lse)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    assert torch.equal(out[1], want[1]) and torch.equal(lse[1], stats[1])
+
+
 def test_strides():
     g = gen(83)
     lens_ = [70, 33, 5]
