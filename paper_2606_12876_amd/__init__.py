@@ -865,6 +865,8 @@ class KVCache:
         wp, wb = None, 0
         if workspace is not None:
             _here(where, workspace=workspace)
+            if not workspace.is_contiguous():
+                _refuse(where, "workspace must be dense")
             wp, wb = workspace.data_ptr(), _nbytes(workspace)
         elif need:
             if stream is None:

@@ -206,6 +206,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     void* ws = nullptr;
     if (a[10] != Py_None) {
       const Tensor& t = tensor(a[10], dev, true);
+      need(t.is_contiguous());        // its bytes are its own
       ws = t.data_ptr();
       bytes = (size_t)t.numel() * t.element_size();
     } else if (bytes) {               // from the allocator, which ties it to the current stream

@@ -345,6 +345,23 @@ def test_workspace_is_checked_and_used():
     assert torch.equal(out, want) and torch.isnan(ws[need // 4:]).all()
 
 
+@pytest.mark.parametrize("stream", [False, True])
+def test_a_workspace_that_is_not_dense_is_refused(stream):
+    """An expanded or strided tensor has fewer bytes of its own than its number of elements says."""
+    g = gen(87)
+    c, table, lens = build(g, [1300], 2, 64, 16, torch.float16)
+    q = normal(g, 1, 2, 64, dtype=torch.float16)
+    need = c.workspace_bytes(2, 1, table.shape[1] * 16)
+    out = torch.full_like(q, 5.0)
+    base = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+    kw = dict(stream=torch.cuda.current_stream()) if stream else {}
+    for ws in (base[:1].expand(need), torch.stack((base, base), 1)[:, 0]):
+        with pytest.raises(A.AqmbError, match="dense"):
+            c.attention(q, table, lens, out, scale=0.125, workspace=ws, **kw)
+    torch.cuda.synchronize()
+    assert (out == 5).all() and (base == 7).all()
+
+
 def test_binding_refuses():
     g = gen(86)
     c, table, lens = build(g, [20, 20], 2, 64, 16, torch.bfloat16)
