@@ -116,6 +116,16 @@ def test_attention_refuses(kw, status):
     assert A.last_error()
 
 
+def test_calls_past_one_launch_are_refused():
+    c = cache(n_kv_heads=8, page_stride=1 << 20)
+    assert A.lib.aqmb_kv_append(ctypes.byref(c), 64, 1 << 12, 64, 1 << 12, BF16, 64, 1 << 23, None) == S.EUNSUPPORTED
+    assert "2^26" in A.last_error()
+    for rows, cols in ((1 << 22, 4096), (1 << 27, 128), (1 << 28, 64), (2 ** 31 - 1, 1), (1 << 19, 32768)):
+        assert A.lib.aqmb_rms_norm(64, BF16, cols, None, None, 0, 64, 0.0, 1e-5, rows, cols, 64, BF16, cols, None, 0,
+                                   None) == S.EUNSUPPORTED
+        assert "one launch" in A.last_error()
+
+
 def test_append_and_copy_refuse():
     c = cache()
     f = A.lib.aqmb_kv_append
