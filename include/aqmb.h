@@ -483,7 +483,8 @@ typedef struct {
  * page_table[s][t / page_size]. A sequence with no position gives out = 0 and lse = -infinity.
  * lse (may be NULL): the logarithm of the softmax's denominator, log sum_t exp(score_t), fp32
  * [n_seqs][n_heads], with which results over disjoint parts of a context can be joined. A score that is NaN
- * or +infinity makes out and lse of its head NaN.
+ * or +infinity makes out and lse of its head NaN; one of -infinity weighs nothing (a head that has no other is as
+ * one without a position).
  *   q, out      [n_seqs][n_heads][head_dim] F16 or BF16 (`dtype`; the cache's own type, or any of
  *               the two with an F8 cache), stride between sequences q_stride / out_stride, each a
  *               multiple of 8; 16-byte aligned

@@ -16,9 +16,11 @@
 // between the quarters per tile.
 //
 // Probabilities enter the second product as two 16-bit parts (value and remainder): rounding them once
-// to bf16 would cost as much as rounding the result does when few positions carry the weight. With an
-// fp16 cache they are formed 2^14 larger, so that small ones keep their digits above fp16's smallest
-// subnormal. An F8 cache is widened to bf16 for V (its scale joins the probability) and to the type of q
+// to bf16 would cost as much as rounding the result does when few positions carry the weight. bf16 parts hold
+// 16 bits of a probability, fp16 parts 22. With an fp16 cache they are formed 2^14 larger, and relative to a
+// tile's own largest where that is far below the maximum, so that small ones keep their digits above fp16's
+// smallest subnormal: one is off by at most 2^-21 of itself or 2^-39 of the maximum, in a tile far below by 2^-38 of
+// that tile's largest. An F8 cache is widened to bf16 for V (its scale joins the probability) and to the type of q
 // for K (its scale joins the score): both exact.
 //
 // Chunks of a sequence are joined by a second kernel from (max, sum, unnormalised out) in the workspace.
@@ -40,7 +42,9 @@ __device__ __forceinline__ float below(float x) {
 
 // split: two probabilities (>= 0) as two 16-bit parts each, cut off rather than rounded and from just
 // below, so that both parts of a positive one are positive: an infinite value of V then gives infinity,
-// not the NaN that inf * 0 or inf - inf would be.
+// not the NaN that inf * 0 or inf - inf would be. A zero stays zero. fp16: the first part is also 2^-24, fp16's
+// smallest number, below, which leaves that much for the second; the parts together are off by at most 2^-25 or
+// 2^-21 of the probability, and one below 2^-23 is its second part alone.
 template <int T> struct Mma;
 template <> struct Mma<AQMB_F16> {
   static __device__ __forceinline__ f32x4_t mul(u32x4_t a, u32x4_t b, f32x4_t c) {
@@ -48,8 +52,9 @@ template <> struct Mma<AQMB_F16> {
   }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16x2(lo, hi); }
   static __device__ __forceinline__ void split(float x, float y, uint32_t& a, uint32_t& b) {
-    a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(below(x), below(y)));
-    b = pack_f16x2(fmaxf(x - f16lo(a), 0x1p-24f), fmaxf(y - f16hi(a), 0x1p-24f));
+    const float u = fmaxf(__builtin_fmaf(x, 1.f - 0x1p-23f, -0x1p-24f), 0.f), v = fmaxf(__builtin_fmaf(y, 1.f - 0x1p-23f, -0x1p-24f), 0.f);
+    a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(u, v));
+    b = pack_f16x2(x - f16lo(a), y - f16hi(a));
   }
   static constexpr float kShift = 14.f;
 };
@@ -64,6 +69,11 @@ template <> struct Mma<AQMB_BF16> {
   }
   static constexpr float kShift = 0.f;
 };
+
+// A tile whose largest score is this much (in units of log 2) below the maximum so far: probabilities 2^-26 of
+// its largest are still whole numbers of 2^-24.
+constexpr float kFar = 12.f;
+__device__ __forceinline__ float power_of_2(int e) { return __builtin_bit_cast(float, (127 + e) << 23); }
 
 // Four e4m3 values (one dword) widened to 16 bits, exactly: one instruction for two, where the way through
 // binary32 takes three (and 7 registers more: 3 workgroups on a unit, not 4). One stream of 65536: 31.4 us
@@ -289,9 +299,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
     }
     top = quarters(top, max_floats);
     const float m2 = fmaxf(m, top);
-    const float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
-    if (t0 != first && __any(m2 > m)) {
-      const float f = __builtin_amdgcn_exp2f(m2 == -__builtin_inff() ? 0.f : m - m2);
+    float mu = m2 == -__builtin_inff() ? 0.f : m2 - Mma<PT>::kShift;
+    // fp16 parts of a tile far below the maximum would have few digits left or none: they are formed 2^up larger,
+    // and the sums (at most 2^42) with them for the length of this tile.
+    int up = 0;
+    if constexpr (PT == AQMB_F16) {
+      up = m2 - top > kFar ? (int)fminf(m2 - top, 60.f) : 0;
+      mu -= (float)up;
+    }
+    if (t0 != first && __any(m2 > m || up > 0)) {
+      float f = __builtin_amdgcn_exp2f(m2 == -__builtin_inff() ? 0.f : m - m2);
+      if constexpr (PT == AQMB_F16) f = up > 0 ? power_of_2(up) : f;
       l *= f;
 #pragma unroll
       for (int e = 0; e < DC; ++e) o[e] *= f;
@@ -340,6 +358,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
         }
         o[4 * i + e] = Mma<PT>::mul(w, pho, o[4 * i + e]);
         o[4 * i + e] = Mma<PT>::mul(w, plo, o[4 * i + e]);
+      }
+    }
+    if constexpr (PT == AQMB_F16) {
+      if (__any(up > 0)) {
+        const float f = power_of_2(-up);
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < DC; ++e) o[e] *= f;
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

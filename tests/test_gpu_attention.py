@@ -386,3 +386,52 @@ def test_binding_refuses():
                   ((k[:1].expand(4, 2, 16, 64), k[:1].expand(4, 2, 16, 64)), {}), ((k.cpu(), k.cpu()), {})):
         with pytest.raises(A.AqmbError):
             A.KVCache(*a, **kw)
+
+
+@pytest.mark.parametrize("below", [8, 18, 24, 26, 27, 28, 34, 40, 60, 200])
+@pytest.mark.parametrize("length,page,per", [(300, 16, None), (1300, 16, None), (40000, 16, None), (9000, 4096, 512)])
+@pytest.mark.parametrize("dtype,cache", [(torch.float16, None), (torch.bfloat16, None), (torch.float16, F8)])
+def test_small_weights_before_large_values(dtype, cache, length, page, per, below):
+    """One position far above the others (by `below` units of the natural logarithm), whose value is a ten-millionth
+    of theirs: what each of the others weighs must neither be lost nor grow. A sequence whole, in few chunks, in many,
+    and in the largest chunks, where a wave takes 32 tiles one after the other."""
+    g = gen(91)
+    c, table, lens = build(g, [length], 1, 64, page, dtype, cache, per=per)
+    held = [(int(table[0, t // page]), t % page) for t in (0, length // 2, length - 1)]
+    q = torch.ones((1, 3, 64), dtype=dtype, device="cuda")
+    for p, slot in held:
+        c.k.view(torch.uint8).zero_()
+        c.v.copy_(torch.where(torch.rand(c.v.shape, generator=g, device="cuda") < 0.7, 256.0, -128.0).to(c.v.dtype))
+        c.k[p, 0, slot] = 1.0
+        if cache is None:
+            c.v.mul_(48.0)
+            c.v[p, 0, slot] = 0.001
+        else:
+            c.k_scale.fill_(1.0), c.v_scale.fill_(48.0)
+            c.v[p, 0, slot] = 1.0
+            c.v_scale[p, 0, slot] = 0.001
+        attend(c, q, table, lens, scale=below / 64.0)
+
+
+@pytest.mark.parametrize("length", [40, 300, 1300, 40000])
+def test_weights_of_zero_and_infinite_values(length):
+    """fp16: a value of infinity gives infinity, scores of -infinity give weights of zero, and nothing else counts."""
+    g = gen(92)
+    c, table, lens = build(g, [length], 1, 64, 16, torch.float16)
+    q = normal(g, 1, 3, 64, dtype=torch.float16)
+    want = attend(c, q, table, lens)
+    c.v[table[0, 1], 0, 3, 5] = float("inf")
+    out, lse = torch.empty_like(q), torch.empty((1, 3), device="cuda")
+    c.attention(q, table, lens, out, scale=64 ** -0.5)
+    keep = [d for d in range(64) if d != 5]
+    assert (out[0, :, 5] == float("inf")).all() and torch.equal(out[0][:, keep], want[0][:, keep])
+    q.abs_().add_(1.0)
+    c.k.fill_(0.0)
+    c.k[..., 0] = float("-inf")
+    c.v.fill_(60000.0)
+    c.attention(q, table, lens, out, scale=64 ** -0.5, lse=lse)
+    assert (out == 0).all() and (lse == float("-inf")).all()
+    c.k[table[0, 2], 0, 0, 0] = 1.0
+    c.v[table[0, 2], 0, 0] = 2.0 ** -14
+    c.attention(q, table, lens, out, scale=64 ** -0.5, lse=lse)
+    assert (out == 2.0 ** -14).all() and torch.isfinite(lse).all()
