@@ -35,13 +35,20 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kTile = 32, kChunkMax = 4096, kXcds = 8;
 constexpr int kWavesSplit = 4, kWavesWhole = 8;   // per workgroup, where sequences are split and where not
 
-// The binary32 number next below a positive one; 0 for 0.
+// The binary32 number next to another one on the side of 0; 0 for 0 (but not for -0).
 __device__ __forceinline__ float below(float x) {
   return __builtin_bit_cast(float, __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, x), 1u));
 }
 
-// split: two probabilities (>= 0) as two 16-bit parts each, cut off rather than rounded and from just
-// below, so that both parts of a positive one are positive: an infinite value of V then gives infinity,
+// A probability (>= 0) by its value's scale. A product of -0 (a weight of 0, or a product too small, by a negative
+// scale) becomes 0, which is what below knows; the addition must not be drawn into the product.
+__device__ __forceinline__ float by_scale(float p, float scale) {
+#pragma clang fp contract(off)
+  return p * scale + 0.f;
+}
+
+// split: two probabilities (of an 8-bit cache: times their scales) as two 16-bit parts each, cut off rather than
+// rounded and from just below, so that both parts of a positive one are positive: an infinite value of V then gives infinity,
 // not the NaN that inf * 0 or inf - inf would be. A zero stays zero. fp16: the first part is also 2^-24, fp16's
 // smallest number, below, which leaves that much for the second; the parts together are off by at most 2^-25 or
 // 2^-21 of the probability, and one below 2^-23 is its second part alone.
@@ -322,8 +329,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
       float x = __builtin_amdgcn_exp2f(p[j] - mu), y = __builtin_amdgcn_exp2f(p[j + 1] - mu);
       l += x + y;
       if constexpr (F8) {
-        x = vmask >> j & 1 ? x * sc[j] : 0.f;
-        y = vmask >> (j + 1) & 1 ? y * sc[j + 1] : 0.f;
+        x = vmask >> j & 1 ? by_scale(x, sc[j]) : 0.f;
+        y = vmask >> (j + 1) & 1 ? by_scale(y, sc[j + 1]) : 0.f;
       }
       Mma<PT>::split(x, y, ph[j / 2], pl[j / 2]);
     }

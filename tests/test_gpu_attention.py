@@ -435,3 +435,15 @@ def test_weights_of_zero_and_infinite_values(length):
     c.v[table[0, 2], 0, 0] = 2.0 ** -14
     c.attention(q, table, lens, out, scale=64 ** -0.5, lse=lse)
     assert (out == 2.0 ** -14).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("scale", [0.125, 3.0, 1e3])          # weights that are all there, that fade, that are 0
+@pytest.mark.parametrize("length", [40, 700, 20000])
+def test_negative_scales(length, scale, dtype):
+    """An 8-bit cache whose scales have either sign, or are 0: they multiply, whatever the weight."""
+    g = gen(93)
+    c, table, lens = build(g, [length, 3], 2, 64, 16, dtype, F8)
+    for s in (c.k_scale, c.v_scale):
+        s.mul_(torch.randint(-1, 2, s.shape, generator=g, device="cuda"))
+    attend(c, normal(g, 2, 4, 64, dtype=dtype, std=2.0), table, lens, scale=scale)
