@@ -67,28 +67,38 @@ class DecodeBlock:
 class Streams:
     """The streams of a server: page tables and lengths of one step, from a PagePool."""
 
-    def __init__(self, pool: A.PagePool, caches):
-        self.pool, self.caches = pool, caches
+    def __init__(self, pool: A.PagePool, caches, device="cuda"):
+        self.pool, self.caches, self.device = pool, caches, device
+        self.ready = {}                     # slots of streams extended in a step that then ran out of pages
 
     def copy(self, pairs):
         if pairs:
-            src, dst = (torch.tensor(p, dtype=torch.int32).cuda() for p in zip(*pairs))
+            src, dst = (torch.tensor(p, dtype=torch.int32).to(self.device) for p in zip(*pairs))
             A.kv_copy_pages(self.caches, src, dst)
 
+    def free(self, seq):
+        self.ready.pop(seq, None)
+        self.pool.free(seq)
+
     def advance(self, seqs):
-        """One more token for every stream: (positions, slots, table, lengths, max_length) on the GPU."""
-        slots, pairs = [], []
-        for s in seqs:
-            slot, copies = self.pool.extend(s, 1)
-            slots.append(slot)
-            pairs += copies
-        self.copy(pairs)
+        """One more token for every stream: (positions, slots, table, lengths, max_length) on the GPU. Where the
+        pool runs out of pages (ENOMEM), free a stream and call again."""
+        pairs = []
+        try:
+            for s in seqs:
+                if s not in self.ready:
+                    self.ready[s], copies = self.pool.extend(s, 1)
+                    pairs += copies
+        finally:                            # what was given out stands, and a free may follow
+            self.copy(pairs)
+        slots = [self.ready.pop(s) for s in seqs]
         lengths = torch.tensor([self.pool.length(s) for s in seqs], dtype=torch.int32)
         tables = [self.pool.table(s) for s in seqs]
         table = torch.full((len(seqs), max(len(t) for t in tables)), -1, dtype=torch.int32)
         for i, t in enumerate(tables):
             table[i, :len(t)] = t
-        return (lengths.long().cuda() - 1, torch.cat(slots).cuda(), table.cuda(), lengths.cuda(), int(lengths.max()))
+        return (lengths.long().to(self.device) - 1, torch.cat(slots).to(self.device), table.to(self.device),
+                lengths.to(self.device), int(lengths.max()))
 
 
 def random_block(hidden=512, heads=8, kv_heads=2, dim=64, ffn=1376, pages=64, page=16, cache_dtype=torch.bfloat16, seed=0):
@@ -128,7 +138,7 @@ def main():
         if step == 20:
             live.append(pool.fork(live[0]))          # shares its pages with stream 0 until either writes
         if step == 30:
-            pool.free(live.pop(1))
+            streams.free(live.pop(1))
             streams.copy(pool.compact())
         h = torch.randn((len(live), block.hidden), device="cuda").bfloat16()
         h = block.step(h, 4 if step % 2 else 2, *streams.advance(live))

@@ -544,12 +544,17 @@ aqmb_status aqmb_kv_copy_pages(const aqmb_kv_cache* caches, int n_caches, const 
  * 0..max_seqs-1, given out lowest first.
  *   aqmb_pages_add      a new, empty sequence. ENOMEM when max_seqs are live.
  *   aqmb_pages_fork     a new sequence that shares all pages of `seq`, the last, partly filled one
- *                       included. ENOMEM as above.
+ *                       included. ENOMEM as above. The tokens of `seq` have to be written (or their writing
+ *                       enqueued) before: what the new one copies on its first write is the page as it is then.
  *   aqmb_pages_extend   n_tokens more tokens: slots[n_tokens] receives their cache slots (the
  *                       argument of aqmb_kv_append). Where the first of them falls into a page that
  *                       another sequence shares, the sequence gets a page of its own and
  *                       (*copy_src, *copy_dst) say which page to copy before writing, else both
  *                       are -1. ENOMEM, with nothing changed, when too few pages are free.
+ *                       The copy has to be enqueued before the next fork, free or compact on this pool (after
+ *                       an ENOMEM too: the pairs that came before it stand), since a freed page is given out
+ *                       again at once. The pairs of extends with nothing of the kind between them never
+ *                       conflict: one call may copy them all.
  *   aqmb_pages_free     ends a sequence; pages that no other one shares become free.
  *   aqmb_pages_compact  moves used pages from the end of the pool into free ones at its start, so
  *                       that the used pages are 0..used-1: the *n_pairs copies to make are written

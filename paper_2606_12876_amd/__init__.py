@@ -956,7 +956,8 @@ class PagePool:
     """aqmb_pages_*: which pages of a cache each sequence holds, on the host. Sequences are small integers.
 
     extend returns (slots int64 tensor, copies) where copies is [] or [(src, dst)]: the page to copy in
-    every layer's cache before the tokens are written; compact returns such a list for the whole pool.
+    every layer's cache before the tokens are written, and before the next fork, free or compact (the pairs of
+    extends in a row may be copied together); compact returns such a list for the whole pool.
     table returns the pages as an int32 tensor. All of them are CPU tensors and lists: one upload of a
     step's tables, slots and copies serves all layers."""
 
