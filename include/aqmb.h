@@ -436,8 +436,10 @@ aqmb_status aqmb_w4_get_desc(aqmb_w4_t layer, aqmb_w4_desc* out);
  * I8 (what aqmb_rms_norm writes; x_scale_group 0: one scale for each row). Within a group the
  * products q * x and the sum of x (for the zero point) are formed on the matrix cores: exact
  * products, sums in binary32 (I8: exact in int32); the groups are scaled and added in binary32, in
- * a fixed order; one rounding to y_dtype in {F16, BF16, F32}. An x that is not finite makes all of
- * its row's outputs not finite.
+ * a fixed order; one rounding to y_dtype in {F16, BF16, F32}. The weights enter as 16 + q (I8: as q); the 16 and the
+ * zero point come off a group's sums before its scale. These sums cannot overflow while every |X| <= 2^112; above
+ * (BF16 x, or 8-bit x with such scales) outputs may be NaN where the formula is finite. An X that is not finite
+ * makes all of its row's outputs not finite.
  *   x  [batch][d_in], row stride x_stride; y [batch][d_out], row stride y_stride
  * 1 <= batch <= AQMB_MAX_BATCH.
  * Errors: EINVAL (bad handle, null or misaligned pointer, batch < 1, a stride below the row,

@@ -243,3 +243,28 @@ def test_layer_class_and_refusals():
     for bad in ((w[:, :47], s, z), (w, s[:, :2], z), (w, s, z[:, :2]), (w, s.float(), z), (w.to(torch.int8), s, z)):
         with pytest.raises(A.AqmbError):
             A.W4Linear(*bad, d_in=96, group_size=32)
+
+
+@pytest.mark.parametrize("xt", [torch.bfloat16, F8, I8])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("zero", [None, 0, 255])
+def test_largest_inputs(zero, group, xt):
+    """|X| = 2^112 throughout, of one sign in some rows, with the largest and smallest weights and zero points: every
+    sum stays finite and as exact as ever."""
+    g = gen(13)
+    d_out, d_in = 40, 300
+    w, s, z = layer(g, d_out, d_in, group, zero is not None)
+    w[:16], w[16:32] = 0xFF, 0
+    if zero is not None:
+        z.fill_(zero)
+    sign = torch.where(torch.rand((3, d_in), generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    sign[1], sign[2] = 1.0, -1.0
+    xs = None
+    if xt == torch.bfloat16:
+        x = (sign * 2.0 ** 112).to(xt)
+    else:
+        top = {F8: 448.0, I8: 127.0}[xt]
+        x, xs = (sign * top).to(xt), torch.full((3, -(-d_in // group)), 2.0 ** 112 / top * (1 - 2.0 ** -23), device="cuda")
+    y, bound = reference(x, xs, w, s, z, d_in, group)
+    got = run(x, xs, w, s, z, d_in, group, torch.float32)
+    assert np.all(np.isfinite(got)) and np.all(np.abs(got - y) <= bound + half_ulp(y, torch.float32))
