@@ -415,9 +415,9 @@ aqmb_status aqmb_rms_norm(const void* x, aqmb_dtype dtype, int64_t x_stride, con
  * d_in need not be a multiple of the group size. The library copies everything into device memory
  * it owns, re-tiled for the matrix cores; aqmb_w4_create is synchronous (the caller may free its
  * buffers afterwards). A layer is read-only after creation.
- * Errors: EINVAL (null pointer, sizes < 1 or > 2^30, d_out * d_in >= 2^32), EUNSUPPORTED (group_size other
- * than 32, 64, 128), ENOMEM, EHIP; on error *out is NULL. aqmb_w4_destroy waits for the device;
- * NULL is a no-op, EINVAL for a handle that is not a live layer.
+ * Errors: EINVAL (null pointer, sizes < 1 or > 2^30, d_out * d_in >= 2^32, 2^24 tiles of 16 x 128 weights or
+ * more, the last ones counted whole), EUNSUPPORTED (group_size other than 32, 64, 128), ENOMEM, EHIP; on error
+ * *out is NULL. aqmb_w4_destroy waits for the device; NULL is a no-op, EINVAL for a handle that is not a live layer.
  */
 typedef struct aqmb_w4_s* aqmb_w4_t;
 typedef struct {

@@ -151,6 +151,11 @@ aqmb_status aqmb_w4_create(aqmb_w4_t* out, const aqmb_w4_desc* desc, const uint8
     return fail(AQMB_EINVAL, "w4_create: d_out and d_in must be at most 2^30, their product below 2^32");
   if (desc->group_size != 32 && desc->group_size != 64 && desc->group_size != 128)
     return fail(AQMB_EUNSUPPORTED, "w4_create: group_size = %d is not 32, 64 or 128", desc->group_size);
+  // Laid out by one launch, a thread for every dword of the tiles (256 of each): fewer than 2^32.
+  const int n_rt = (desc->d_out - 1) / kW4Rows + 1, n_kt = (desc->d_in - 1) / kW4Cols + 1;
+  if ((int64_t)n_rt * n_kt >= 1 << 24)
+    return fail(AQMB_EINVAL, "w4_create: %d x %d weights are 2^24 tiles of %d x %d or more", desc->d_out, desc->d_in,
+                kW4Rows, kW4Cols);
   if (!weights || !scales) return fail(AQMB_EINVAL, "w4_create: weights or scales is NULL");
   if (!aligned(scales, 2)) return fail(AQMB_EINVAL, "w4_create: scales must be 2-byte aligned");
 
@@ -161,8 +166,8 @@ aqmb_status aqmb_w4_create(aqmb_w4_t* out, const aqmb_w4_desc* desc, const uint8
   hipError_t e = hipGetDevice(&L->device);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&L->n_cu, hipDeviceAttributeMultiprocessorCount, L->device);
   if (e != hipSuccess) { free_w4(L); return hip_status(e, "w4_create: device"); }
-  L->n_rt = (desc->d_out - 1) / kW4Rows + 1;
-  L->n_kt = (desc->d_in - 1) / kW4Cols + 1;
+  L->n_rt = n_rt;
+  L->n_kt = n_kt;
   const size_t tiles = (size_t)L->n_rt * L->n_kt, n_scales = tiles * (kW4Cols / desc->group_size) * kW4Rows;
   L->asymmetric = zeros != nullptr;
   struct { void** p; size_t n; } allocs[] = {{(void**)&L->tiles, tiles * 1024}, {(void**)&L->scales, n_scales * 2},

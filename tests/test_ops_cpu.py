@@ -257,3 +257,17 @@ def test_page_pool_refuses():
     assert e.value.status == S.ENOMEM
     pool.close()
     assert A.lib.aqmb_pages_add(bogus, ctypes.byref(i)) == S.EINVAL
+
+
+@pytest.mark.parametrize("d_out,d_in", [(1 << 28, 1), (1 << 30, 3), ((1 << 28) - 15, 15), (1 << 21, 2000), (1, 1 << 30)])
+def test_w4_create_refuses_what_one_launch_cannot_lay_out(d_out, d_in):
+    """Tall, narrow layers are mostly padding: a thread for every dword of the tiles, fewer than 2^32."""
+    fits = -(-d_out // 16) * -(-d_in // 128) < 1 << 24
+    h, d = ctypes.c_void_p(0x1234), A.W4Desc(d_out, d_in, 128)
+    if fits:        # refused for something that is looked at later
+        assert A.lib.aqmb_w4_create(ctypes.byref(h), ctypes.byref(d), None, 16, None, None) == S.EINVAL
+        assert "NULL" in A.last_error()
+    else:
+        assert A.lib.aqmb_w4_create(ctypes.byref(h), ctypes.byref(d), 16, 16, None, None) == S.EINVAL
+        assert "tiles" in A.last_error()
+    assert h.value is None
