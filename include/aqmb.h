@@ -396,7 +396,8 @@ double aqmb_bits_per_weight(const aqmb_desc* desc, int k);
  * 1 <= cols <= AQMB_MAX_NORM_COLS; scale_group 0, 32, 64 or 128.
  * Errors: EINVAL (null or misaligned pointer, rows or cols < 1, a stride below cols, one residual
  * pointer without the other, scales missing or not wanted, negative or NaN eps), EUNSUPPORTED
- * (dtype, cols above the limit, scale_group, rows * max(16, cols / 4) of 2^32 or more), EHIP.
+ * (dtype, cols above the limit, scale_group, rows * max(8, ceil(cols / 8)) of 2^31 or more, with rows rounded up to
+ * a multiple of 16 where cols <= 64), EHIP.
  */
 #define AQMB_MAX_NORM_COLS 32768
 aqmb_status aqmb_rms_norm(const void* x, aqmb_dtype dtype, int64_t x_stride, const void* residual,
@@ -521,7 +522,7 @@ aqmb_status aqmb_paged_attention_workspace_bytes(const aqmb_kv_cache* cache, int
  *          the two for an F8 cache), stride between tokens k_stride / v_stride
  *   slots  int64 [n_tokens], device memory
  * Errors: EINVAL (null or misaligned pointer, n_tokens < 1, stride below a token), EUNSUPPORTED (dtype,
- * n_tokens * n_kv_heads of 2^26 or more), EHIP.
+ * n_tokens * n_kv_heads above 2^26 - 4), EHIP.
  */
 aqmb_status aqmb_kv_append(const aqmb_kv_cache* cache, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, aqmb_dtype dtype, const int64_t* slots, int n_tokens,

@@ -122,8 +122,10 @@ aqmb_status aqmb_rms_norm(const void* x, aqmb_dtype dtype, int64_t x_stride, con
   if (!residual != !residual_out) return fail(AQMB_EINVAL, "rms_norm: residual and residual_out go together");
   if (rows < 1 || cols < 1) return fail(AQMB_EINVAL, "rms_norm: rows = %d and cols = %d must be >= 1", rows, cols);
   if (cols > AQMB_MAX_NORM_COLS) return fail(AQMB_EUNSUPPORTED, "rms_norm: cols = %d above %d", cols, AQMB_MAX_NORM_COLS);
-  // A launch has fewer than 2^32 threads; a row takes at most two for every 8 columns, and 16 if it is short.
-  if ((int64_t)rows * (cols <= 64 ? 16 : (cols + 7) / 8 * 2) >= (int64_t)1 << 32)
+  // A launch has fewer than 2^32 threads; a row takes at most two for every 8 columns, and 16 if it is short (then
+  // 16 rows share a workgroup).
+  const int64_t threads = cols <= 64 ? ((int64_t)rows + 15) / 16 * 256 : (int64_t)rows * ((cols + 7) / 8 * 2);
+  if (threads >= (int64_t)1 << 32)
     return fail(AQMB_EUNSUPPORTED, "rms_norm: rows = %d of %d columns are more than one launch takes", rows, cols);
   if (x_stride < cols || y_stride < cols || (residual && residual_stride < cols))
     return fail(AQMB_EINVAL, "rms_norm: a row stride is below cols = %d", cols);
@@ -334,8 +336,9 @@ aqmb_status aqmb_kv_append(const aqmb_kv_cache* cache, const void* k, int64_t k_
   const int64_t row = (int64_t)cache->n_kv_heads * cache->head_dim;
   if (k_stride < row || v_stride < row) return fail(AQMB_EINVAL, "kv_append: a stride is below a token");
   if (!aligned(k, 2) || !aligned(v, 2) || !aligned(slots, 8)) return fail(AQMB_EINVAL, "kv_append: a misaligned pointer");
-  if ((int64_t)n_tokens * cache->n_kv_heads >= (int64_t)1 << 26)      // 64 threads each, 2^32 a launch
-    return fail(AQMB_EUNSUPPORTED, "kv_append: n_tokens * n_kv_heads of 2^26 or more");
+  // 64 threads each, in workgroups of four, fewer than 2^32 a launch
+  if (((int64_t)n_tokens * cache->n_kv_heads + 3) / 4 >= (int64_t)1 << 24)
+    return fail(AQMB_EUNSUPPORTED, "kv_append: n_tokens * n_kv_heads above 2^26 - 4");
   return hip_status(launch_kv_append(*cache, k, k_stride, v, v_stride, dtype, slots, n_tokens, (hipStream_t)stream),
                     "kv_append: launch");
 }

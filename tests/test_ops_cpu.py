@@ -271,3 +271,16 @@ def test_w4_create_refuses_what_one_launch_cannot_lay_out(d_out, d_in):
         assert A.lib.aqmb_w4_create(ctypes.byref(h), ctypes.byref(d), 16, 16, None, None) == S.EINVAL
         assert "tiles" in A.last_error()
     assert h.value is None
+
+
+def test_launches_are_counted_in_whole_workgroups():
+    """One row, or one token's head, below the limits still rounds up to a launch of 2^32 threads."""
+    c = cache(n_kv_heads=1, page_stride=1 << 20)
+    for tokens in ((1 << 26) - 3, (1 << 26) - 1):
+        assert A.lib.aqmb_kv_append(ctypes.byref(c), 64, 64, 64, 64, BF16, 64, tokens, None) == S.EUNSUPPORTED
+        assert "2^26" in A.last_error()
+    for rows in ((1 << 28) - 15, (1 << 28) - 1):
+        for cols in (1, 64):
+            assert A.lib.aqmb_rms_norm(64, BF16, cols, None, None, 0, 64, 0.0, 1e-5, rows, cols, 64, BF16, cols, None, 0,
+                                       None) == S.EUNSUPPORTED
+            assert "one launch" in A.last_error()
