@@ -7,13 +7,15 @@ buffers and the current PyTorch stream is used when no stream is given; PyTorch 
 (allocation and streams), not part of the computation.
 
 If the library has not been built, importing this package fails loudly: there is no
-fallback implementation.
+fallback implementation. ``_direct.so``, which takes usual calls past ctypes, may be missing:
+a warning says so, and every call reaches the same kernels through ctypes.
 """
 from __future__ import annotations
 
 import ctypes
 import enum
 import os
+import warnings
 from typing import Optional
 
 __all__ = ["Status", "DType", "Desc", "AqmbError", "GemvKernel", "GemmTiling", "lib", "create", "destroy", "get_desc",
@@ -163,15 +165,17 @@ lib = _load()
 import torch  # noqa: E402  (after the library's own import of it, see _load)
 
 # The operators between the layers take their usual calls past ctypes: _direct checks the tensors, makes the call
-# and returns its status, or None where the functions below have to look.
+# and returns its status, or None where the functions below have to look. Without it they take every call.
 try:
     from . import _direct  # noqa: E402
+    _direct.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+        "aqmb_rms_norm", "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes",
+        "aqmb_kv_append", "aqmb_kv_copy_pages")))
 except ImportError as e:
-    raise ImportError(f"{os.path.join(os.path.dirname(LIB_PATH), '_direct.so')} is missing or was built for another "
-                      f"PyTorch: build it first (python -m paper_2606_12876_amd.build)") from e
-_direct.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
-    "aqmb_rms_norm", "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes",
-    "aqmb_kv_append", "aqmb_kv_copy_pages")))
+    _direct = None
+    warnings.warn(f"{os.path.join(os.path.dirname(LIB_PATH), '_direct.so')} is missing or was built for another PyTorch "
+                  f"({e}): the operators between the layers go through ctypes, about 3 us a call dearer. Build it with "
+                  f"python -m paper_2606_12876_amd.build", RuntimeWarning)
 
 _TORCH_DT = {torch.float16: int(DType.F16), torch.bfloat16: int(DType.BF16), torch.float32: int(DType.F32)}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -592,7 +596,7 @@ def rms_norm(x, weight, y, *, eps: float, weight_offset: float = 0.0, residual=N
     [rows][ceil(cols / scale_group)] fp32; scale_group 0 is the whole row) float8_e4m3fn or int8.
     With a residual, x + residual is rounded into residual_out."""
     where = "aqmb_rms_norm"
-    if stream is None:
+    if stream is None and _direct is not None:
         st = _direct.rms_norm(x, weight, y, eps, weight_offset, residual, residual_out, scales, scale_group)
         if st is not None:
             return _check(st, where) if st else None
@@ -669,7 +673,7 @@ def w4_get_desc(layer: int) -> W4Desc:
 
 def _w4_gemv(layer: int, d_out: int, d_in: int, group_size: int, x, y, x_scales, stream) -> None:
     where = "aqmb_w4_gemv"
-    if stream is None:
+    if stream is None and _direct is not None:
         st = _direct.w4_gemv(layer, d_out, d_in, group_size, x, y, x_scales)
         if st is not None:
             return _check(st, where) if st else None
@@ -825,7 +829,7 @@ class KVCache:
         (default: what the table holds). Without a workspace one is taken from PyTorch's allocator on the
         call's stream."""
         where = "aqmb_paged_attention"
-        if stream is None:
+        if stream is None and _direct is not None:
             st = _direct.paged_attention(self._address, self.device_index, q, page_table, lengths, out, scale, max_length,
                                          window, lse, workspace)
             if st is not None:
@@ -894,7 +898,7 @@ class KVCache:
         """aqmb_kv_append: write k, v [n_tokens][n_kv_heads][head_dim] (fp16 or bf16) into slots int64
         [n_tokens] on the GPU (page * page_size + offset; outside the cache: skipped)."""
         where = "aqmb_kv_append"
-        if stream is None:
+        if stream is None and _direct is not None:
             st = _direct.kv_append(self._address, self.device_index, k, v, slots)
             if st is not None:
                 return _check(st, where) if st else None
@@ -936,7 +940,7 @@ def kv_copy_pages(caches, src, dst, stream=None) -> None:
     where = "aqmb_kv_copy_pages"
     if not isinstance(caches, (list, tuple)):
         caches = list(caches)
-    if stream is None:
+    if stream is None and _direct is not None:
         st = _direct.kv_copy_pages(caches, src, dst)
         if st is not None:
             return _check(st, where) if st else None

@@ -4,7 +4,8 @@ Objects go to ``_build/`` at the repository root; the shared library is written 
 this file, where the binding loads it. Every HIP source is compiled with packed-fp32
 instruction generation turned off. ``libaqmb_ceilings.so`` (the benchmark's measured-ceiling
 kernels, not part of the layer) and ``_direct.so`` (the binding's way from tensors to the library
-without ctypes; host code against the headers of Python and of the installed PyTorch) are built beside it.
+without ctypes; host code against the headers of Python and of the installed PyTorch, left out where those
+are missing) are built beside it.
 """
 from __future__ import annotations
 
@@ -54,8 +55,19 @@ def _rocm() -> str:
 
 
 def _torch() -> str:
-    """The installed PyTorch's folder (found, not imported: it would load its HIP runtime)."""
-    return os.path.dirname(importlib.util.find_spec("torch").origin)
+    """The installed PyTorch's folder (found, not imported: it would load its HIP runtime), "" if there is none."""
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else ""
+
+
+def _direct_lacks() -> str:
+    """The header that ``_direct.so`` needs and this machine does not have, "" if all are there."""
+    for header in (os.path.join(sysconfig.get_paths()["include"], "Python.h"),
+                   os.path.join(_torch(), "include", "torch", "csrc", "autograd", "python_variable.h"),
+                   os.path.join(_rocm(), "include", "hip", "hip_runtime_api.h")):
+        if not os.path.exists(header):
+            return header
+    return ""
 
 
 def _compile(src: str) -> str:
@@ -78,17 +90,24 @@ def _link(objs, lib, more=()):
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    srcs = SOURCES + CEIL_SOURCES + DIRECT_SOURCES
+    missing = _direct_lacks()
+    srcs = SOURCES + CEIL_SOURCES + ([] if missing else DIRECT_SOURCES)
     jobs = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(jobs) as ex:
-        objs = dict(zip(srcs, ex.map(_compile, srcs)))
-    _link([objs[s] for s in SOURCES], LIB)
-    _link([objs[s] for s in CEIL_SOURCES], CEIL_LIB)
-    # PyTorch's libraries are found by name: the package imports torch first.
-    _link([objs[s] for s in DIRECT_SOURCES], DIRECT_LIB,
-          ["-L" + os.path.join(_torch(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])
+        objs = {s: ex.submit(_compile, s) for s in srcs}
+    _link([objs[s].result() for s in SOURCES], LIB)
+    _link([objs[s].result() for s in CEIL_SOURCES], CEIL_LIB)
+    # The libraries are there; _direct.so, which the binding can do without, comes last. An old one must not stay.
+    if os.path.exists(DIRECT_LIB):
+        os.remove(DIRECT_LIB)
+    if missing:
+        print(f"{DIRECT_LIB} is not built: {missing} not found", file=sys.stderr)
+    else:
+        # PyTorch's libraries are found by name: the package imports torch first.
+        _link([objs[s].result() for s in DIRECT_SOURCES], DIRECT_LIB,
+              ["-L" + os.path.join(_torch(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])
     if verbose:
-        print(f"built {LIB}, {CEIL_LIB} and {DIRECT_LIB}")
+        print(f"built {LIB}, {CEIL_LIB}" + ("" if missing else f" and {DIRECT_LIB}"))
     return LIB
 
 
