@@ -383,7 +383,7 @@ double aqmb_bits_per_weight(const aqmb_desc* desc, int k);
  * and y = v rounded once (nearest even) for y_dtype F16, BF16 or F32; or, for y_dtype F8 or I8, per
  * group of `scale_group` columns (0: the whole row; the last group of a row may be shorter):
  *   a = max(max |v|, 2^-100), y = round(v * (L / a)) to nearest even, scale = a / L,
- *   L = 448 for F8, 127 for I8
+ *   L = 448 for F8, 127 for I8, both quotients rounded to binary32
  * so that y * scale stands for v. A group that holds a value that is not finite gets the scale NaN
  * and y = 0. h is not rounded before it is squared or scaled; a row whose squares overflow binary32
  * gives zeros, as the formula does.

@@ -50,9 +50,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) big = max(big, __builtin_bit_cast(uint32_t, f[i]) & 0x7FFFFFFFu);
     big = over_lanes<32>(big, max_bits);
-    const bool finite = big < 0x7F800000u;
-    const float m = fmaxf(__builtin_bit_cast(float, big), 7.888609052210118e-31f);   // at least 2^-100
-    const float mul = 448.f / m;
+    const Scaling scaling = scaling_of(big, 448.f);
+    const float mul = scaling.mul;
     uint2 b;
     uint32_t w[2];
 #pragma unroll
@@ -60,12 +59,11 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
       const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k] * mul, f[4 * k + 1] * mul, 0, false);
       w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k + 2] * mul, f[4 * k + 3] * mul, lo, true);
     }
-    b = finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
+    b = scaling.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
     if (on) *(uint2*)((uint8_t*)out + dst) = b;
     if (lane == 0) {
       float* sc = is_v ? a.c.v_scale : a.c.k_scale;
-      sc[page * a.c.n_kv_heads * a.c.page_size + head * a.sc_head + slot * a.sc_slot] =
-          finite ? m / 448.f : __builtin_nanf("");
+      sc[page * a.c.n_kv_heads * a.c.page_size + head * a.sc_head + slot * a.sc_slot] = scaling.scale;
     }
   }
 }

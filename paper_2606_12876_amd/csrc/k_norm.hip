@@ -108,8 +108,6 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
   return v;
 }
 
-constexpr float kScaleFloor = 7.888609052210118e-31f;  // 2^-100: keeps L / a and a / L normal numbers
-
 // NT threads per row: up to 64, part of a wave or a wave (256 / NT rows per workgroup); else the workgroup.
 template <int DT, int NT, int NV>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
@@ -158,8 +156,8 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
     for (int j = 0; j < 8; ++j) ss += h[i][j] * h[i][j];
   }
   ss = row_sum<NT>(ss, lds_sum);
-  // Reciprocals and root by the instructions, an ulp each (rsqrtf takes care of subnormals): a launch of few rows
-  // is bound by its waves' instructions, and the exact forms are 60 of them.
+  // Reciprocal and root by the instructions, an ulp each (rsqrtf takes care of subnormals): a launch of few rows
+  // is bound by its waves' instructions, and the sum before them is off by more.
   const float inv = rsqrtf(ss * __builtin_amdgcn_rcpf((float)a.cols) + a.eps);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -238,11 +236,9 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
   for (int i = 0; i < NV; ++i) {
     const int c = (i * NT + t) * 8, n = a.cols - c;
     if (n <= 0) continue;
-    const bool finite = m[i] < 0x7F800000u;
-    const float big = fmaxf(__builtin_bit_cast(float, m[i]), kScaleFloor);
-    const float mul = (top * 0x1p-20f) * __builtin_amdgcn_rcpf(big * 0x1p-20f);    // no step of it is subnormal
-    const float scale = finite ? big * (1.f / top) : __builtin_nanf("");
-    if ((c & ((1u << shift) - 1)) == 0) a.scales[row * n_groups + (c >> shift)] = scale;
+    const Scaling sc = scaling_of(m[i], top);
+    const float mul = sc.mul;
+    if ((c & ((1u << shift) - 1)) == 0) a.scales[row * n_groups + (c >> shift)] = sc.scale;
     B8 b;
     if (a.y_dtype == AQMB_F8) {
 #pragma unroll
@@ -261,7 +257,7 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
                                        __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400u), 0x05040100u);
       }
     }
-    if (!finite) b.w[0] = b.w[1] = 0;
+    if (!sc.finite) b.w[0] = b.w[1] = 0;
     uint8_t* y = (uint8_t*)a.y + row * a.y_stride + c;
     if (n >= 8) {
       *(B8*)y = b;

@@ -1,3 +1,4 @@
+// Shared by the kernels between the layers.
 // Reductions across lanes without LDS: within a row of 16 lanes by data-parallel moves, across rows by
 // the row swaps of gfx950. Every lane receives the result.
 #pragma once
@@ -38,6 +39,19 @@ __device__ __forceinline__ uint32_t over_lanes(uint32_t x, F f) {
 __device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t add_floats(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+}
+
+// How a group of values is brought to 8 bits: from the largest magnitude's bits (those of infinity and NaN are
+// above every finite value's) the factor of the values and the scale that the results stand for, each the rounded
+// quotient, so that every kernel that scales does it alike. The floor keeps both normal numbers.
+struct Scaling {
+  float mul, scale;
+  bool finite;
+};
+__device__ __forceinline__ Scaling scaling_of(uint32_t largest, float top) {
+  const bool finite = largest < 0x7F800000u;
+  const float a = fmaxf(__builtin_bit_cast(float, largest), 0x1p-100f);
+  return {top / a, finite ? a / top : __builtin_nanf(""), finite};
 }
 
 }  // namespace aqmb
