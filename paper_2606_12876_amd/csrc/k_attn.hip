@@ -34,6 +34,8 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 32, kChunkMax = 4096, kXcds = 8;
 constexpr int kWavesSplit = 4, kWavesWhole = 8;   // per workgroup, where sequences are split and where not
+// The kernel's own LDS beside its dynamic part, at most: statistics, offsets and scales of 8 waves, joined statistics.
+constexpr size_t kStaticLds = kWavesWhole * (2 * 16 * 4 + 32 * 8 + 64 * 4) + 2 * 16 * 4;
 
 // The binary32 number next to another one on the side of 0; 0 for 0 (but not for -0).
 __device__ __forceinline__ float below(float x) {
@@ -154,6 +156,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   __shared__ float s_ml[kWaves][2][16], s_join[2][16];
   __shared__ __attribute__((aligned(16))) int64_t s_row[kWaves][32];      // byte offsets of a tile's positions
   __shared__ __attribute__((aligned(16))) float s_scale[kWaves][64];      // scales of its keys, then values
+  static_assert(sizeof(s_ml) + sizeof(s_join) + sizeof(s_row) + sizeof(s_scale) <= kStaticLds, "launch attribute");
 
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, q = lane / 16;
@@ -586,7 +589,7 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   const dim3 grid = A.block ? dim3((unsigned)ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
-    if (lds > 65536 - 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (lds + kStaticLds > 65536) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e == hipSuccess) kernel<<<grid, 64 * a.waves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };

@@ -447,3 +447,14 @@ def test_negative_scales(length, scale, dtype):
     for s in (c.k_scale, c.v_scale):
         s.mul_(torch.randint(-1, 2, s.shape, generator=g, device="cuda"))
     attend(c, normal(g, 2, 4, 64, dtype=dtype, std=2.0), table, lens, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,cache", [(torch.float16, None), (torch.bfloat16, F8)])
+@pytest.mark.parametrize("dim,bound", [(112, 200), (120, 200), (120, 380), (128, 200), (232, 500), (240, 500), (248, 500), (256, 500)])
+def test_workgroups_around_64_kib_of_lds(dim, bound, dtype, cache):
+    """16 query heads to a key-value head, whole sequences by 8 waves (to 128) and chunks by 4: the sums and what the
+    kernel holds beside them come to 60 to 70 KiB."""
+    g = gen(dim)
+    c, table, lens = build(g, [bound, 1, 77], 2, dim, 20, dtype, cache)
+    assert (c.workspace_bytes(32, 3, bound) == 0) == (dim <= 128)
+    attend(c, normal(g, 3, 32, dim, dtype=dtype, std=2.0), table, lens, max_length=bound)
