@@ -131,6 +131,13 @@ __device__ __forceinline__ uint32_t max_floats(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
 }
 
+// A launch takes fewer than 2^32 threads along a dimension: longer rows of workgroups go on along the next. A
+// multiple of kXcds.
+constexpr int kGridX = 1 << 20;
+static dim3 folded(int64_t workgroups) {
+  return workgroups <= kGridX ? dim3((unsigned)workgroups) : dim3(kGridX, (unsigned)((workgroups + kGridX - 1) / kGridX));
+}
+
 struct AttnDev {
   AttnArgs a;
   int page_shift;          // log2 of page_size, -1 if it is no power of two
@@ -167,7 +174,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
   // XCD is left with the late chunks that short sequences lack (64 ragged streams: 155 us, of which 30 were that).
   int kvh = blockIdx.x, ht = 0, seq = blockIdx.y, split = blockIdx.z;
   if (A.block) {
-    const int k = blockIdx.x / kXcds, unit = k / A.block * kXcds + blockIdx.x % kXcds, row = a.n_seqs * A.blocks;
+    const int id = blockIdx.y * kGridX + blockIdx.x;            // one row of workgroups, folded where it is long
+    const int k = id / kXcds, unit = k / A.block * kXcds + id % kXcds, row = a.n_seqs * A.blocks;
     if (unit >= row * a.n_splits) return;
     split = unit / row;
     const int rest = unit - split * row, s = rest / A.blocks, head = (rest - s * A.blocks) * A.block + k % A.block;
@@ -479,7 +487,7 @@ __device__ __forceinline__ void join_one(float m, float l, f32x4_t x, float& M, 
 template <int T>
 __global__ __launch_bounds__(kJoinFew) void attn_join_few_kernel(AttnArgs a, float shift) {
   const int quads = a.head_dim / 4, heads = kJoinFew / quads, g = threadIdx.x / quads, d = threadIdx.x % quads * 4;
-  const int64_t at = (int64_t)blockIdx.x * heads + g;
+  const int64_t at = ((int64_t)blockIdx.y * kGridX + blockIdx.x) * heads + g;
   if (g >= heads || at >= (int64_t)a.n_seqs * a.n_heads) return;
   const int seq = (int)(at / a.n_heads), n = chunks_of(a, seq);
   const float* ml = a.part + (int64_t)a.n_seqs * a.n_heads * a.n_splits * a.head_dim + at * a.n_splits * 2;
@@ -585,8 +593,8 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   A.blocks = a.n_kv / share;
   const int64_t units = (int64_t)a.n_seqs * a.n_splits * A.blocks;
   const int64_t ids = (units + kXcds - 1) / kXcds * kXcds * A.block;
-  if (ids > 0x7FFFFFFF) return hipErrorInvalidValue;
-  const dim3 grid = A.block ? dim3((unsigned)ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
+  if (ids > 0x7FFFFFFF - kGridX) return hipErrorInvalidValue;
+  const dim3 grid = A.block ? folded(ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
     if (lds + kStaticLds > 65536) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -606,7 +614,7 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   if (a.n_splits <= kFewChunks) {
     const int heads = kJoinFew / (a.head_dim / 4);
     const int64_t all = (int64_t)a.n_heads * a.n_seqs;
-    attn_join_few_kernel<T><<<(unsigned)((all + heads - 1) / heads), kJoinFew, 0, st>>>(a, Mma<PT>::kShift);
+    attn_join_few_kernel<T><<<folded((all + heads - 1) / heads), kJoinFew, 0, st>>>(a, Mma<PT>::kShift);
   } else {
     attn_join_kernel<T><<<dim3(a.n_heads, a.n_seqs), kJoin, 0, st>>>(a, Mma<PT>::kShift);
   }

@@ -458,3 +458,25 @@ def test_workgroups_around_64_kib_of_lds(dim, bound, dtype, cache):
     c, table, lens = build(g, [bound, 1, 77], 2, dim, 20, dtype, cache)
     assert (c.workspace_bytes(32, 3, bound) == 0) == (dim <= 128)
     attend(c, normal(g, 3, 32, dim, dtype=dtype, std=2.0), table, lens, max_length=bound)
+
+
+def test_more_workgroups_than_fit_along_one_dimension():
+    """65535 sequences under a bound of 33 chunks, 8 heads that share lines: 2^32 threads and more, most without a
+    position."""
+    n, kv, dim, page = 65535, 8, 8, 32768
+    g = gen(94)
+    c = A.KVCache(normal(g, 6, page, kv, dim, dtype=torch.float16), normal(g, 6, page, kv, dim, dtype=torch.float16), layout="slot")
+    lens = torch.zeros((n,), dtype=torch.int32, device="cuda")
+    table = torch.full((n, 5), -1, dtype=torch.int32, device="cuda")
+    held = [0, 1, 4095, 40000, n - 1]
+    for i, length in zip(held, (5000, 1, 32769, 100, 9000)):
+        lens[i] = length
+        table[i] = torch.randperm(6, generator=g, device="cuda")[:5]
+    q = normal(g, n, kv, dim, dtype=torch.float16)
+    out = torch.full_like(q, 9.0)
+    bound = 33 * 4096
+    assert n * 33 * kv * 256 >= 2 ** 32 and c.workspace_bytes(kv, n, bound) == n * kv * 33 * (dim + 2) * 4
+    c.attention(q, table, lens, out, scale=0.3, max_length=bound)
+    check(c, q[held], table[held], lens[held], 0.3, 0, out[held], None)
+    out[held] = 0
+    assert (out == 0).all()
