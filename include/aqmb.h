@@ -495,8 +495,10 @@ typedef struct {
  *               no position < lengths[s] needs may hold anything. A page outside [0, n_pages) is
  *               skipped: its positions do not exist.
  *   lengths     int32 [n_seqs], device memory; values outside [0, max_length] are clamped
- *   max_length  an upper bound of the lengths, <= table_stride * page_size and <= 2^27: fixes how the work is
- *               split, so results do not depend on other sequences' lengths
+ *   max_length  an upper bound of the lengths, <= table_stride * page_size and <= 2^27: fixes, with window, n_seqs
+ *               and the cache's shape, how a sequence's work is split and in which order it is summed. A
+ *               sequence's result does not depend, to the bit, on the lengths and contents of the others; under
+ *               another bound or beside another number of sequences its last digits may differ
  * Slots that hold no token may hold anything (NaN included). Scores and softmax are binary32; the
  * probabilities enter the matrix cores as two 16-bit parts. One rounding to `dtype`.
  * workspace: aqmb_paged_attention_workspace_bytes bytes of device memory, 16-byte aligned, written

@@ -480,3 +480,27 @@ def test_more_workgroups_than_fit_along_one_dimension():
     check(c, q[held], table[held], lens[held], 0.3, 0, out[held], None)
     out[held] = 0
     assert (out == 0).all()
+
+
+@pytest.mark.parametrize("dtype,cache", [(torch.float16, None), (torch.bfloat16, F8)])
+@pytest.mark.parametrize("layout,dim", [("head", 128), ("slot", 80)])
+@pytest.mark.parametrize("bound,window", [(300, 0), (1300, 0), (1300, 1000), (20000, 0)])        # whole, few chunks, many
+def test_neighbours_do_not_change_a_bit(bound, window, layout, dim, dtype, cache):
+    """The same call but for the other sequences' lengths and pages: the same bits."""
+    g = gen(95)
+    lens_ = [bound, 7, bound // 2 + 1, bound - 1]
+    c, table, lens = build(g, lens_, 2, dim, 16, dtype, cache, layout)
+    q = normal(g, 4, 6, dim, dtype=dtype, std=2.0)
+
+    def run(table, lens):
+        out, lse = torch.empty_like(q), torch.empty((4, 6), device="cuda")
+        c.attention(q, table, lens, out, scale=dim ** -0.5, max_length=bound, window=window, lse=lse)
+        return out, lse
+
+    want = run(table, lens)
+    for keep in range(4):
+        for other in (0, 1, bound // 3, bound):
+            lens2, table2 = torch.full_like(lens, other), table[[3, 3, 3, 3]].clone()
+            lens2[keep], table2[keep] = lens[keep], table[keep]
+            got = run(table2, lens2)
+            assert torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[1][keep], want[1][keep])
