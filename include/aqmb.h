@@ -500,7 +500,8 @@ typedef struct {
  *               sequence's result does not depend, to the bit, on the lengths and contents of the others; under
  *               another bound or beside another number of sequences its last digits may differ
  * Slots that hold no token may hold anything (NaN included). Scores and softmax are binary32; the
- * probabilities enter the matrix cores as two 16-bit parts. One rounding to `dtype`.
+ * probabilities enter the matrix cores as two 16-bit parts (22 bits with an F16 cache, 16 with a BF16 or F8 one).
+ * One rounding to `dtype`.
  * workspace: aqmb_paged_attention_workspace_bytes bytes of device memory, 16-byte aligned, written
  * by the call (calls that share one must be ordered); 0 bytes: NULL is fine.
  * Errors: EINVAL (null or misaligned pointer, sizes < 1, n_heads not a multiple of n_kv_heads,

@@ -457,7 +457,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_kernel(AttnDev A) {
 // lanes take one chunk after the other (with the loads under way together) and a workgroup has several
 // heads; beyond, a workgroup has one head and each group of lanes every so-many-th chunk with a running
 // maximum of its own, and the groups meet in LDS. 64 streams x 32 heads x 2 chunks: 7.3 us by the second
-// form, 4.8 by the first; 16 chunks of one stream 3.8 and 4.0.
+// form, 4.8 by the first; 16 chunks of one stream 3.8 and 4.0. Between these the limit is a guess: nothing was timed.
 constexpr int kJoin = 512, kJoinFew = 256, kFewChunks = 4;
 
 __device__ __forceinline__ int chunks_of(const AttnArgs& a, int seq) {
@@ -547,7 +547,7 @@ AttnPlan attn_plan(int n_heads, int n_kv, int head_dim, int n_seqs, int max_leng
   chunk = chunk < unit ? unit : chunk > kChunkMax ? kChunkMax : chunk;
   AttnPlan p;
   // Short sequences stay whole, with twice the waves, which saves the second launch; where they leave most of the
-  // card idle, a quarter less is short. Calls in sequence, whole and split, 8 key-value heads of 128 (queries 4
+  // card idle, a quarter less is short (384 positions with heads of 128; from there to about 450 there is little in it). Calls in sequence, whole and split, 8 key-value heads of 128 (queries 4
   // times as many): one sequence of 300, 6.8 and 8.5 us; of 400, 7.7 and 7.9; of 500, 8.3 and 7.9; 64 of up to 500,
   // 16.6 and 18.9. Heads of 64: one of 700, 7.3 and 7.8 us; of 1000, 8.8 and 7.8; 64 of up to 1000, 16.3 and 19.8.
   // Heads of 256, 2 of 250: 9.2 and 9.9.
