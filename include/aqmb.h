@@ -586,6 +586,155 @@ aqmb_status aqmb_pages_compact(aqmb_pages_t pool, int32_t* src, int32_t* dst, in
 aqmb_status aqmb_pages_table(aqmb_pages_t pool, int seq, int32_t* table, int capacity, int* n_used, int* length);
 aqmb_status aqmb_pages_counts(aqmb_pages_t pool, int* n_free, int* n_live);
 
+/*
+ * Rotary positions. Of every head the first rotary_dim values form rotary_dim / 2 pairs (a, b), turned by the
+ * angle position * frequencies[i] of pair i:
+ *   a' = amplitude * (a cos - b sin), b' = amplitude * (b cos + a sin), inverse: by the angle's negative (what the
+ *   gradient of the turned values is turned by)
+ *   AQMB_ROTARY_HALF         pair i is values i and i + rotary_dim / 2
+ *   AQMB_ROTARY_INTERLEAVED  pair i is values 2 i and 2 i + 1
+ * The other values of a head stay as they are.
+ *   frequencies  fp64 [rotary_dim / 2], radians per position, device memory, 8-byte aligned
+ *                (aqmb_rotary_frequencies gives the usual ones)
+ *   rotary_dim   even, 2..head_dim
+ */
+typedef enum { AQMB_ROTARY_HALF = 0, AQMB_ROTARY_INTERLEAVED = 1 } aqmb_rotary_layout;
+typedef struct {
+  const double* frequencies;
+  int32_t rotary_dim;
+  int32_t layout;         /* aqmb_rotary_layout */
+  float amplitude;
+  int32_t inverse;        /* 0 or 1 */
+} aqmb_rotary_desc;
+
+/*
+ * Frequencies f_i = base^(-2 i / rotary_dim), i < rotary_dim / 2, in HOST memory, and the amplitude that goes with
+ * them, scaled for a context `factor` times the original one:
+ *   AQMB_ROTARY_PLAIN    as they are (scaling NULL is the same); amplitude 1
+ *   AQMB_ROTARY_LINEAR   f_i / factor; amplitude 1
+ *   AQMB_ROTARY_BASE     of the base base * factor^(rotary_dim / (rotary_dim - 2)): the first stays, the last is
+ *                        divided by factor (rotary_dim 2: as plain); amplitude 1
+ *   AQMB_ROTARY_RAMP     between f_i / factor and f_i by the pair's index: with d(n) = rotary_dim / 2 *
+ *                        log(original_length / (2 pi n)) / log(base) the index that turns n times over the original
+ *                        length, lo = max(floor(d(high)), 0), hi = min(ceil(d(low)), rotary_dim - 1), t = clamp((i - lo) /
+ *                        max(hi - lo, 0.001), 0, 1), the frequency is f_i (1 - t) + f_i / factor t; amplitude
+ *                        0.1 log(factor) + 1
+ *   AQMB_ROTARY_TURNS    between them by the turns n_i = original_length f_i / (2 pi) themselves: t = clamp((n_i -
+ *                        low) / (high - low), 0, 1), the frequency is f_i / factor (1 - t) + f_i t; amplitude 1
+ * All in binary64. Either output may be NULL.
+ * Errors: EINVAL (rotary_dim odd or < 2, base not finite or <= 1, factor not finite or < 1, original_length < 1, low
+ * or high not finite, low <= 0 or high <= low where they are used), EUNSUPPORTED (unknown kind).
+ */
+typedef enum { AQMB_ROTARY_PLAIN = 0, AQMB_ROTARY_LINEAR = 1, AQMB_ROTARY_BASE = 2, AQMB_ROTARY_RAMP = 3,
+               AQMB_ROTARY_TURNS = 4 } aqmb_rotary_kind;
+typedef struct {
+  int32_t kind;           /* aqmb_rotary_kind */
+  int32_t original_length;/* RAMP and TURNS only, as the next two */
+  double factor;
+  double low, high;       /* turns over the original length (RAMP: 1 and 32 are usual; TURNS: 1 and 4) */
+} aqmb_rotary_scaling;
+aqmb_status aqmb_rotary_frequencies(int rotary_dim, double base, const aqmb_rotary_scaling* scaling,
+                                    double* frequencies, float* amplitude);
+
+/*
+ * Turns the queries and keys of n_tokens tokens. Angles are binary64 products of the position and the frequency,
+ * reduced by whole turns before they are rounded; sines, cosines and the turn are binary32 (sine and cosine to
+ * 2^-22), one rounding to `dtype`.
+ *   q, q_out   [n_tokens][n_heads][head_dim] F16 or BF16 (`dtype`), stride between tokens q_stride / q_out_stride
+ *   k, k_out   the same with n_kv_heads; both NULL (n_kv_heads 0): no keys
+ *   positions  int64 [n_tokens], device memory, of any size and sign
+ * q_out may be q and k_out may be k (same stride); no other overlap. head_dim: a multiple of 8 up to 256.
+ * Errors: EINVAL (null or misaligned pointer, sizes < 1, a stride below a token, rotary_dim odd or outside
+ * [2, head_dim], amplitude not finite, unknown layout or inverse), EUNSUPPORTED (dtype, head_dim, n_heads or n_kv_heads above
+ * 65535, n_tokens * (n_heads + n_kv_heads rounded up to a multiple of 8) of 2^27 or more), EHIP.
+ */
+aqmb_status aqmb_rotary(const aqmb_rotary_desc* rotary, const void* q, int64_t q_stride, void* q_out,
+                        int64_t q_out_stride, int n_heads, const void* k, int64_t k_stride, void* k_out,
+                        int64_t k_out_stride, int n_kv_heads, aqmb_dtype dtype, int head_dim, const int64_t* positions,
+                        int n_tokens, aqmb_stream_t stream);
+
+/*
+ * The same with the keys written into a cache at once, and the values beside them: q_out = q turned, and what
+ * aqmb_kv_append does with the turned keys and v, in one launch. With a 16-bit cache the results are those of the two
+ * calls to the bit; with an F8 cache the keys are scaled from their binary32 values, with one rounding less.
+ *   k, v   [n_tokens][cache's n_kv_heads][cache's head_dim] `dtype` as aqmb_kv_append, strides k_stride, v_stride
+ *   slots  int64 [n_tokens] as aqmb_kv_append; q_out is written for every token, also where the slot is skipped
+ * Errors: those of aqmb_rotary and aqmb_kv_append, with n_heads + 2 n_kv_heads in the limit of the former.
+ */
+aqmb_status aqmb_rotary_append(const aqmb_kv_cache* cache, const aqmb_rotary_desc* rotary, const void* q,
+                               int64_t q_stride, void* q_out, int64_t q_out_stride, int n_heads, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, aqmb_dtype dtype,
+                               const int64_t* positions, const int64_t* slots, int n_tokens, aqmb_stream_t stream);
+
+/*
+ * Low-rank adapters of many requests beside one projection: the caller's stacks of n_adapters pairs of matrices.
+ *   a       [n_adapters][rank][d_in] F16 or BF16 (`dtype`), dense
+ *   b       [n_adapters][d_out][rank] `dtype`, dense
+ *   scales  fp32 [n_adapters]; NULL: 1 everywhere
+ *   ranks   int32 [n_adapters]: how many rows of an adapter's a and columns of its b are its own (clamped to
+ *           [0, rank]); what lies behind them is not used and may hold anything. NULL: rank everywhere
+ * All in device memory, read when a call runs: an adapter may be exchanged between calls.
+ * 1 <= rank <= AQMB_MAX_RANK; d_in and d_out of any size up to 2^24.
+ */
+#define AQMB_MAX_RANK 256
+typedef struct {
+  const void* a;
+  const void* b;
+  const float* scales;
+  const int32_t* ranks;
+  int32_t dtype;          /* aqmb_dtype */
+  int32_t n_adapters;
+  int32_t rank;
+  int32_t d_in;
+  int32_t d_out;
+} aqmb_adapters;
+
+/*
+ * out[i] = base[i] + scales[n] * B_n (A_n x[i]) with n = index[i]; out[i] = base[i] where index[i] is outside
+ * [0, n_adapters) (-1: a request without an adapter). Products are exact and summed in binary32 on the matrix cores;
+ * A_n x times the scale enters the second product as two (F16, 22 bits of the row's largest) or three (BF16, 24 bits)
+ * 16-bit parts; one rounding to y_dtype. A row whose A_n x holds a value that is not finite gives values that are not finite.
+ *   x      [n_rows][d_in] of the adapters' dtype, row stride x_stride
+ *   index  int32 [n_rows], device memory, in any order
+ *   base   [n_rows][d_out] y_dtype in {F16, BF16, F32}, row stride base_stride; what aqmb_gemv or aqmb_w4_gemv gave
+ *   out    the same type, row stride out_stride
+ * out may be base (same stride; then rows without an adapter are not touched); no other overlap. A row's sums do not depend on the
+ * other rows' contents, only on their number.
+ * workspace: aqmb_adapters_workspace_bytes bytes of device memory, 16-byte aligned, written by the call (calls that
+ * share one must be ordered); 0 bytes: NULL is fine.
+ * Errors: EINVAL (null or misaligned pointer, sizes < 1, a stride below a row, out in place with another stride,
+ * workspace too small), EUNSUPPORTED (dtype, rank, d_in, d_out, n_adapters above 2^24, n_rows above 2^22 - 64,
+ * ceil(n_rows / 64) * ceil(d_out / 256) of 2^23 or more), EHIP.
+ */
+aqmb_status aqmb_adapters_add(const aqmb_adapters* adapters, const void* x, int64_t x_stride, const int32_t* index,
+                              int n_rows, const void* base, int64_t base_stride, void* out, int64_t out_stride,
+                              aqmb_dtype y_dtype, void* workspace, size_t workspace_bytes, aqmb_stream_t stream);
+aqmb_status aqmb_adapters_workspace_bytes(const aqmb_adapters* adapters, int n_rows, size_t* bytes);
+
+/*
+ * Of every row of logits, with z = scale * logits: the log probabilities z_t - log sum exp z of given tokens, the
+ * logarithm of the sum, the entropy - sum p log p, and the largest values with their log probabilities, in
+ * descending order (equal ones: the lower token first; -0 equals 0).
+ *   logits        [rows][vocab] F16, BF16 or F32 (`dtype`), row stride `stride`
+ *   targets       int64 [rows][n_targets], dense; a negative one (padding) gets 0, one >= vocab NaN
+ *   logprobs      fp32 [rows][n_targets]; targets and logprobs both NULL with n_targets 0
+ *   lse, entropy  fp32 [rows], or NULL
+ *   top_ids, top_logprobs  int64 and fp32 [rows][n_top]; n_top 0: both NULL, else either may be NULL
+ * A value of -infinity has probability 0 (log probability -infinity) and may be among the top ones where fewer others
+ * are there; n_top <= vocab. A row of nothing but -infinity: lse and log probabilities -infinity, entropy 0. A row with a NaN
+ * or +infinity: everything NaN, top_ids -1. Sums are binary32, relative to the largest value. A row's results do not depend on the others' contents.
+ * workspace: aqmb_log_probs_workspace_bytes bytes of device memory, 16-byte aligned, written by the call (calls that
+ * share one must be ordered); 0 bytes: NULL is fine.
+ * Errors: EINVAL (null or misaligned pointer, sizes < 1, n_targets < 0, n_top < 0 or > vocab, stride below vocab, scale not finite
+ * or below 2^-120, outputs without inputs, no output at all, workspace too small), EUNSUPPORTED (dtype, n_top > AQMB_MAX_TOP, rows above 2^22), EHIP.
+ */
+#define AQMB_MAX_TOP 64
+aqmb_status aqmb_log_probs(const void* logits, aqmb_dtype dtype, int64_t stride, int rows, int vocab, float scale,
+                           const int64_t* targets, int n_targets, float* logprobs, float* lse, float* entropy,
+                           int64_t* top_ids, float* top_logprobs, int n_top, void* workspace, size_t workspace_bytes,
+                           aqmb_stream_t stream);
+aqmb_status aqmb_log_probs_workspace_bytes(aqmb_dtype dtype, int rows, int vocab, int n_top, size_t* bytes);
+
 /* Static description of a status code. Never NULL. */
 const char* aqmb_strerror(aqmb_status status);
 

@@ -1,7 +1,7 @@
 """Definitions in 64 bits of the operators between the layers of a decode step.
 
 Root-mean-square norm with the residual's addition, scaling to 8 bits, products with 4-bit weights,
-attention of one token over a paged cache. Plain NumPy loops and sums; inputs are fp64 arrays that
+attention of one token over a paged cache; rotary positions, low-rank adapters and log probabilities. Plain NumPy loops and sums; inputs are fp64 arrays that
 hold the exact values of the stored formats. The definitions are those of ``include/aqmb.h``;
 the paper does not treat these operators (parity unpinned by it; closed forms pin them in
 ``tests/test_oracle_decode.py``).
@@ -91,3 +91,37 @@ def paged_attention(q, k, v, table, lengths, scale, window=0, layout="head"):
             out[i, h], lse[i, h] = attend(q[i, h], k[page, g, slot] if where else np.zeros((0, dim)),
                                           v[page, g, slot] if where else np.zeros((0, dim)), scale)
     return out, lse
+
+
+def rotary(x, angles, half, amplitude=1.0):
+    """x [n][heads][dim] with its first 2 * angles.shape[1] values turned in pairs by angles [n][pairs]: values i and
+    i + pairs (half) or 2 i and 2 i + 1."""
+    n, y = angles.shape[1], np.array(x, dtype=np.float64)
+    for i in range(n):
+        a, b = (i, i + n) if half else (2 * i, 2 * i + 1)
+        c, s = np.cos(angles[:, i])[:, None], np.sin(angles[:, i])[:, None]
+        y[..., a] = amplitude * (x[..., a] * c - x[..., b] * s)
+        y[..., b] = amplitude * (x[..., b] * c + x[..., a] * s)
+    return y
+
+
+def adapted(x, index, a, b, scales, ranks):
+    """scales[n] * b[n] (a[n] x) for every row of x with n = index[row], 0 where there is no such adapter."""
+    y = np.zeros((x.shape[0], b.shape[1]))
+    for i, n in enumerate(index):
+        if 0 <= n < a.shape[0]:
+            r = min(max(int(ranks[n]), 0), a.shape[1])
+            y[i] = scales[n] * (b[n, :, :r] @ (a[n, :r] @ x[i]))
+    return y
+
+
+def log_probs(z):
+    """(log p, log sum exp, entropy) of one row z; -infinity weighs nothing, NaN or +infinity makes all of it NaN."""
+    if np.isnan(z).any() or (z == np.inf).any():
+        return np.full_like(z, np.nan), np.nan, np.nan
+    top = z.max()
+    if top == -np.inf:
+        return z, -np.inf, 0.0
+    s = np.log(np.exp(z - top).sum())
+    lp = z - top - s                  # of the sum's logarithm nothing is left in 64 bits beside a top of 1e38
+    return lp, top + s, -sum(np.exp(v) * v for v in lp if v > -np.inf)

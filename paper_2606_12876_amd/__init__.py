@@ -22,7 +22,9 @@ __all__ = ["Status", "DType", "Desc", "AqmbError", "GemvKernel", "GemmTiling", "
            "gemv", "gemv_select", "gemm", "gemm_select", "dequant", "bits_per_weight", "strerror", "last_error",
            "validate", "QuantLinear", "LIB_PATH", "KVLayout", "W4Desc", "rms_norm", "w4_create", "w4_destroy",
            "w4_get_desc", "w4_gemv", "W4Linear", "KVCache", "paged_attention", "paged_attention_workspace_bytes",
-           "kv_append", "kv_copy_pages", "PagePool"]
+           "kv_append", "kv_copy_pages", "PagePool", "RotaryLayout", "RotaryScaling", "Rotary", "rotary_frequencies",
+           "rotary", "rotary_append", "Adapters", "adapters_add", "adapters_workspace_bytes", "log_probs",
+           "log_probs_workspace_bytes"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libaqmb.so")
 
@@ -47,6 +49,21 @@ class KVLayout(enum.IntEnum):
     """aqmb_kv_layout: the order inside a page of a key-value cache."""
     HEAD_MAJOR = 0
     SLOT_MAJOR = 1
+
+
+class RotaryLayout(enum.IntEnum):
+    """aqmb_rotary_layout: which values of a head form a pair."""
+    HALF = 0
+    INTERLEAVED = 1
+
+
+class RotaryScaling(enum.IntEnum):
+    """aqmb_rotary_kind: how frequencies are scaled for a longer context."""
+    PLAIN = 0
+    LINEAR = 1
+    BASE = 2
+    RAMP = 3
+    TURNS = 4
 
 
 class GemvKernel(enum.IntEnum):
@@ -81,6 +98,25 @@ class KVCacheDesc(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("layout", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """aqmb_rotary_desc."""
+    _fields_ = [("frequencies", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("amplitude", ctypes.c_float), ("inverse", ctypes.c_int32)]
+
+
+class RotaryScalingDesc(ctypes.Structure):
+    """aqmb_rotary_scaling."""
+    _fields_ = [("kind", ctypes.c_int32), ("original_length", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    """aqmb_adapters."""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ranks", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32)]
 
 
 class AqmbError(RuntimeError):
@@ -130,6 +166,15 @@ def _load() -> ctypes.CDLL:
     L.aqmb_paged_attention_workspace_bytes.argtypes = [cp, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
     L.aqmb_kv_append.argtypes = [cp, vp, i64, vp, i64, i32, vp, i32, vp]
     L.aqmb_kv_copy_pages.argtypes = [cp, i32, vp, vp, i32, vp]
+    sz = ctypes.POINTER(ctypes.c_size_t)
+    rp, ap = ctypes.POINTER(RotaryDesc), ctypes.POINTER(AdaptersDesc)
+    L.aqmb_rotary_frequencies.argtypes = [i32, ctypes.c_double, ctypes.POINTER(RotaryScalingDesc), vp, ctypes.POINTER(f32)]
+    L.aqmb_rotary.argtypes = [rp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, i32, i32, vp, i32, vp]
+    L.aqmb_rotary_append.argtypes = [cp, rp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, vp, i32, vp]
+    L.aqmb_adapters_workspace_bytes.argtypes = [ap, i32, sz]
+    L.aqmb_adapters_add.argtypes = [ap, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp, ctypes.c_size_t, vp]
+    L.aqmb_log_probs_workspace_bytes.argtypes = [i32, i32, i32, i32, sz]
+    L.aqmb_log_probs.argtypes = [vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     L.aqmb_pages_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32]
     L.aqmb_pages_destroy.argtypes = [vp]
     L.aqmb_pages_add.argtypes = [vp, ip]
@@ -155,7 +200,8 @@ def _load() -> ctypes.CDLL:
               "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes", "aqmb_kv_append",
               "aqmb_kv_copy_pages", "aqmb_pages_create", "aqmb_pages_destroy", "aqmb_pages_add", "aqmb_pages_fork",
               "aqmb_pages_extend", "aqmb_pages_free", "aqmb_pages_compact", "aqmb_pages_table",
-              "aqmb_pages_counts"):
+              "aqmb_pages_counts", "aqmb_rotary_frequencies", "aqmb_rotary", "aqmb_rotary_append",
+              "aqmb_adapters_workspace_bytes", "aqmb_adapters_add", "aqmb_log_probs_workspace_bytes", "aqmb_log_probs"):
         getattr(L, f).restype = st
     return L
 
@@ -894,6 +940,25 @@ class KVCache:
             _refuse(where, f"{what}: the heads of a row must be dense")
         return t.stride(0) if n > 1 else row
 
+    def rotary_append(self, rotary: "Rotary", q, k, v, positions, slots, q_out, stream=None) -> None:
+        """aqmb_rotary_append: q [n_tokens][n_heads][head_dim] turned into q_out, k turned and v written into slots
+        int64 [n_tokens], at positions int64 [n_tokens], all on the GPU."""
+        where = "aqmb_rotary_append"
+        dev = _current_device()
+        if dev != self.device_index:
+            self._current(where)
+        _here(where, q=q, k=k, v=v, positions=positions, slots=slots, q_out=q_out, frequencies=rotary.frequencies)
+        n, heads, dt, qs, os_ = _rotary_tensors(q, q_out, positions, self.head_dim, where)
+        shape, row = (n, self.n_kv_heads, self.head_dim), self.n_kv_heads * self.head_dim
+        if k.shape != shape or v.shape != shape or k.dtype != q.dtype or v.dtype != q.dtype:
+            _refuse(where, f"k is {tuple(k.shape)} of {k.dtype} and v {tuple(v.shape)} of {v.dtype}, not {shape} of {q.dtype}")
+        _dense(slots, torch.int64, n, "slots", where)
+        st = lib.aqmb_rotary_append(self._ref, rotary._ref, q.data_ptr(), qs, q_out.data_ptr(), os_, heads, k.data_ptr(),
+                                    self._stride(k, n, row, "k", where), v.data_ptr(), self._stride(v, n, row, "v", where),
+                                    dt, positions.data_ptr(), slots.data_ptr(), n, _stream(stream))
+        if st:
+            _check(st, where)
+
     def append(self, k, v, slots, stream=None) -> None:
         """aqmb_kv_append: write k, v [n_tokens][n_kv_heads][head_dim] (fp16 or bf16) into slots int64
         [n_tokens] on the GPU (page * page_size + offset; outside the cache: skipped)."""
@@ -933,6 +998,11 @@ def paged_attention_workspace_bytes(cache: KVCache, n_heads: int, n_seqs: int, m
 def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
     """aqmb_kv_append (see KVCache.append)."""
     cache.append(k, v, slots, stream)
+
+
+def rotary_append(cache: KVCache, rotary: "Rotary", q, k, v, positions, slots, q_out, stream=None) -> None:
+    """aqmb_rotary_append (see KVCache.rotary_append)."""
+    cache.rotary_append(rotary, q, k, v, positions, slots, q_out, stream)
 
 
 def kv_copy_pages(caches, src, dst, stream=None) -> None:
@@ -1030,3 +1100,233 @@ class PagePool:
             self.close()
         except Exception:
             pass
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: RotaryScaling = RotaryScaling.PLAIN, *,
+                       factor: float = 1.0, original_length: int = 0, low: Optional[float] = None,
+                       high: Optional[float] = None):
+    """aqmb_rotary_frequencies: (float64 CPU tensor [rotary_dim / 2] of radians per position, amplitude). low and
+    high default to the kind's usual ones (RAMP: 1 and 32 turns over original_length, TURNS: 1 and 4)."""
+    where = "aqmb_rotary_frequencies"
+    kind = RotaryScaling(scaling)
+    usual = {RotaryScaling.RAMP: (1.0, 32.0), RotaryScaling.TURNS: (1.0, 4.0)}.get(kind, (0.0, 0.0))
+    desc = RotaryScalingDesc(int(kind), original_length, factor, usual[0] if low is None else low,
+                             usual[1] if high is None else high)
+    freq, amplitude = torch.empty((max(rotary_dim // 2, 0),), dtype=torch.float64), ctypes.c_float()
+    _check(lib.aqmb_rotary_frequencies(rotary_dim, base, ctypes.byref(desc), freq.data_ptr() if freq.numel() else None,
+                                       ctypes.byref(amplitude)), where)
+    return freq, amplitude.value
+
+
+def _rotary_tensors(q, q_out, positions, head_dim: Optional[int], where: str):
+    """(tokens, heads, type, strides of q and q_out) of queries [n_tokens][n_heads][head_dim]."""
+    if q.dim() != 3 or (head_dim is not None and q.shape[2] != head_dim):
+        _refuse(where, f"q is {tuple(q.shape)}, not (n_tokens, n_heads, {head_dim or 'head_dim'})")
+    n, heads, dim = q.shape
+    if q_out.shape != q.shape or q_out.dtype != q.dtype:
+        _refuse(where, f"q_out is {tuple(q_out.shape)} of {q_out.dtype}, not {tuple(q.shape)} of {q.dtype}")
+    _dense(positions, torch.int64, n, "positions", where)
+    return (n, heads, _dt8(q, "q", where), KVCache._stride(q, n, heads * dim, "q", where),
+            KVCache._stride(q_out, n, heads * dim, "q_out", where))
+
+
+class Rotary:
+    """Rotary positions with given frequencies (float64 [rotary_dim / 2], radians per position, on the GPU; see
+    rotary_frequencies). layout: "half" pairs values i and i + rotary_dim / 2 of a head, "interleaved" 2 i and 2 i + 1.
+    KVCache.rotary_append turns and writes into a cache at once."""
+
+    _LAYOUTS = {"half": RotaryLayout.HALF, "interleaved": RotaryLayout.INTERLEAVED}
+
+    def __init__(self, frequencies, *, layout: str = "half", amplitude: float = 1.0):
+        where = "Rotary"
+        if layout not in self._LAYOUTS:
+            _refuse(where, f"layout {layout!r} is not 'half' or 'interleaved'")
+        if not frequencies.is_cuda or frequencies.dim() != 1 or not frequencies.numel():
+            _refuse(where, "frequencies must be a vector on a GPU")
+        _dense(frequencies, torch.float64, frequencies.numel(), "frequencies", where)
+        self.frequencies, self.layout, self.amplitude = frequencies, layout, float(amplitude)
+        self.rotary_dim, self.device_index = 2 * frequencies.numel(), frequencies.get_device()
+        both = [RotaryDesc(frequencies.data_ptr(), self.rotary_dim, int(self._LAYOUTS[layout]), self.amplitude, inverse)
+                for inverse in (0, 1)]
+        self.desc, self._inverse = both
+        self._ref, self._inverse_ref = (ctypes.byref(d) for d in both)
+        self._address, self._inverse_address = (ctypes.addressof(d) for d in both)
+
+    @classmethod
+    def scaled(cls, rotary_dim: int, base: float = 10000.0, scaling: RotaryScaling = RotaryScaling.PLAIN, *,
+               layout: str = "half", device="cuda", **kw) -> "Rotary":
+        """With the frequencies and the amplitude of rotary_frequencies (and its arguments)."""
+        freq, amplitude = rotary_frequencies(rotary_dim, base, scaling, **kw)
+        return cls(freq.to(device), layout=layout, amplitude=amplitude)
+
+    def apply(self, q, positions, q_out, k=None, k_out=None, *, inverse: bool = False, stream=None) -> None:
+        """aqmb_rotary: q [n_tokens][n_heads][head_dim] fp16 or bf16 turned by positions int64 [n_tokens] into q_out
+        (may be q), and k into k_out alike. inverse turns back: the gradient of q from that of q_out."""
+        where = "aqmb_rotary"
+        _here(where, q=q, q_out=q_out, k=k, k_out=k_out, positions=positions, frequencies=self.frequencies)
+        n, heads, dt, qs, os_ = _rotary_tensors(q, q_out, positions, None, where)
+        kv, ks, ko, kp, kop = 0, 0, 0, None, None
+        if k is not None:
+            if k.dim() != 3 or k.shape[0] != n or k.shape[2] != q.shape[2] or k.dtype != q.dtype:
+                _refuse(where, f"k is {tuple(k.shape)} of {k.dtype} beside q {tuple(q.shape)} of {q.dtype}")
+            if k_out is None or k_out.shape != k.shape or k_out.dtype != k.dtype:
+                _refuse(where, "k and k_out go together, alike in shape and type")
+            kv = k.shape[1]
+            ks, ko = (KVCache._stride(t, n, kv * k.shape[2], what, where) for t, what in ((k, "k"), (k_out, "k_out")))
+            kp, kop = k.data_ptr(), k_out.data_ptr()
+        elif k_out is not None:
+            _refuse(where, "k and k_out go together, alike in shape and type")
+        st = lib.aqmb_rotary(self._inverse_ref if inverse else self._ref, q.data_ptr(), qs, q_out.data_ptr(), os_, heads, kp,
+                             ks, kop, ko, kv, dt, q.shape[2], positions.data_ptr(), n, _stream(stream))
+        if st:
+            _check(st, where)
+
+
+def rotary(rot: Rotary, q, positions, q_out, k=None, k_out=None, **kw) -> None:
+    """aqmb_rotary (see Rotary.apply)."""
+    rot.apply(q, positions, q_out, k, k_out, **kw)
+
+
+def _workspace(workspace, need: int, device, stream, where: str):
+    """(tensor, bytes) of a call's workspace: the caller's, or one from PyTorch's allocator on the call's stream."""
+    if workspace is not None:
+        _here(where, workspace=workspace)
+        if not workspace.is_contiguous():
+            _refuse(where, "workspace must be dense")
+        return workspace, _nbytes(workspace)
+    if not need:
+        return None, 0
+    if stream is None:
+        return torch.empty((need,), dtype=torch.uint8, device=device), need
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)
+    with torch.cuda.stream(s):             # the allocator ties memory to the stream that is current
+        return torch.empty((need,), dtype=torch.uint8, device=device), need
+
+
+class Adapters:
+    """Low-rank adapters of many requests beside one projection: a [n][rank][d_in] and b [n][d_out][rank] fp16 or bf16,
+    scales [n] fp32 or None (1), ranks [n] int32 or None (all of rank), dense, on one GPU. The tensors stay the
+    caller's; what they hold may change between calls."""
+
+    def __init__(self, a, b, scales=None, ranks=None):
+        where = "Adapters"
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2] or a.dtype != b.dtype:
+            _refuse(where, f"a is {tuple(a.shape)} of {a.dtype} and b {tuple(b.shape)} of {b.dtype}, not [n][rank][d_in] and "
+                           f"[n][d_out][rank]")
+        if 0 in a.shape or 0 in b.shape:
+            _refuse(where, f"an empty stack {tuple(a.shape)}, {tuple(b.shape)}")
+        dt = _TORCH_DT8.get(a.dtype)
+        if dt not in (DType.F16, DType.BF16):
+            _refuse(where, f"a has dtype {a.dtype}", Status.EUNSUPPORTED)
+        n = a.shape[0]
+        _dense(a, a.dtype, a.numel(), "a", where)
+        _dense(b, a.dtype, b.numel(), "b", where)
+        if scales is not None:
+            _dense(scales, torch.float32, n, "scales", where)
+        if ranks is not None:
+            _dense(ranks, torch.int32, n, "ranks", where)
+        if not a.is_cuda or any(t is not None and t.device != a.device for t in (b, scales, ranks)):
+            _refuse(where, "a, b, scales and ranks must be on one GPU")
+        self.a, self.b, self.scales, self.ranks, self.dtype = a, b, scales, ranks, a.dtype
+        self.n_adapters, self.rank, self.d_in, self.d_out = n, a.shape[1], a.shape[2], b.shape[1]
+        self.device_index = a.get_device()
+        self.desc = AdaptersDesc(a.data_ptr(), b.data_ptr(), _ptr(scales), _ptr(ranks), int(dt), n, self.rank, self.d_in,
+                                 self.d_out)
+        self._ref = ctypes.byref(self.desc)
+        self._address = ctypes.addressof(self.desc)
+
+    def workspace_bytes(self, n_rows: int) -> int:
+        """aqmb_adapters_workspace_bytes."""
+        b = ctypes.c_size_t(0)
+        _check(lib.aqmb_adapters_workspace_bytes(self._ref, n_rows, ctypes.byref(b)), "aqmb_adapters_workspace_bytes")
+        return b.value
+
+    def add(self, x, index, base, out, *, workspace=None, stream=None) -> None:
+        """aqmb_adapters_add: out = base + scale * B A x for the rows of x [n_rows][d_in], each with the adapter
+        that index int32 [n_rows] names (-1: none; on the GPU). base and out (may be base): [n_rows][d_out] fp16, bf16 or
+        fp32, what the projection gave. Without a workspace one is taken from PyTorch's allocator."""
+        where = "aqmb_adapters_add"
+        dev = _current_device()
+        if dev != self.device_index:
+            _refuse(where, f"the adapters are on device {self.device_index}, device {dev} is current")
+        _here(where, x=x, index=index, base=base, out=out)
+        if x.dim() != 2 or x.dtype != self.dtype:
+            _refuse(where, f"x is {tuple(x.shape)} of {x.dtype}, not (n_rows, {self.d_in}) of {self.dtype}")
+        n, ydt = x.shape[0], _TORCH_DT.get(base.dtype)
+        if ydt is None or out.dtype != base.dtype:
+            _refuse(where, f"base of {base.dtype}, out of {out.dtype}", Status.EUNSUPPORTED)
+        xs = _rows(x, n, self.d_in, "x", where)
+        bs, os_ = _rows(base, n, self.d_out, "base", where), _rows(out, n, self.d_out, "out", where)
+        _dense(index, torch.int32, n, "index", where)
+        ws, wb = _workspace(workspace, self.workspace_bytes(n), x.device, stream, where)
+        st = lib.aqmb_adapters_add(self._ref, x.data_ptr(), xs, index.data_ptr(), n, base.data_ptr(), bs, out.data_ptr(), os_,
+                                   ydt, _ptr(ws), wb, _stream(stream))
+        if st:
+            _check(st, where)
+
+
+def adapters_add(adapters: Adapters, x, index, base, out, **kw) -> None:
+    """aqmb_adapters_add (see Adapters.add)."""
+    adapters.add(x, index, base, out, **kw)
+
+
+def adapters_workspace_bytes(adapters: Adapters, n_rows: int) -> int:
+    return adapters.workspace_bytes(n_rows)
+
+
+def log_probs_workspace_bytes(dtype, rows: int, vocab: int, n_top: int = 0) -> int:
+    """aqmb_log_probs_workspace_bytes; dtype: of the logits, a torch dtype or a DType."""
+    dt = _TORCH_DT.get(dtype)
+    b = ctypes.c_size_t(0)
+    _check(lib.aqmb_log_probs_workspace_bytes(int(dtype) if dt is None else dt, rows, vocab, n_top, ctypes.byref(b)),
+           "aqmb_log_probs_workspace_bytes")
+    return b.value
+
+
+def log_probs(logits, targets=None, logprobs=None, *, scale: float = 1.0, lse=None, entropy=None, top_ids=None,
+              top_logprobs=None, workspace=None, stream=None) -> None:
+    """aqmb_log_probs: of the rows of scale * logits [rows][vocab] fp16, bf16 or fp32: logprobs fp32 [rows][n] of targets
+    int64 [rows][n] (or both [rows]; a negative one gets 0), lse and entropy fp32 [rows], and top_ids int64,
+    top_logprobs fp32 [rows][n_top] in descending order. Every output may be left out, not all."""
+    where = "aqmb_log_probs"
+    if logits.dim() != 2:
+        _refuse(where, f"logits are {tuple(logits.shape)}, not (rows, vocab)")
+    _here(where, logits=logits, targets=targets, logprobs=logprobs, lse=lse, entropy=entropy, top_ids=top_ids,
+          top_logprobs=top_logprobs)
+    rows, vocab = logits.shape
+    dt = _TORCH_DT.get(logits.dtype)
+    if dt is None:
+        _refuse(where, f"logits of {logits.dtype}", Status.EUNSUPPORTED)
+    if not rows or not vocab:
+        _refuse(where, f"logits are {tuple(logits.shape)}")
+    stride = _rows(logits, rows, vocab, "logits", where)
+
+    def per_row(t, what):
+        if t.dim() not in (1, 2) or t.shape[0] != rows:
+            _refuse(where, f"{what} is {tuple(t.shape)}, not ({rows}, n)")
+        return t.numel() // rows
+
+    n = 0
+    if (targets is None) != (logprobs is None):
+        _refuse(where, "targets and logprobs go together")
+    if targets is not None:
+        n = per_row(targets, "targets")
+        _dense(targets, torch.int64, rows * n, "targets", where)
+        _dense(logprobs, torch.float32, rows * n, "logprobs", where)
+    for what, t in (("lse", lse), ("entropy", entropy)):
+        if t is not None:
+            _dense(t, torch.float32, rows, what, where)
+    top = 0
+    for what, t, dtype in (("top_ids", top_ids, torch.int64), ("top_logprobs", top_logprobs, torch.float32)):
+        if t is not None:
+            k = per_row(t, what)
+            if top and k != top:
+                _refuse(where, f"top_ids and top_logprobs are of {top} and {k} values a row")
+            top = k
+            _dense(t, dtype, rows * top, what, where)
+    ws, wb = _workspace(workspace, log_probs_workspace_bytes(dt, rows, vocab, top), logits.device, stream, where)
+    st = lib.aqmb_log_probs(logits.data_ptr(), dt, stride, rows, vocab, scale, _ptr(targets) if n else None, n,
+                            _ptr(logprobs) if n else None, _ptr(lse), _ptr(entropy), _ptr(top_ids) if top else None,
+                            _ptr(top_logprobs) if top else None, top, _ptr(ws), wb, _stream(stream))
+    if st:
+        _check(st, where)

@@ -28,7 +28,7 @@ CEIL_LIB = os.path.join(HERE, "libaqmb_ceilings.so")
 DIRECT_LIB = os.path.join(HERE, "_direct.so")
 
 SOURCES = ["validate.cpp", "api.cpp", "k_dequant.hip", "k_gemv.hip", "k_gemv16.hip", "k_gemv4.hip", "k_gemv_mma.hip", "k_gemm.hip", "k_gemm_small.hip", "k_gemm_mid.hip", "k_distortion.hip", "k_beam.hip", "k_beam_mma.hip", "ops_api.cpp", "pages.cpp",
-           "k_norm.hip", "k_w4.hip", "k_attn.hip", "k_kv.hip"]
+           "k_norm.hip", "k_w4.hip", "k_attn.hip", "k_kv.hip", "k_rotary.hip", "k_adapters.hip", "k_logprobs.hip"]
 ARCH = "gfx950"
 
 

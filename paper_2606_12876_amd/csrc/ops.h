@@ -73,4 +73,54 @@ hipError_t launch_kv_append(const aqmb_kv_cache& c, const void* k, int64_t k_str
 hipError_t launch_kv_copy(const aqmb_kv_cache* caches, int n_caches, const int32_t* src, const int32_t* dst, int n_pairs,
                           hipStream_t st);
 
+struct RotaryArgs {
+  aqmb_rotary_desc rot;
+  const void* q;
+  void* q_out;
+  const void* k;
+  void* k_out;             // without a cache
+  const void* v;           // with one
+  int64_t q_stride, q_out_stride, k_stride, k_out_stride, v_stride;
+  const int64_t* positions;
+  const int64_t* slots;    // null: no cache
+  aqmb_kv_cache cache;
+  int n_heads, n_kv, head_dim, n_tokens;
+};
+hipError_t launch_rotary(const RotaryArgs& a, aqmb_dtype dtype, hipStream_t st);
+
+struct AdapterArgs {
+  aqmb_adapters ad;
+  const void* x;
+  const int* index;
+  const void* base;
+  void* out;
+  int64_t x_stride, base_stride, out_stride;
+  float* t;                // [splits][n_rows][t_stride]: A x, partial sums over parts of the inputs
+  int n_rows, t_stride, splits, per_wave;
+};
+// How a call is cut: `few` rows (one wave's votes sort them) by tile, else by 64 rows; tiles: an upper bound of the
+// tiles of few rows; per_wave: outputs of a wave in the second launch.
+struct AdapterPlan { bool few; int tiles, splits, per_wave, t_stride; size_t bytes; };
+AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows);
+hipError_t launch_adapters(AdapterArgs a, const AdapterPlan& p, aqmb_dtype y, hipStream_t st);
+
+struct LogProbArgs {
+  const void* logits;
+  int64_t stride;
+  float scale;
+  const int64_t* targets;
+  float* logprobs;
+  float* lse;
+  float* entropy;
+  int64_t* top_ids;
+  float* top_logprobs;
+  int rows, vocab, n_targets, n_top;
+  int chunk, splits;       // values per workgroup, workgroups along a row
+  float4* stats;           // splits > 1: [rows][splits] (largest, sum, weighted sum), and the largest values' keys
+  uint64_t* keys;          // [rows][splits][n_top]
+};
+struct LogProbPlan { int chunk, splits; size_t bytes; };
+LogProbPlan log_prob_plan(aqmb_dtype dtype, int rows, int vocab, int n_top);
+hipError_t launch_log_probs(const LogProbArgs& a, aqmb_dtype dtype, hipStream_t st);
+
 }  // namespace aqmb

@@ -87,6 +87,61 @@ static aqmb_status check_attention(const aqmb_kv_cache* c, int n_heads, int n_se
   return AQMB_OK;
 }
 
+static aqmb_status check_rotary(const aqmb_rotary_desc* r, const void* q, int64_t q_stride, const void* q_out,
+                                int64_t q_out_stride, int n_heads, int n_kv, int64_t n_total, int dtype, int head_dim,
+                                const int64_t* positions, int n_tokens, const char* where) {
+  if (!r) return fail(AQMB_EINVAL, "%s: rotary is NULL", where);
+  if (!is16(dtype)) return fail(AQMB_EUNSUPPORTED, "%s: dtype %d is not F16 or BF16", where, dtype);
+  if (n_heads < 1 || n_kv < 0 || head_dim < 1 || n_tokens < 1)
+    return fail(AQMB_EINVAL, "%s: n_heads, head_dim and n_tokens must be >= 1", where);
+  if (head_dim % 8 || head_dim > 256)
+    return fail(AQMB_EUNSUPPORTED, "%s: head_dim = %d is not a multiple of 8 up to 256", where, head_dim);
+  if (r->layout != AQMB_ROTARY_HALF && r->layout != AQMB_ROTARY_INTERLEAVED)
+    return fail(AQMB_EINVAL, "%s: unknown layout %d", where, r->layout);
+  if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > head_dim)
+    return fail(AQMB_EINVAL, "%s: rotary_dim = %d is odd or outside [2, %d]", where, r->rotary_dim, head_dim);
+  if (!std::isfinite(r->amplitude)) return fail(AQMB_EINVAL, "%s: amplitude is not finite", where);
+  if (r->inverse != 0 && r->inverse != 1) return fail(AQMB_EINVAL, "%s: inverse = %d is not 0 or 1", where, r->inverse);
+  if (!r->frequencies || !q || !q_out || !positions)
+    return fail(AQMB_EINVAL, "%s: frequencies, q, q_out or positions is NULL", where);
+  const int64_t row = (int64_t)n_heads * head_dim;
+  if (q_stride < row || q_out_stride < row) return fail(AQMB_EINVAL, "%s: a stride of q or q_out is below a token", where);
+  if (q == q_out && q_stride != q_out_stride) return fail(AQMB_EINVAL, "%s: in place with another stride", where);
+  if (!aligned(r->frequencies, 8) || !aligned(q, 2) || !aligned(q_out, 2) || !aligned(positions, 8))
+    return fail(AQMB_EINVAL, "%s: a pointer is not aligned to its elements", where);
+  if (n_heads > 65535 || n_kv > 65535) return fail(AQMB_EUNSUPPORTED, "%s: more than 65535 heads", where);
+  // 256 threads own at least 8 heads at once: fewer than 2^24 workgroups.
+  if ((n_total + 7) / 8 * n_tokens >= (int64_t)1 << 24)
+    return fail(AQMB_EUNSUPPORTED, "%s: n_tokens = %d of %d heads are more than one launch takes", where, n_tokens, (int)n_total);
+  return AQMB_OK;
+}
+
+static aqmb_status check_adapters(const aqmb_adapters* a, int n_rows, const char* where) {
+  if (!a) return fail(AQMB_EINVAL, "%s: adapters is NULL", where);
+  if (!is16(a->dtype)) return fail(AQMB_EUNSUPPORTED, "%s: dtype %d is not F16 or BF16", where, a->dtype);
+  if (a->n_adapters < 1 || a->rank < 1 || a->d_in < 1 || a->d_out < 1 || n_rows < 1)
+    return fail(AQMB_EINVAL, "%s: n_adapters, rank, d_in, d_out and n_rows must be >= 1", where);
+  if (a->rank > AQMB_MAX_RANK) return fail(AQMB_EUNSUPPORTED, "%s: rank = %d above %d", where, a->rank, AQMB_MAX_RANK);
+  if (a->n_adapters > 1 << 24 || a->d_in > 1 << 24 || a->d_out > 1 << 24)
+    return fail(AQMB_EUNSUPPORTED, "%s: n_adapters, d_in or d_out above 2^24", where);
+  if (n_rows > (1 << 22) - 64) return fail(AQMB_EUNSUPPORTED, "%s: n_rows = %d above 2^22 - 64", where, n_rows);
+  if (((int64_t)n_rows + 63) / 64 * (((int64_t)a->d_out + 255) / 256) >= 1 << 23)
+    return fail(AQMB_EUNSUPPORTED, "%s: n_rows = %d of d_out = %d are more than one launch takes", where, n_rows, a->d_out);
+  if (!a->a || !a->b) return fail(AQMB_EINVAL, "%s: a or b is NULL", where);
+  if (!aligned(a->a, 2) || !aligned(a->b, 2) || !aligned(a->scales, 4) || !aligned(a->ranks, 4))
+    return fail(AQMB_EINVAL, "%s: a pointer is not aligned to its elements", where);
+  return AQMB_OK;
+}
+
+static aqmb_status check_log_probs(int dtype, int rows, int vocab, int n_top, const char* where) {
+  if (!is16(dtype) && dtype != AQMB_F32) return fail(AQMB_EUNSUPPORTED, "%s: dtype %d is not F16, BF16 or F32", where, dtype);
+  if (rows < 1 || vocab < 1) return fail(AQMB_EINVAL, "%s: rows = %d and vocab = %d must be >= 1", where, rows, vocab);
+  if (n_top < 0 || n_top > vocab) return fail(AQMB_EINVAL, "%s: n_top = %d outside [0, %d]", where, n_top, vocab);
+  if (n_top > AQMB_MAX_TOP) return fail(AQMB_EUNSUPPORTED, "%s: n_top = %d above %d", where, n_top, AQMB_MAX_TOP);
+  if (rows > 1 << 22) return fail(AQMB_EUNSUPPORTED, "%s: rows = %d above 2^22", where, rows);
+  return AQMB_OK;
+}
+
 // Compute units of the current device, asked of the runtime once per device.
 static hipError_t compute_units(int* n) {
   static std::mutex mu;
@@ -360,6 +415,209 @@ aqmb_status aqmb_kv_copy_pages(const aqmb_kv_cache* caches, int n_caches, const 
   }
   if (!aligned(src, 4) || !aligned(dst, 4)) return fail(AQMB_EINVAL, "kv_copy_pages: a misaligned pointer");
   return hip_status(launch_kv_copy(caches, n_caches, src, dst, n_pairs, (hipStream_t)stream), "kv_copy_pages: launch");
+}
+
+aqmb_status aqmb_rotary_frequencies(int rotary_dim, double base, const aqmb_rotary_scaling* scaling, double* frequencies,
+                                    float* amplitude) {
+  clear_error();
+  const char* where = "rotary_frequencies";
+  const int kind = scaling ? scaling->kind : (int)AQMB_ROTARY_PLAIN;
+  if (kind < AQMB_ROTARY_PLAIN || kind > AQMB_ROTARY_TURNS) return fail(AQMB_EUNSUPPORTED, "%s: unknown kind %d", where, kind);
+  if (rotary_dim < 2 || rotary_dim % 2) return fail(AQMB_EINVAL, "%s: rotary_dim = %d is odd or below 2", where, rotary_dim);
+  if (!std::isfinite(base) || base <= 1.0) return fail(AQMB_EINVAL, "%s: base must be finite and above 1", where);
+  const bool parts = kind == AQMB_ROTARY_RAMP || kind == AQMB_ROTARY_TURNS;
+  const double factor = kind == AQMB_ROTARY_PLAIN ? 1.0 : scaling->factor;
+  if (!std::isfinite(factor) || factor < 1.0) return fail(AQMB_EINVAL, "%s: factor must be finite and >= 1", where);
+  if (parts && (scaling->original_length < 1 || !(scaling->low > 0.0) || !(scaling->high > scaling->low) ||
+                !std::isfinite(scaling->high)))
+    return fail(AQMB_EINVAL, "%s: original_length must be >= 1 and 0 < low < high", where);
+  const double two_pi = 6.283185307179586, dim = rotary_dim;
+  if (kind == AQMB_ROTARY_BASE && rotary_dim > 2) base *= std::pow(factor, dim / (dim - 2.0));
+  double lo = 0.0, hi = 0.0;
+  if (kind == AQMB_ROTARY_RAMP) {
+    const auto index = [&](double turns) {
+      return dim / 2.0 * std::log(scaling->original_length / (two_pi * turns)) / std::log(base);
+    };
+    lo = std::fmax(std::floor(index(scaling->high)), 0.0);
+    hi = std::fmin(std::ceil(index(scaling->low)), dim - 1.0);
+  }
+  for (int i = 0; frequencies && i < rotary_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / dim);
+    double t = 0.0;            // how far towards f / factor
+    if (kind == AQMB_ROTARY_LINEAR) t = 1.0;
+    if (kind == AQMB_ROTARY_RAMP) t = (i - lo) / std::fmax(hi - lo, 0.001);
+    if (kind == AQMB_ROTARY_TURNS)
+      t = 1.0 - (scaling->original_length * f / two_pi - scaling->low) / (scaling->high - scaling->low);
+    t = std::fmin(std::fmax(t, 0.0), 1.0);
+    frequencies[i] = f * (1.0 - t) + f / factor * t;
+  }
+  if (amplitude) *amplitude = kind == AQMB_ROTARY_RAMP ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return AQMB_OK;
+}
+
+aqmb_status aqmb_rotary(const aqmb_rotary_desc* rotary, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                        int n_heads, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, int n_kv_heads,
+                        aqmb_dtype dtype, int head_dim, const int64_t* positions, int n_tokens, aqmb_stream_t stream) {
+  clear_error();
+  const char* where = "rotary";
+  const aqmb_status s = check_rotary(rotary, q, q_stride, q_out, q_out_stride, n_heads, n_kv_heads, (int64_t)n_heads + n_kv_heads,
+                                     dtype, head_dim, positions, n_tokens, where);
+  if (s != AQMB_OK) return s;
+  if (!k != !k_out || !k != (n_kv_heads == 0)) return fail(AQMB_EINVAL, "%s: k, k_out and n_kv_heads go together", where);
+  if (k) {
+    const int64_t row = (int64_t)n_kv_heads * head_dim;
+    if (k_stride < row || k_out_stride < row) return fail(AQMB_EINVAL, "%s: a stride of k or k_out is below a token", where);
+    if (k == k_out && k_stride != k_out_stride) return fail(AQMB_EINVAL, "%s: in place with another stride", where);
+    if (!aligned(k, 2) || !aligned(k_out, 2)) return fail(AQMB_EINVAL, "%s: k or k_out is not aligned to its elements", where);
+  }
+  RotaryArgs a = {};
+  a.rot = *rotary;
+  a.q = q;
+  a.q_out = q_out;
+  a.k = k;
+  a.k_out = k_out;
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_stride = k_stride;
+  a.k_out_stride = k_out_stride;
+  a.positions = positions;
+  a.n_heads = n_heads;
+  a.n_kv = n_kv_heads;
+  a.head_dim = head_dim;
+  a.n_tokens = n_tokens;
+  return hip_status(launch_rotary(a, dtype, (hipStream_t)stream), "rotary: launch");
+}
+
+aqmb_status aqmb_rotary_append(const aqmb_kv_cache* cache, const aqmb_rotary_desc* rotary, const void* q, int64_t q_stride,
+                               void* q_out, int64_t q_out_stride, int n_heads, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, aqmb_dtype dtype, const int64_t* positions,
+                               const int64_t* slots, int n_tokens, aqmb_stream_t stream) {
+  clear_error();
+  const char* where = "rotary_append";
+  aqmb_status s = check_cache(cache, where);
+  if (s != AQMB_OK || (s = check_beside(cache, dtype, where)) != AQMB_OK) return s;
+  const int kv = cache->n_kv_heads;
+  s = check_rotary(rotary, q, q_stride, q_out, q_out_stride, n_heads, kv, (int64_t)n_heads + 2 * kv, dtype, cache->head_dim,
+                   positions, n_tokens, where);
+  if (s != AQMB_OK) return s;
+  if (!k || !v || !slots) return fail(AQMB_EINVAL, "%s: k, v or slots is NULL", where);
+  const int64_t row = (int64_t)kv * cache->head_dim;
+  if (k_stride < row || v_stride < row) return fail(AQMB_EINVAL, "%s: a stride of k or v is below a token", where);
+  if (!aligned(k, 2) || !aligned(v, 2) || !aligned(slots, 8)) return fail(AQMB_EINVAL, "%s: a misaligned pointer", where);
+  RotaryArgs a = {};
+  a.rot = *rotary;
+  a.q = q;
+  a.q_out = q_out;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.positions = positions;
+  a.slots = slots;
+  a.cache = *cache;
+  a.n_heads = n_heads;
+  a.n_kv = kv;
+  a.head_dim = cache->head_dim;
+  a.n_tokens = n_tokens;
+  return hip_status(launch_rotary(a, dtype, (hipStream_t)stream), "rotary_append: launch");
+}
+
+aqmb_status aqmb_adapters_workspace_bytes(const aqmb_adapters* adapters, int n_rows, size_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(AQMB_EINVAL, "adapters_workspace_bytes: bytes is NULL");
+  const aqmb_status s = check_adapters(adapters, n_rows, "adapters_workspace_bytes");
+  if (s != AQMB_OK) return s;
+  *bytes = adapter_plan(*adapters, n_rows).bytes;
+  return AQMB_OK;
+}
+
+aqmb_status aqmb_adapters_add(const aqmb_adapters* adapters, const void* x, int64_t x_stride, const int32_t* index,
+                              int n_rows, const void* base, int64_t base_stride, void* out, int64_t out_stride,
+                              aqmb_dtype y_dtype, void* workspace, size_t workspace_bytes, aqmb_stream_t stream) {
+  clear_error();
+  const char* where = "adapters_add";
+  const aqmb_status s = check_adapters(adapters, n_rows, where);
+  if (s != AQMB_OK) return s;
+  if (!is16(y_dtype) && y_dtype != AQMB_F32)
+    return fail(AQMB_EUNSUPPORTED, "%s: y dtype %d is not F16, BF16 or F32", where, (int)y_dtype);
+  if (!x || !index || !base || !out) return fail(AQMB_EINVAL, "%s: x, index, base or out is NULL", where);
+  if (x_stride < adapters->d_in || base_stride < adapters->d_out || out_stride < adapters->d_out)
+    return fail(AQMB_EINVAL, "%s: a row stride is below the row", where);
+  if (base == out && base_stride != out_stride) return fail(AQMB_EINVAL, "%s: in place with another stride", where);
+  if (!aligned(x, 2) || !aligned(index, 4) || !aligned(base, elem(y_dtype)) || !aligned(out, elem(y_dtype)))
+    return fail(AQMB_EINVAL, "%s: a pointer is not aligned to its elements", where);
+  const AdapterPlan plan = adapter_plan(*adapters, n_rows);
+  if (plan.bytes && (!workspace || workspace_bytes < plan.bytes))
+    return fail(AQMB_EINVAL, "%s: workspace of %zu bytes, %zu needed", where, workspace ? workspace_bytes : (size_t)0, plan.bytes);
+  if (plan.bytes && !aligned(workspace, 16)) return fail(AQMB_EINVAL, "%s: workspace must be 16-byte aligned", where);
+  AdapterArgs a = {};
+  a.ad = *adapters;
+  a.x = x;
+  a.index = index;
+  a.base = base;
+  a.out = out;
+  a.x_stride = x_stride;
+  a.base_stride = base_stride;
+  a.out_stride = out_stride;
+  a.t = (float*)workspace;
+  a.n_rows = n_rows;
+  return hip_status(launch_adapters(a, plan, y_dtype, (hipStream_t)stream), "adapters_add: launch");
+}
+
+aqmb_status aqmb_log_probs_workspace_bytes(aqmb_dtype dtype, int rows, int vocab, int n_top, size_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(AQMB_EINVAL, "log_probs_workspace_bytes: bytes is NULL");
+  const aqmb_status s = check_log_probs(dtype, rows, vocab, n_top, "log_probs_workspace_bytes");
+  if (s != AQMB_OK) return s;
+  *bytes = log_prob_plan(dtype, rows, vocab, n_top).bytes;
+  return AQMB_OK;
+}
+
+aqmb_status aqmb_log_probs(const void* logits, aqmb_dtype dtype, int64_t stride, int rows, int vocab, float scale,
+                           const int64_t* targets, int n_targets, float* logprobs, float* lse, float* entropy,
+                           int64_t* top_ids, float* top_logprobs, int n_top, void* workspace, size_t workspace_bytes,
+                           aqmb_stream_t stream) {
+  clear_error();
+  const char* where = "log_probs";
+  const aqmb_status s = check_log_probs(dtype, rows, vocab, n_top, where);
+  if (s != AQMB_OK) return s;
+  if (!logits) return fail(AQMB_EINVAL, "%s: logits is NULL", where);
+  if (stride < vocab) return fail(AQMB_EINVAL, "%s: stride is below vocab = %d", where, vocab);
+  // Below, what overflows a difference of two logits would still have a weight.
+  if (!std::isfinite(scale) || scale < 0x1p-120f) return fail(AQMB_EINVAL, "%s: scale must be finite and >= 2^-120", where);
+  if (n_targets < 0) return fail(AQMB_EINVAL, "%s: n_targets = %d is negative", where, n_targets);
+  if (!targets != (n_targets == 0) || !targets != !logprobs)
+    return fail(AQMB_EINVAL, "%s: targets, logprobs and n_targets go together", where);
+  if ((top_ids || top_logprobs) != (n_top > 0)) return fail(AQMB_EINVAL, "%s: n_top and its outputs go together", where);
+  if (!logprobs && !lse && !entropy && !n_top) return fail(AQMB_EINVAL, "%s: no output is asked for", where);
+  if (!aligned(logits, elem(dtype)) || !aligned(targets, 8) || !aligned(logprobs, 4) || !aligned(lse, 4) ||
+      !aligned(entropy, 4) || !aligned(top_ids, 8) || !aligned(top_logprobs, 4))
+    return fail(AQMB_EINVAL, "%s: a pointer is not aligned to its elements", where);
+  const LogProbPlan plan = log_prob_plan(dtype, rows, vocab, n_top);
+  if (plan.bytes && (!workspace || workspace_bytes < plan.bytes))
+    return fail(AQMB_EINVAL, "%s: workspace of %zu bytes, %zu needed", where, workspace ? workspace_bytes : (size_t)0, plan.bytes);
+  if (plan.bytes && !aligned(workspace, 16)) return fail(AQMB_EINVAL, "%s: workspace must be 16-byte aligned", where);
+  LogProbArgs a = {};
+  a.logits = logits;
+  a.stride = stride;
+  a.scale = scale;
+  a.targets = targets;
+  a.logprobs = logprobs;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.top_ids = top_ids;
+  a.top_logprobs = top_logprobs;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.n_targets = n_targets;
+  a.n_top = n_top;
+  a.chunk = plan.chunk;
+  a.splits = plan.splits;
+  a.stats = (float4*)workspace;
+  a.keys = (uint64_t*)((char*)workspace + (size_t)rows * plan.splits * 16);
+  return hip_status(launch_log_probs(a, dtype, (hipStream_t)stream), "log_probs: launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,201 @@
+"""Low-rank adapters of many requests against the oracle in 64 bits (GPU).
+
+Tolerance of out = base + s B t, t = A x, u = 2^-24: t is a sum of d_in products in matrix instructions of 32 inputs: as many
+additions in a row as steps, 32 within one, 32 partial sums at most, each by 2 u of what is summed (an addition may
+truncate): et = 2 u (d_in / 32 + 64) |A| |x|, and u |t| for the scale. The parts of s t stand for it to 2^-24 (bf16: three of
+8 bits) or 2^-22 of the row's largest (fp16: two of 11, one bit of slack for a power of two). The second sum has
+3 rank / 32 + 32 additions. Then base's addition and half a step of the output's type."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2606_12876_amd as A  # noqa: E402
+from ops_helpers import U, gen, half_ulp, normal, values  # noqa: E402
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def make(g, n, rank, d_in, d_out, dtype, ranks=None, std=1.0):
+    a = normal(g, n, rank, d_in, dtype=dtype, std=std * d_in ** -0.5)
+    b = normal(g, n, d_out, rank, dtype=dtype, std=rank ** -0.5)
+    s = 0.5 + torch.rand((n,), generator=g, device="cuda")
+    if ranks is not None:                         # what lies behind an adapter's rank may hold anything
+        for i, r in enumerate(ranks):
+            a[i, max(r, 0):], b[i, :, max(r, 0):] = float("nan"), float("nan")
+        ranks = torch.tensor(ranks, dtype=torch.int32, device="cuda")
+    return A.Adapters(a, b, s, ranks)
+
+
+def check(ad, x, index, base, out):
+    a, b, s = np.nan_to_num(values(ad.a)), np.nan_to_num(values(ad.b)), values(ad.scales) if ad.scales is not None else np.ones(ad.n_adapters)
+    idx = index.cpu().numpy()
+    ranks = np.full(ad.n_adapters, ad.rank) if ad.ranks is None else ad.ranks.cpu().numpy()
+    xv, bv = values(x), values(base)
+    want = bv + decode.adapted(xv, idx, a, b, s, ranks)
+    e = np.zeros_like(want)
+    for i, n in enumerate(idx):
+        if not 0 <= n < ad.n_adapters:
+            continue
+        r = min(max(int(ranks[n]), 0), ad.rank)
+        an, bn = a[n, :r], np.abs(b[n, :, :r])
+        if r == 0:
+            continue
+        t = np.abs(s[n] * (an @ xv[i]))
+        et = s[n] * 2 * U * (ad.d_in / 32 + 64) * (np.abs(an) @ np.abs(xv[i])) + U * t
+        et = et + (2.0 ** -24 * t if ad.dtype == BF16 else 2.0 ** -22 * (t + et).max())
+        e[i] = bn @ et + 2 * U * (3 * r / 32 + 33) * (bn @ (t + et))
+    e = e + 2 * U * (np.abs(want) + e)
+    same = np.array([not 0 <= n < ad.n_adapters for n in idx])
+    assert torch.equal(out[torch.tensor(same, device="cuda")], base[torch.tensor(same, device="cuda")])
+    off = np.abs(values(out) - want) - (e + half_ulp(np.abs(want) + e, out.dtype))
+    assert np.all(off <= 0), (off.max(), np.argwhere(off > 0)[:5])
+
+
+def index_of(g, n_rows, n, spans):
+    if spans:
+        i = torch.sort(torch.randint(-1, n, (n_rows,), generator=g, device="cuda")).values
+        return i[torch.arange(n_rows, device="cuda").roll(n_rows // 3)].to(torch.int32)
+    return torch.randint(-1, n, (n_rows,), generator=g, device="cuda").to(torch.int32)
+
+
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F16, F16), (BF16, F32), (F16, BF16), (BF16, F16), (F16, F32)])
+@pytest.mark.parametrize("rows,n,rank,d_in,d_out,spans", [
+    (1, 1, 16, 512, 512, False), (1, 3, 8, 8, 8, False), (2, 4, 1, 1, 1, False), (16, 20, 16, 264, 136, False), (33, 7, 20, 257, 131, False),
+    (64, 64, 64, 520, 300, False), (63, 2, 33, 1000, 65, True), (65, 3, 128, 96, 64, True), (200, 70, 12, 100, 77, False),
+    (300, 4, 256, 40, 333, True), (17, 2, 5, 7, 63, True), (129, 1, 32, 320, 257, False), (1000, 5, 40, 72, 48, True)])
+def test_adapters(rows, n, rank, d_in, d_out, spans, dtype, out):
+    g = gen(rows + rank + d_in)
+    ad = make(g, n, rank, d_in, d_out, dtype)
+    x = normal(g, rows, d_in, dtype=dtype)
+    index, base = index_of(g, rows, n, spans), normal(g, rows, d_out, dtype=out)
+    y = torch.full_like(base, 7.0)
+    ad.add(x, index, base, y)
+    check(ad, x, index, base, y)
+    z = base.clone()                                                   # in place
+    A.adapters_add(ad, x, index, z, z)
+    assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [1, 40, 100])
+@pytest.mark.parametrize("rank,ranks", [(16, [16, 1, 0, 9]), (64, [64, 8, 33, 32, -3, 17, 100]), (24, [24, 5, 12]), (200, [200, 31, 129, 64])])
+def test_mixed_ranks(rank, ranks, rows, dtype):
+    g = gen(rank + rows)
+    ad = make(g, len(ranks), rank, 200, 150, dtype, ranks)
+    x, base = normal(g, rows, 200, dtype=dtype), normal(g, rows, 150, dtype=dtype)
+    index = (torch.arange(rows, device="cuda") % len(ranks)).to(torch.int32)
+    out = torch.empty_like(base)
+    ad.add(x, index, base, out)
+    check(ad, x, index, base, out)
+
+
+@pytest.mark.parametrize("rows", [3, 90])
+def test_strides_no_scales_and_foreign_indexes(rows):
+    """Rows of a wider tensor, unaligned; what lies between them stays; indexes outside the stack mean none."""
+    g = gen(rows)
+    ad = make(g, 3, 16, 133, 99, BF16)
+    ad = A.Adapters(ad.a, ad.b)
+    x = normal(g, rows, 140, dtype=BF16)[:, 3:136]
+    wide = normal(g, rows, 120, dtype=BF16)
+    base, kept = wide[:, 5:104], wide.clone()
+    index = torch.tensor([0, 3, -7, 2 ** 31 - 1, -2 ** 31, 2, 1], device="cuda").to(torch.int32).repeat(rows)[:rows].contiguous()
+    before = base.clone()
+    ad.add(x, index, base, base)
+    check(ad, x, index, before, base.contiguous())
+    assert torch.equal(wide[:, :5], kept[:, :5]) and torch.equal(wide[:, 104:], kept[:, 104:])
+
+
+def test_no_row_has_an_adapter():
+    g = gen(3)
+    ad = make(g, 2, 8, 64, 70, F16)
+    for rows in (1, 20, 100):
+        x, base = normal(g, rows, 64, dtype=F16), normal(g, rows, 70, dtype=F16)
+        out = torch.zeros_like(base)
+        ad.add(x, torch.full((rows,), -1, dtype=torch.int32, device="cuda"), base, out)
+        assert torch.equal(out, base)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [20, 80])
+def test_rows_do_not_touch_each_other(rows, dtype):
+    """NaN and infinity in one row's x, in another adapter's weights, in rows without an adapter: only theirs."""
+    g = gen(rows)
+    ad = make(g, 3, 16, 96, 80, dtype)
+    x, base = normal(g, rows, 96, dtype=dtype), normal(g, rows, 80, dtype=dtype)
+    index = (torch.arange(rows, device="cuda") % 3).to(torch.int32)
+    index[7] = -1
+    clean, out = torch.empty_like(base), torch.empty_like(base)
+    ad.add(x, index, base, clean)
+    x[3, 50], x[7, 1] = float("nan"), float("inf")
+    ad.a[1, 2, 3] = float("inf")
+    ad.add(x, index, base, out)
+    bad = (torch.arange(rows, device="cuda") % 3 == 1) & (index >= 0)
+    bad[3] = True
+    assert torch.equal(out[~bad], clean[~bad])
+    assert not out[bad].isfinite().any()
+
+
+def test_large_and_small_values_fp16():
+    """A x far outside fp16's range, which its scale brings back; and far below it."""
+    g = gen(11)
+    for std, s in ((300.0, 2.0 ** -12), (2.0 ** -12, 2.0 ** 10)):
+        ad = make(g, 2, 24, 512, 100, F16, std=std)
+        ad = A.Adapters(ad.a, ad.b, torch.full((2,), s, device="cuda"))
+        x = normal(g, 9, 512, dtype=F16, std=500.0 if std > 1 else 2.0 ** -10)
+        index = (torch.arange(9, device="cuda") % 2).to(torch.int32)
+        base = torch.zeros((9, 100), dtype=F32, device="cuda")
+        out = torch.empty_like(base)
+        ad.add(x, index, base, out)
+        check(ad, x, index, base, out)
+        assert out.isfinite().all() and out.any()
+
+
+def test_a_row_does_not_depend_on_the_others():
+    g = gen(13)
+    for rows in (30, 150):
+        ad = make(g, 6, 32, 300, 200, BF16)
+        x, base = normal(g, rows, 300, dtype=BF16), normal(g, rows, 200, dtype=BF16)
+        index = torch.randint(-1, 6, (rows,), generator=g, device="cuda").to(torch.int32)
+        out, again = torch.empty_like(base), torch.empty_like(base)
+        ad.add(x, index, base, out)
+        order = torch.randperm(rows, generator=g, device="cuda")
+        ad.add(x[order], index[order], base[order], again)
+        assert torch.equal(again, out[order])
+
+
+def test_a_wide_layer_and_a_given_workspace():
+    g = gen(17)
+    ad = make(g, 4, 16, 4096, 11008, BF16)
+    for rows in (2, 70):
+        x, base = normal(g, rows, 4096, dtype=BF16), normal(g, rows, 11008, dtype=BF16)
+        index = torch.randint(0, 4, (rows,), generator=g, device="cuda").to(torch.int32)
+        ws = torch.full((A.adapters_workspace_bytes(ad, rows) + 64,), 255, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(base)
+        ad.add(x, index, base, out, workspace=ws[:-64])
+        check(ad, x, index, base, out)
+        assert (ws[-64:] == 255).all()
+
+
+def test_refusals_of_the_binding():
+    g = gen(1)
+    ad = make(g, 2, 8, 64, 32, BF16)
+    x, i, b = normal(g, 3, 64, dtype=BF16), torch.zeros((3,), dtype=torch.int32, device="cuda"), normal(g, 3, 32, dtype=BF16)
+    for call in (lambda: ad.add(x.half(), i, b, b), lambda: ad.add(x, i.long(), b, b), lambda: ad.add(x, i[:2], b, b), lambda: ad.add(x.cpu(), i, b, b),
+                 lambda: ad.add(x[:, :63], i, b, b), lambda: ad.add(x, i, b[:, :31], b), lambda: ad.add(x, i, b, b.float()), lambda: ad.add(x[0], i, b, b),
+                 lambda: ad.add(x, i, b, b, workspace=torch.empty((8,), dtype=torch.uint8, device="cuda")), lambda: ad.add(x, i, b.double(), b.double()),
+                 lambda: ad.add(x, i, b, b, workspace=torch.empty((1 << 20,), dtype=torch.uint8, device="cuda")[::2]), lambda: ad.add(x[:0], i[:0], b[:0], b[:0]),
+                 lambda: ad.add(x.t().contiguous().t(), i, b, b), lambda: ad.add(x, i, b.t().contiguous().t(), b),
+                 lambda: A.Adapters(ad.a, ad.b.half()), lambda: A.Adapters(ad.a[:1], ad.b), lambda: A.Adapters(ad.a.float(), ad.b.float()),
+                 lambda: A.Adapters(ad.a, ad.b, ad.scales.half()), lambda: A.Adapters(ad.a, ad.b, None, i), lambda: A.Adapters(ad.a.cpu(), ad.b),
+                 lambda: A.Adapters(ad.a[:, :, ::2], ad.b), lambda: A.Adapters(ad.a[:0], ad.b[:0])):
+        with pytest.raises(A.AqmbError):
+            call()
