@@ -674,9 +674,10 @@ aqmb_status aqmb_rotary_append(const aqmb_kv_cache* cache, const aqmb_rotary_des
  *   ranks   int32 [n_adapters]: how many rows of an adapter's a and columns of its b are its own (clamped to
  *           [0, rank]); what lies behind them is not used and may hold anything. NULL: rank everywhere
  * All in device memory, read when a call runs: an adapter may be exchanged between calls.
- * 1 <= rank <= AQMB_MAX_RANK; d_in and d_out of any size up to 2^24.
+ * 1 <= rank <= AQMB_MAX_RANK, 1 <= n_adapters <= AQMB_MAX_ADAPTERS; d_in and d_out of any size up to 2^23.
  */
 #define AQMB_MAX_RANK 256
+#define AQMB_MAX_ADAPTERS 8192
 typedef struct {
   const void* a;
   const void* b;
@@ -703,8 +704,8 @@ typedef struct {
  * workspace: aqmb_adapters_workspace_bytes bytes of device memory, 16-byte aligned, written by the call (calls that
  * share one must be ordered); 0 bytes: NULL is fine.
  * Errors: EINVAL (null or misaligned pointer, sizes < 1, a stride below a row, out in place with another stride,
- * workspace too small), EUNSUPPORTED (dtype, rank, d_in, d_out, n_adapters above 2^24, n_rows above 2^22 - 64,
- * ceil(n_rows / 64) * ceil(d_out / 256) of 2^23 or more), EHIP.
+ * workspace too small), EUNSUPPORTED (dtype, rank, n_adapters, d_in, d_out, n_rows above 2^22 - 64,
+ * (min(n_rows, n_adapters + 1) + n_rows / 64) * ceil(d_out / 256) of 2^24 or more), EHIP.
  */
 aqmb_status aqmb_adapters_add(const aqmb_adapters* adapters, const void* x, int64_t x_stride, const int32_t* index,
                               int n_rows, const void* base, int64_t base_stride, void* out, int64_t out_stride,

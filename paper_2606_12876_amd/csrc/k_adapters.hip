@@ -1,23 +1,46 @@
 // Low-rank adapters of many requests beside one projection, out_i = base_i + s_n B_n (A_n x_i), n = index_i.
 //
 // Two launches: t = A_n x (binary32, partial sums over parts of the inputs side by side in the workspace), then
-// out = base + B_n (s_n t). Both take 64 neighbouring rows at a time and sort them by adapter with wave-wide votes: a
-// tile is up to 16 of them that share an adapter, the columns of one matrix instruction, with 16 rows of A or B as
-// its rows. So each row meets only its own adapter, in any order of the indexes, without atomics, and what
-// an adapter weighs is read once per tile. Few rows are bound by the adapters' bytes and two launches' latency, many by x, base
-// and out.
+// out = base + B_n (s_n t). Both look at 64 neighbouring rows with wave-wide votes: those that share an adapter are the
+// columns of matrix instructions, 16 each, with 16 rows of A or B as their rows. So each row meets only its own
+// adapter, in any order of the indexes, without atomics. Few rows: a workgroup per 16 rows of an adapter, bound by the
+// adapters' bytes and the latency of two launches. Many: a workgroup takes the adapters of 64 rows in turn, up to 64 columns at once
+// for what it reads of A and B, bound by x, base and out.
 #include "device.h"
 #include "ops.h"
 
 namespace aqmb {
 
+#include <cstdlib>
+static int TUNE(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 struct __attribute__((packed, aligned(2))) Raw8 { uint32_t w[4]; };
 struct __attribute__((packed, aligned(4))) F4 { float f[4]; };
 
-constexpr int kRows = 64;      // rows that a wave sorts by adapter
+__device__ __forceinline__ void lds_order() {      // a wave's LDS accesses run in order; the compiler's do now too
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+#ifndef ADNW
+#define ADNW 4
+#endif
+#ifndef ADU
+#define ADU 2
+#endif
+#ifndef ADBUF
+#define ADBUF 1
+#endif
+#ifndef ADOCC
+#define ADOCC 2
+#endif
+constexpr int kRows = 64;      // rows that a wave looks at
+constexpr int kFewWaves = 8;   // of a workgroup that sums over the inputs for one tile
+constexpr int kManyWaves = ADNW;
+constexpr int kMaxSplits = 4;
+constexpr int kMaxAdapters = AQMB_MAX_ADAPTERS;     // the sort's bins
 
 // Values k .. k + 7 of a row of n, 0 from n on. Rows may start at any element.
 __device__ __forceinline__ u32x4_t load8(const uint16_t* row, int k) {
@@ -26,11 +49,36 @@ __device__ __forceinline__ u32x4_t load8(const uint16_t* row, int k) {
 }
 __device__ __forceinline__ u32x4_t load8(const uint16_t* row, int k, int n) {
   if (k + 8 <= n) return load8(row, k);
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (k + j < n) w[j / 2] |= (uint32_t)row[k + j] << (16 * (j % 2));
-  return u32x4_t{w[0], w[1], w[2], w[3]};
+  if (k >= n) return u32x4_t{0, 0, 0, 0};
+  uint64_t lo = 0, hi = 0;
+  if (n >= 8) {                   // the row's last 8 values, moved down by those before k
+    const u32x4_t v = load8(row, n - 8);
+    lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+    const int past = k - (n - 8);
+    if (past >= 4) lo = hi, hi = 0;
+    const int s = 16 * (past % 4);
+    if (s) lo = lo >> s | hi << (64 - s), hi >>= s;
+  } else {
+    for (int j = 0; k + j < n; ++j)
+      if (j < 4) lo |= (uint64_t)row[k + j] << (16 * j);
+      else hi |= (uint64_t)row[k + j] << (16 * (j - 4));
+  }
+  return u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// The same without a branch, n >= 8: a row's last 8 values, moved down by those before k.
+__device__ __forceinline__ u32x4_t load8_moved(const uint16_t* row, int k, int n) {
+  const u32x4_t v = load8(row, min(k, n - 8));
+  const int past = max(k - (n - 8), 0);
+  uint32_t a = v.x, b = v.y, c = v.z, d = v.w;
+  const bool four = past & 4, two = past & 2;
+  const uint32_t odd = 16 * (past & 1);
+  a = four ? c : a, b = four ? d : b, c = four ? 0 : c, d = four ? 0 : d;
+  a = two ? b : a, b = two ? c : b, c = two ? d : c, d = two ? 0 : d;
+  a = __builtin_amdgcn_alignbit(b, a, odd), b = __builtin_amdgcn_alignbit(c, b, odd), c = __builtin_amdgcn_alignbit(d, c, odd);
+  d >>= odd;
+  const bool none = past >= 8;
+  return u32x4_t{none ? 0 : a, none ? 0 : b, none ? 0 : c, none ? 0 : d};
 }
 
 template <int DT>
@@ -41,118 +89,175 @@ __device__ __forceinline__ f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// Up to 16 of the 64 rows from row0 on that share an adapter (-1: none).
-struct Tile {
-  bool found;
-  int adapter, count;
-  int row;             // of slot lane % 16; slots past count repeat the first
+// Of 64 rows from row0 on: lane l has row row0 + l and the number of its adapter (-1: none).
+struct Rows {
+  int row, adapter;
+  bool in;
 };
-
-// Tile number `want` of these rows, in the order of their adapters' first rows. All lanes of the wave take part.
-__device__ __forceinline__ Tile find_tile(const AdapterArgs& a, int row0, int want) {
-  const int lane = threadIdx.x % 64, r = row0 + lane;
-  const bool in = r < a.n_rows;
-  int n = in ? a.index[r] : -1;
-  if ((unsigned)n >= (unsigned)a.ad.n_adapters) n = -1;
-  uint64_t todo = __ballot(in);
-  Tile t = {false, -1, 0, row0};
-  int seen = 0;
-  while (todo) {
-    const int leader = __builtin_ctzll(todo), own = __builtin_amdgcn_readlane(n, leader);
-    const uint64_t mask = __ballot(in && n == own);
-    todo &= ~mask;
-    const int tiles = (__builtin_popcountll(mask) + 15) / 16;
-    if (want < seen + tiles) {
-      const int first = (want - seen) * 16;
-      const int at = __builtin_popcountll(mask & ((1ull << lane) - 1)) - first;
-      const bool mine = (mask >> lane & 1) && at >= 0 && at < 16;
-      t.found = true;
-      t.adapter = own;
-      t.count = min(__builtin_popcountll(mask) - first, 16);
-      // Each row's lane sends its number to its slot (the others to a lane that no one asks), then all read theirs.
-      const int sent = __builtin_amdgcn_ds_permute((mine ? at : 63) * 4, r);
-      const int slot = lane % 16;
-      t.row = __builtin_amdgcn_ds_bpermute((slot < t.count ? slot : 0) * 4, sent);
-      return t;
-    }
-    seen += tiles;
+__device__ __forceinline__ Rows rows_at(const AdapterArgs& a, int row0) {
+  Rows r;
+  r.row = row0 + threadIdx.x % 64;
+  r.in = r.row < a.n_rows;
+  r.adapter = r.in ? a.index[r.row] : -1;
+  if ((unsigned)r.adapter >= (unsigned)a.ad.n_adapters) r.adapter = -1;
+  return r;
+}
+// Up to 16 CT of them that share an adapter. Slot 16 c + i of them is column i of c.
+template <int CT>
+struct Tile {
+  int adapter, count;
+  int row[CT];         // of slots 16 c + lane % 16; those past count repeat the first
+};
+// The rows of `mask` from number `first` on. All lanes of the wave take part.
+template <int CT>
+__device__ __forceinline__ Tile<CT> tile_of(const Rows& r, uint64_t mask, int adapter, int first) {
+  const int lane = threadIdx.x % 64;
+  Tile<CT> t;
+  t.adapter = adapter;
+  t.count = min(__builtin_popcountll(mask) - first, 16 * CT);
+  // Each row's lane sends its number to its slot; the others to lane 63, which is no slot then. Then all read theirs.
+  const int at = __builtin_popcountll(mask & ((1ull << lane) - 1)) - first;
+  const bool mine = (mask >> lane & 1) && at >= 0 && at < t.count;
+  const int sent = __builtin_amdgcn_ds_permute((mine ? at : 63) * 4, r.row);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int slot = 16 * c + lane % 16;
+    t.row[c] = __builtin_amdgcn_ds_bpermute((slot < t.count ? slot : 0) * 4, sent);
   }
   return t;
 }
+// The tile of 16 that starts with row `start`, if one does: every 16th of its adapter's rows among its 64 starts one.
+__device__ __forceinline__ bool tile_at(const AdapterArgs& a, int start, Tile<1>& t) {
+  const Rows r = rows_at(a, start / kRows * kRows);
+  const int l = start % kRows, n = __builtin_amdgcn_readlane(r.adapter, l);
+  const uint64_t mask = __ballot(r.in && r.adapter == n);
+  const int first = __builtin_popcountll(mask & ((1ull << l) - 1));
+  if (first % 16) return false;
+  t = tile_of<1>(r, mask, n, first);
+  return true;
+}
 
 __device__ __forceinline__ int own_rank(const AdapterArgs& a, int adapter) {
-  return a.ad.ranks ? min(max(a.ad.ranks[adapter], 0), a.ad.rank) : a.ad.rank;
+  return adapter < 0 ? 0 : a.ad.ranks ? min(max(a.ad.ranks[adapter], 0), a.ad.rank) : a.ad.rank;
 }
 
-// acc[m] += rows 16 m .. of A times the tile's rows of x, over inputs k0 .. k1 - 1 (k0 a multiple of 32).
+// t of a tile over part `part` of the inputs, by a workgroup whose waves share them out.
+template <int DT, int RT, int CT, int NW>
+__device__ __forceinline__ void shrink(const AdapterArgs& a, const Tile<CT>& t, int part, float (*lds)[NW][CT * 256], int* slots) {
+  constexpr int U = CT > 1 ? ADU : RT + CT <= 3 ? 4 : RT + CT <= 6 ? 2 : 1;       // steps of 32 inputs loaded at once
+  const int rank = own_rank(a, t.adapter);
+  if (rank == 0) return;                                           // the whole workgroup
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, kg = lane / 16 * 8, d_in = a.ad.d_in;
+  const uint16_t* x[CT];
+  const uint16_t* w[RT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) x[c] = (const uint16_t*)a.x + t.row[c] * a.x_stride + kg;
+#pragma unroll
+  for (int m = 0; m < RT; ++m)
+    w[m] = (const uint16_t*)a.ad.a + ((int64_t)t.adapter * a.ad.rank + min(16 * m + i, rank - 1)) * d_in + kg;
+
+  f32x4_t acc[RT][CT] = {};
+  const int steps = (d_in + 31) / 32, parts = a.splits * NW, p = part * NW + wave;
+  const int k0 = (int)((int64_t)steps * p / parts) * 32, k1 = min((int)((int64_t)steps * (p + 1) / parts) * 32, d_in);
+  const int whole = k0 + (k1 - k0) / (32 * U) * (32 * U);
+  struct Batch { u32x4_t x[U][CT], w[U][RT]; };
+  const auto load = [&](Batch& b, int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) b.x[u][c] = load8(x[c], k + 32 * u);
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank) b.w[u][m] = load8(w[m], k + 32 * u);
+    }
+  };
+  const auto multiply = [&](const Batch& b) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[m][c] = mma<DT>(b.w[u][m], b.x[u][c], acc[m][c]);
+  };
+  if constexpr (RT + CT > 8 || (CT > 1 && !ADBUF)) {                                     // no registers left to load ahead
+    for (int k = k0; k < whole; k += 32 * U) {
+      Batch now;
+      load(now, k);
+      multiply(now);
+    }
+  } else if (whole > k0) {
+    Batch now, next;
+    load(now, k0);
+    for (int k = k0 + 32 * U; k < whole; k += 32 * U) {
+      load(next, k);
+      multiply(now);
+      now = next;
+    }
+    multiply(now);
+  }
+  for (int k = whole; k < k1; k += 32) {                           // fewer than U steps, the last of fewer inputs
+    u32x4_t xv[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) xv[c] = load8(x[c] - kg, k + kg, d_in);
+#pragma unroll
+    for (int m = 0; m < RT; ++m)
+      if (16 * m < rank) {
+        const u32x4_t wv = load8(w[m] - kg, k + kg, d_in);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[m][c] = mma<DT>(wv, xv[c], acc[m][c]);
+      }
+  }
+
+  // The waves' sums added up, 16 values of t at a time.
+  float* out = a.t + (int64_t)part * a.n_rows * a.t_stride;
+  if (wave == 0 && lane < 16) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) slots[16 * c + lane] = t.row[c];
+  }
+#pragma unroll
+  for (int m = 0; m < RT; ++m) {
+    if (16 * m >= rank) break;                                     // the whole workgroup
+#pragma unroll
+    for (int c = 0; c < CT; ++c) *(f32x4_t*)&lds[m % 2][wave][c * 256 + lane * 4] = acc[m][c];
+    __syncthreads();
+    for (int e = threadIdx.x; e < CT * 256; e += NW * 64) {
+      float s = 0.f;
+#pragma unroll
+      for (int n = 0; n < NW; ++n) s += lds[m % 2][n][e];
+      const int l = e / 4 % 64, slot = e / 256 * 16 + l % 16;
+      if (slot < t.count) out[(int64_t)slots[slot] * a.t_stride + 16 * m + l / 16 * 4 + e % 4] = s;
+    }
+  }
+}
+
+// Few rows: blockIdx.x is the row that a tile starts with.
 template <int DT, int RT>
-__device__ __forceinline__ void shrink(const AdapterArgs& a, const Tile& t, int rank, int k0, int k1, f32x4_t* acc) {
-  const int lane = threadIdx.x % 64, i = lane % 16, kg = lane / 16 * 8, d_in = a.ad.d_in;
-  const uint16_t* x = (const uint16_t*)a.x + t.row * a.x_stride;
-  const uint16_t* w = (const uint16_t*)a.ad.a + (int64_t)t.adapter * a.ad.rank * d_in;
-  const uint16_t* row[RT];
-#pragma unroll
-  for (int m = 0; m < RT; ++m) row[m] = w + (int64_t)min(16 * m + i, rank - 1) * d_in;
-  const int whole = min(k1, d_in / 32 * 32);
-  int k = k0;
-#pragma unroll 4
-  for (; k < whole; k += 32) {
-    const u32x4_t xv = load8(x, k + kg);
-#pragma unroll
-    for (int m = 0; m < RT; ++m)
-      if (16 * m < rank) acc[m] = mma<DT>(load8(row[m], k + kg), xv, acc[m]);
-  }
-  if (k < k1) {                       // the last inputs, fewer than 32
-    const u32x4_t xv = load8(x, k + kg, d_in);
-#pragma unroll
-    for (int m = 0; m < RT; ++m)
-      if (16 * m < rank) acc[m] = mma<DT>(load8(row[m], k + kg, d_in), xv, acc[m]);
-  }
+__global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
+  __shared__ __align__(16) float lds[2][kFewWaves][256];
+  __shared__ int slots[16];
+  Tile<1> t;
+  if (tile_at(a, blockIdx.x, t)) shrink<DT, RT, 1, kFewWaves>(a, t, blockIdx.y, lds, slots);
 }
-
-// kFew: one tile per workgroup, its waves side by side along the inputs; else a wave per tile.
-template <int DT, int RT, bool kFew>
-__global__ __launch_bounds__(256) void shrink_kernel(AdapterArgs a) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, steps = (a.ad.d_in + 31) / 32;
-  const int64_t pitch = (int64_t)a.n_rows * a.t_stride;
-  if constexpr (kFew) {
-    __shared__ __align__(16) float lds[2][4][256];
-    const Tile t = find_tile(a, 0, blockIdx.x);
-    if (!t.found || t.adapter < 0) return;               // the whole workgroup
-    const int rank = own_rank(a, t.adapter);
-    if (rank == 0) return;
-    const int parts = 4 * a.splits, part = blockIdx.y * 4 + wave;
-    f32x4_t acc[RT] = {};
-    shrink<DT, RT>(a, t, rank, (int)((int64_t)steps * part / parts) * 32,
-                   min((int)((int64_t)steps * (part + 1) / parts) * 32, a.ad.d_in), acc);
+// Many: blockIdx.x is a tile of 64 rows.
+template <int DT, int RT, int CT>
+__global__ __launch_bounds__(64 * kManyWaves, ADOCC) void shrink_many(AdapterArgs a) {
+  __shared__ __align__(16) float lds[2][kManyWaves][CT * 256];
+  __shared__ int slots[16 * CT];
+  if ((int)blockIdx.x >= *a.n_tiles) return;
+  const int4 tile = a.tiles[blockIdx.x];
+  if (tile.x < 0) return;
+  for (int first = 0; first < tile.z; first += 16 * CT) {
+    Tile<CT> t;
+    t.adapter = tile.x;
+    t.count = min(tile.z - first, 16 * CT);
 #pragma unroll
-    for (int m = 0; m < RT; ++m) {
-      if (16 * m >= rank) break;                         // the whole workgroup
-      *(f32x4_t*)&lds[m % 2][wave][lane * 4] = acc[m];
-      __syncthreads();
-      if (wave == m % 4 && lane % 16 < t.count) {
-        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < 4; ++w) s += *(const f32x4_t*)&lds[m % 2][w][lane * 4];
-        *(f32x4_t*)(a.t + blockIdx.y * pitch + (int64_t)t.row * a.t_stride + 16 * m + lane / 16 * 4) = s;
-      }
+    for (int c = 0; c < CT; ++c) {
+      const int slot = 16 * c + threadIdx.x % 16;
+      t.row[c] = a.order[tile.y + first + (slot < t.count ? slot : 0)];
     }
-  } else {
-    for (int want = wave;; want += 4) {
-      const Tile t = find_tile(a, blockIdx.x * kRows, want);
-      if (!t.found) return;
-      if (t.adapter < 0) continue;
-      const int rank = own_rank(a, t.adapter);
-      if (rank == 0) continue;
-      f32x4_t acc[RT] = {};
-      shrink<DT, RT>(a, t, rank, (int)((int64_t)steps * blockIdx.y / a.splits) * 32,
-                     min((int)((int64_t)steps * (blockIdx.y + 1) / a.splits) * 32, a.ad.d_in), acc);
-      if (lane % 16 < t.count) {
-#pragma unroll
-        for (int m = 0; m < RT; ++m)
-          if (16 * m < rank)
-            *(f32x4_t*)(a.t + blockIdx.y * pitch + (int64_t)t.row * a.t_stride + 16 * m + lane / 16 * 4) = acc[m];
-      }
-    }
+    shrink<DT, RT, CT, kManyWaves>(a, t, blockIdx.y, lds, slots);
+    __syncthreads();
   }
 }
 
@@ -171,115 +276,32 @@ template <> struct Parts<AQMB_F16> {
   static __device__ __forceinline__ float lo(uint32_t w) { return f16lo(w); }
   static __device__ __forceinline__ float hi(uint32_t w) { return f16hi(w); }
 };
-template <int DT>
-__device__ __forceinline__ void split(float* f, u32x4_t* out) {
+// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave, into to[kt][part][lane]; what
+// the results are to be multiplied by into back[slot].
+template <int DT, int KT>
+__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, u32x4_t (*to)[Parts<DT>::kN][64],
+                                         float* back) {
   typedef Parts<DT> P;
-#pragma unroll
-  for (int p = 0; p < P::kN; ++p)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t w = P::pack(f[2 * j], f[2 * j + 1]);
-      out[p][j] = w;
-      f[2 * j] -= P::lo(w);
-      f[2 * j + 1] -= P::hi(w);
-    }
-}
-
-// 16 neighbouring values of a row of outputs, from element o on.
-template <int YT>
-__device__ __forceinline__ void load16(const void* row, int o, int n, float* f) {
-  if constexpr (YT == AQMB_F32) {
-    const float* p = (const float*)row + o;
-    if (o + 16 <= n) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const F4 v = *(const F4*)(p + 4 * j);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[4 * j + e] = v.f[e];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) f[j] = o + j < n ? p[j] : 0.f;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const u32x4_t v = load8((const uint16_t*)row, o + 8 * j, n);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[8 * j + 2 * e] = YT == AQMB_F16 ? f16lo(v[e]) : bf16lo(v[e]);
-        f[8 * j + 2 * e + 1] = YT == AQMB_F16 ? f16hi(v[e]) : bf16hi(v[e]);
-      }
-    }
-  }
-}
-template <int YT>
-__device__ __forceinline__ void store16(void* row, int o, int n, const float* f) {
-  if constexpr (YT == AQMB_F32) {
-    float* p = (float*)row + o;
-    if (o + 16 <= n) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *(F4*)(p + 4 * j) = F4{{f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]}};
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (o + j < n) p[j] = f[j];
-    }
-  } else {
-    uint16_t* p = (uint16_t*)row + o;
-    uint32_t w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = YT == AQMB_F16 ? pack_f16x2(f[2 * j], f[2 * j + 1]) : pack_bf16x2(f[2 * j], f[2 * j + 1]);
-    if (o + 16 <= n) {
-      *(Raw8*)p = Raw8{{w[0], w[1], w[2], w[3]}};
-      *(Raw8*)(p + 8) = Raw8{{w[4], w[5], w[6], w[7]}};
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (o + j < n) p[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
-    }
-  }
-}
-
-// Outputs o0 .. o1 - 1 (o0 a multiple of 64) of the tile's rows.
-template <int DT, int YT, int KT>
-__device__ __forceinline__ void expand(const AdapterArgs& a, const Tile& t, int o0, int o1) {
-  constexpr int kParts = Parts<DT>::kN, kSize = YT == AQMB_F32 ? 4 : 2;
-  const int lane = threadIdx.x % 64, i = lane % 16, q = lane / 16, d_out = a.ad.d_out;
-  const bool on = i < t.count;
-  const char* base = (const char*)a.base + t.row * a.base_stride * kSize;
-  char* out = (char*)a.out + t.row * a.out_stride * kSize;
-  const int rank = t.adapter < 0 ? 0 : own_rank(a, t.adapter);
-  if (rank == 0) {
-    if (a.base == a.out || !on) return;
-    for (int o = o0 + 16 * q; o < o1; o += 64) {
-      float f[16];
-      load16<YT>(base, o, d_out, f);
-      store16<YT>(out, o, d_out, f);
-    }
-    return;
-  }
-
-  // The row's t: partial sums added up, scaled, 0 from the adapter's rank on.
+  const int lane = threadIdx.x % 64, q = lane / 16;
+  const float* tp = a.t + (int64_t)row * a.t_stride + 8 * q;
   float v[KT][8];
-  const float s = a.ad.scales ? a.ad.scales[t.adapter] : 1.f;
-  const float* tp = a.t + (int64_t)t.row * a.t_stride + 8 * q;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
+    // Partial sums added up, scaled, 0 from the adapter's rank on.
+    f32x4_t lo[kMaxSplits] = {}, hi[kMaxSplits] = {};
+    if (32 * kt < a.ad.rank && 32 * kt + 8 * q < a.t_stride) {      // not by rank, which may still be on its way
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[kt][j] = 0.f;
-    if (32 * kt + 8 * q < rank) {
-      for (int p = 0; p < a.splits; ++p) {
-        const f32x4_t* w = (const f32x4_t*)(tp + p * (int64_t)a.n_rows * a.t_stride + 32 * kt);
-        const f32x4_t lo = w[0], hi = w[1];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[kt][j] += lo[j], v[kt][4 + j] += hi[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[kt][j] = 32 * kt + 8 * q + j < rank ? v[kt][j] * s : 0.f;
+      for (int p = 0; p < kMaxSplits; ++p)
+        if (p < a.splits) {
+          const f32x4_t* from = (const f32x4_t*)(tp + p * (int64_t)a.n_rows * a.t_stride + 32 * kt);
+          lo[p] = from[0], hi[p] = from[1];
+        }
     }
+#pragma unroll
+    for (int p = 1; p < kMaxSplits; ++p) lo[0] += lo[p], hi[0] += hi[p];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[kt][j] = 32 * kt + 8 * q + j < rank ? (j < 4 ? lo[0][j % 4] : hi[0][j % 4]) * scale : 0.f;
   }
-  float back = 1.f;
   if constexpr (DT == AQMB_F16) {
     // By a power of two, so that the row's largest magnitude is in [2^13, 2^14): in fp16's range, the parts far
     // from its subnormals.
@@ -292,84 +314,339 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile& t, int 
     big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 32), (int)big));
     const int ex = min(max((int)(big >> 23), 14), 254);    // the exponent that goes to 13
     const float fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
-    back = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
+    if (lane < 16) back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[kt][j] *= fwd;
   }
-  u32x4_t tv[KT][kParts];
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt) split<DT>(v[kt], tv[kt]);
-
-  // Row i of matrix tile m is output 16 (i / 4) + 4 m + i % 4 of 64: so a lane's results are 16 neighbours.
-  const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * a.ad.rank;
-  for (int o = o0; o < o1; o += 64) {
-    float f[16];
-    if (on) load16<YT>(base, o + 16 * q, d_out, f);
+  for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const uint16_t* w = b + (int64_t)min(o + i / 4 * 16 + 4 * m + i % 4, d_out - 1) * a.ad.rank;
-      f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < P::kN; ++p) {
+      u32x4_t w;
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        if (32 * kt < rank) {
-          const u32x4_t wv = load8(w, 32 * kt + 8 * q, rank);
-#pragma unroll
-          for (int p = kParts - 1; p >= 0; --p) acc = mma<DT>(wv, tv[kt][p], acc);
-        }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[4 * m + j] = DT == AQMB_F16 ? fmaf(acc[j], back, f[4 * m + j]) : f[4 * m + j] + acc[j];
+      for (int j = 0; j < 4; ++j) {
+        w[j] = P::pack(v[kt][2 * j], v[kt][2 * j + 1]);
+        v[kt][2 * j] -= P::lo(w[j]);
+        v[kt][2 * j + 1] -= P::hi(w[j]);
+      }
+      to[kt][p][lane] = w;
     }
-    if (on) store16<YT>(out, o + 16 * q, d_out, f);
+}
+
+// 8 neighbouring outputs of a row as they are stored (16 bits or, kWide, binary32).
+template <bool kWide> struct Eight { u32x4_t v[kWide ? 2 : 1]; };
+// From element o on. kEights: rows of a multiple of 8 elements, so that all 8 exist or none (then others are read).
+template <bool kWide, bool kEights>
+__device__ __forceinline__ Eight<kWide> load_y(const void* row, int o, int n) {
+  Eight<kWide> r;
+  if constexpr (kWide) {
+    const float* p = (const float*)row + (kEights ? min(o, n - 8) : o);
+    if (kEights || o + 8 <= n) {
+      r.v[0] = __builtin_bit_cast(u32x4_t, *(const F4*)p);
+      r.v[1] = __builtin_bit_cast(u32x4_t, *(const F4*)(p + 4));
+    } else {
+      f32x4_t lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+      if (o < n) lo.x = p[0];
+      if (o + 1 < n) lo.y = p[1];
+      if (o + 2 < n) lo.z = p[2];
+      if (o + 3 < n) lo.w = p[3];
+      if (o + 4 < n) hi.x = p[4];
+      if (o + 5 < n) hi.y = p[5];
+      if (o + 6 < n) hi.z = p[6];
+      r.v[0] = __builtin_bit_cast(u32x4_t, lo), r.v[1] = __builtin_bit_cast(u32x4_t, hi);
+    }
+  } else {
+    r.v[0] = kEights ? load8((const uint16_t*)row, min(o, n - 8)) : load8((const uint16_t*)row, o, n);
+  }
+  return r;
+}
+template <bool kWide, bool kEights>
+__device__ __forceinline__ void store_y(void* row, int o, int n, const Eight<kWide>& r) {
+  if (o >= n) return;
+  if constexpr (kWide) {
+    float* p = (float*)row + o;
+    if (kEights || o + 8 <= n) {
+      *(F4*)p = __builtin_bit_cast(F4, r.v[0]);
+      *(F4*)(p + 4) = __builtin_bit_cast(F4, r.v[1]);
+    } else {
+      const f32x4_t lo = __builtin_bit_cast(f32x4_t, r.v[0]), hi = __builtin_bit_cast(f32x4_t, r.v[1]);
+      p[0] = lo.x;
+      if (o + 1 < n) p[1] = lo.y;
+      if (o + 2 < n) p[2] = lo.z;
+      if (o + 3 < n) p[3] = lo.w;
+      if (o + 4 < n) p[4] = hi.x;
+      if (o + 5 < n) p[5] = hi.y;
+      if (o + 6 < n) p[6] = hi.z;
+    }
+  } else {
+    uint16_t* p = (uint16_t*)row + o;
+    const u32x4_t v = r.v[0];
+    if (kEights || o + 8 <= n) {
+      *(Raw8*)p = __builtin_bit_cast(Raw8, v);
+    } else {
+      p[0] = (uint16_t)v.x;
+      if (o + 1 < n) p[1] = (uint16_t)(v.x >> 16);
+      if (o + 2 < n) p[2] = (uint16_t)v.y;
+      if (o + 3 < n) p[3] = (uint16_t)(v.y >> 16);
+      if (o + 4 < n) p[4] = (uint16_t)v.z;
+      if (o + 5 < n) p[5] = (uint16_t)(v.z >> 16);
+      if (o + 6 < n) p[6] = (uint16_t)v.w;
+    }
+  }
+}
+// r += back * d[n][j], n < 8, rounded once (back is a power of two, 1 where kScaled is not set).
+template <bool kWide, bool kScaled>
+__device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], int j, float back, bool f16) {
+  const auto sum = [&](float x, float y) { return kScaled ? fmaf(y, back, x) : x + y; };
+  if constexpr (kWide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4_t f = __builtin_bit_cast(f32x4_t, r.v[h]);
+      r.v[h] = __builtin_bit_cast(u32x4_t, f32x4_t{sum(f.x, d[4 * h][j]), sum(f.y, d[4 * h + 1][j]), sum(f.z, d[4 * h + 2][j]),
+                                                   sum(f.w, d[4 * h + 3][j])});
+    }
+  } else {
+    const auto two = [&](uint32_t w, float x, float y) {
+      return f16 ? pack_f16x2(sum(f16lo(w), x), sum(f16hi(w), y)) : pack_bf16x2(sum(bf16lo(w), x), sum(bf16hi(w), y));
+    };
+    r.v[0] = u32x4_t{two(r.v[0].x, d[0][j], d[1][j]), two(r.v[0].y, d[2][j], d[3][j]), two(r.v[0].z, d[4][j], d[5][j]),
+                     two(r.v[0].w, d[6][j], d[7][j])};
   }
 }
 
-// kFew: blockIdx.y tile; else blockIdx.y 64 rows, a wave per tile.
-template <int DT, int YT, int KT, bool kFew>
-__global__ __launch_bounds__(256) void expand_kernel(AdapterArgs a) {
-  const int wave = threadIdx.x / 64;
-  if constexpr (kFew) {
-    const Tile t = find_tile(a, 0, blockIdx.y);
-    const int o0 = (blockIdx.x * 4 + wave) * a.per_wave;
-    if (t.found && o0 < a.ad.d_out) expand<DT, YT, KT>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out));
-  } else {
-    const int o0 = blockIdx.x * a.per_wave;
-    for (int want = wave;; want += 4) {
-      const Tile t = find_tile(a, blockIdx.y * kRows, want);
-      if (!t.found) return;
-      expand<DT, YT, KT>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out));
+// What a wave of the second launch keeps in LDS: t's operands, and 128 outputs' weights of a step of 32, output 8 c + n as row
+// 16 n + c, where the matrix instructions take it; 64 bytes a row, the four pieces swapped by c / 4 against bank conflicts.
+template <int DT, int KT>
+struct ExpandLds {
+  u32x4_t t[KT][Parts<DT>::kN][64];
+  float back[16];
+  u32x4_t w[8][68];
+};
+// Outputs o0 .. o1 - 1 (o0 a multiple of 128) of up to 16 rows that share an adapter, by one wave. Lane (q, c) of 4 x 16 has
+// outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and writes 256 bytes of a row at once
+// (with lanes side by side on different rows every lane was an access of its own to the vector cache, which bound
+// the kernel: 8192 rows of 4096 outputs 45 us).
+template <int DT, bool kWide, int KT, bool kEights>
+__device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, int o0, int o1, ExpandLds<DT, KT>& lds) {
+  constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
+  const int lane = threadIdx.x % 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
+  const int rank = own_rank(a, t.adapter);
+  if (rank == 0 && a.base == a.out) return;
+  int64_t row[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row[0]);
+  const auto load_rows = [&](Eight<kWide>* y, int o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = load_y<kWide, kEights>((const char*)a.base + row[j] * a.base_stride * kSize, o + 8 * c, d_out);
+  };
+  const auto store_rows = [&](const Eight<kWide>* y, int o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (4 * q + j < t.count) store_y<kWide, kEights>((char*)a.out + row[j] * a.out_stride * kSize, o + 8 * c, d_out, y[j]);
+  };
+  Eight<kWide> y[4];
+  if (rank == 0) {
+    for (int o = o0; o < o1; o += 128) {
+      load_rows(y, o);
+      store_rows(y, o);
     }
+    return;
   }
+
+  // Weights in pieces of 8: `pieces` lanes side by side (a power of two) to an output's row of a step.
+  const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * stack;
+  const auto shift_of = [&](int kt) { const int left = (kt == 0 ? stack : rank) - 32 * kt; return left > 16 ? 2 : left > 8 ? 1 : 0; };
+  const auto load_w = [&](u32x4_t* w, int o, int kt) {
+    const int shift = shift_of(kt);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= 2 << shift) break;
+      const int at = 64 * j + lane, k = 32 * kt + 8 * (at & ((1 << shift) - 1));
+      const uint16_t* r = b + (int64_t)min(o + (at >> shift), d_out - 1) * stack;
+      if constexpr (kEights) w[j] = load8(r, min(k, stack - 8));
+      else w[j] = stack >= 8 ? load8_moved(r, k, stack) : load8(r, k, stack);
+    }
+  };
+  const auto place_w = [&](const u32x4_t* w, int kt) {
+    const int shift = shift_of(kt);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= 2 << shift) break;
+      const int at = 64 * j + lane, o = at >> shift, piece = at & ((1 << shift) - 1);
+      lds.w[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
+    }
+  };
+  const int left = rank - (rank - 1) / 32 * 32 - 8 * q;  // own values in the lane's piece of the last step
+  u32x4_t mask;
+  mask.x = left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0;
+  mask.y = left >= 4 ? 0xFFFFFFFFu : left == 3 ? 0xFFFFu : 0;
+  mask.z = left >= 6 ? 0xFFFFFFFFu : left == 5 ? 0xFFFFu : 0;
+  mask.w = left >= 8 ? 0xFFFFFFFFu : left == 7 ? 0xFFFFu : 0;
+
+  // The first weights and rows of base are on their way while t comes; so are the next ones later.
+  u32x4_t w[8];
+  load_w(w, o0, 0);
+  load_rows(y, o0);
+  operands<DT, KT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds.t, lds.back);
+
+  for (int o = o0; o < o1; o += 128) {
+    const bool more = o + 128 < o1;
+    f32x4_t acc[8] = {};
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      if (32 * kt >= rank) break;
+      const bool last = kt + 1 == KT || 32 * (kt + 1) >= rank;
+      lds_order();
+      place_w(w, kt);
+      if (!last) load_w(w, o, kt + 1);
+      else if (more) load_w(w, o + 128, 0);
+      lds_order();
+      u32x4_t tv[kParts];
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) tv[p] = lds.t[kt][p][lane];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        u32x4_t wv = lds.w[n][c * 4 + (q ^ (c / 4))];
+        if (last) wv &= mask;
+#pragma unroll
+        for (int p = kParts - 1; p >= 0; --p) acc[n] = mma<DT>(tv[p], wv, acc[n]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? lds.back[4 * q + j] : 1.f, a.y_f16);
+    store_rows(y, o);
+    if (more) load_rows(y, o + 128);
+  }
+}
+
+// Few rows: blockIdx.y is the row that a tile starts with.
+template <int DT, bool kWide, int KT, bool kEights>
+__global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
+  __shared__ ExpandLds<DT, KT> lds[4];
+  const int wave = threadIdx.x / 64, o0 = (blockIdx.x * 4 + wave) * a.per_wave;
+  Tile<1> t;
+  if (tile_at(a, blockIdx.y, t) && o0 < a.ad.d_out)
+    expand<DT, kWide, KT, kEights>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), lds[wave]);
+}
+// Many: blockIdx.x is a tile of 64 rows, a wave for 16.
+template <int DT, bool kWide, int KT, bool kEights>
+__global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
+  __shared__ ExpandLds<DT, KT> lds[4];
+  const int wave = threadIdx.x / 64, o0 = blockIdx.y * a.per_wave;
+  if ((int)blockIdx.x >= *a.n_tiles) return;
+  const int4 tile = a.tiles[blockIdx.x];
+  if (16 * wave >= tile.z) return;
+  const int slot = 16 * wave + threadIdx.x % 16;
+  const Tile<1> t = {tile.x, min(tile.z - 16 * wave, 16), {a.order[tile.y + (slot < tile.z ? slot : 16 * wave)]}};
+  expand<DT, kWide, KT, kEights>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), lds[wave]);
+}
+
+// Many rows sorted by adapter (those without one last), and cut into tiles of up to 64 (adapter, first, count): one workgroup
+// counts, adds up and places. Rows of one adapter come in any order, which nothing depends on.
+__global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
+  __shared__ int bins[kMaxAdapters + 1], sums[2][16];
+  constexpr int kEach = 8;       // rows of a thread at once
+  const int n_bins = a.ad.n_adapters + 1, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  for (int i = threadIdx.x; i < n_bins; i += 1024) bins[i] = 0;
+  __syncthreads();
+  // use(row, its place in its bin); the places of a wave's rows that all have one adapter are taken at once.
+  const auto take = [&](auto use) {
+    for (int r0 = 0; r0 < a.n_rows; r0 += 1024 * kEach) {
+      int n[kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int r = r0 + 1024 * j + threadIdx.x;
+        n[j] = r < a.n_rows ? a.index[r] : -1;
+        if ((unsigned)n[j] >= (unsigned)a.ad.n_adapters) n[j] = a.ad.n_adapters;
+      }
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int r = r0 + 1024 * j + threadIdx.x;
+        const uint64_t in = __ballot(r < a.n_rows);
+        if (in == 0) break;
+        const int first = __builtin_amdgcn_readfirstlane(n[j]);
+        int at = 0;
+        if ((in & ~__ballot(n[j] == first)) == 0) {
+          if (lane == 0) at = atomicAdd(&bins[first], __builtin_popcountll(in));
+          at = __builtin_amdgcn_readfirstlane(at) + lane;
+        } else if (r < a.n_rows) {
+          at = atomicAdd(&bins[n[j]], 1);
+        }
+        if (r < a.n_rows) use(r, at);
+      }
+    }
+  };
+  take([](int, int) {});
+  __syncthreads();
+  // Each thread's bins, neighbours; their rows and tiles before it.
+  const int per = (n_bins + 1023) / 1024, b0 = threadIdx.x * per, b1 = min(b0 + per, n_bins);
+  int rows = 0, tiles = 0;
+  for (int i = b0; i < b1; ++i) rows += bins[i], tiles += (bins[i] + 63) / 64;
+  int before[2] = {rows, tiles};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int own = before[k];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int v = __builtin_amdgcn_ds_bpermute(4 * (lane - d), before[k]);
+      if (lane >= d) before[k] += v;
+    }
+    if (lane == 63) sums[k][wave] = before[k];
+    before[k] -= own;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (int w = 0; w < wave; ++w) before[k] += sums[k][w];
+  for (int i = b0; i < b1; ++i) {
+    const int count = bins[i];
+    bins[i] = before[0];
+    for (int j = 0; j < count; j += 64) a.tiles[before[1]++] = make_int4(i < a.ad.n_adapters ? i : -1, before[0] + j, min(count - j, 64), 0);
+    before[0] += count;
+  }
+  if (threadIdx.x == 1023) *a.n_tiles = before[1];
+  __syncthreads();
+  take([&](int r, int at) { a.order[at] = r; });
 }
 
 template <int DT, int RT>
 hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  if (p.few) shrink_kernel<DT, RT, true><<<dim3(p.tiles, p.splits), 256, 0, st>>>(a);
-  else shrink_kernel<DT, RT, false><<<dim3((a.n_rows + kRows - 1) / kRows, p.splits), 256, 0, st>>>(a);
+  if (p.few) shrink_few<DT, RT><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
+  else shrink_many<DT, RT, (RT <= 4 ? 4 : RT <= 8 ? 2 : 1)><<<dim3(p.tiles, p.splits), 64 * kManyWaves, 0, st>>>(a);
   return hipGetLastError();
 }
-template <int DT, int YT, int KT>
+template <int DT, bool kWide, int KT, bool kEights>
 hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
   const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
-  if (p.few) expand_kernel<DT, YT, KT, true><<<dim3((parts + 3) / 4, p.tiles), 256, 0, st>>>(a);
-  else expand_kernel<DT, YT, KT, false><<<dim3(parts, (a.n_rows + kRows - 1) / kRows), 256, 0, st>>>(a);
+  if (p.few) expand_few<DT, kWide, KT, kEights><<<dim3((parts + 3) / 4, a.n_rows), 256, 0, st>>>(a);
+  else expand_many<DT, kWide, KT, kEights><<<dim3(p.tiles, parts), 256, 0, st>>>(a);
   return hipGetLastError();
 }
-template <int DT, int YT>
+template <int DT, bool kWide, bool kEights>
 hipError_t by_rank(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
   const int r = a.ad.rank;
-  return r <= 32 ? go_expand<DT, YT, 1>(a, p, st) : r <= 64 ? go_expand<DT, YT, 2>(a, p, st)
-         : r <= 128 ? go_expand<DT, YT, 4>(a, p, st) : go_expand<DT, YT, 8>(a, p, st);
+  return r <= 32 ? go_expand<DT, kWide, 1, kEights>(a, p, st) : r <= 64 ? go_expand<DT, kWide, 2, kEights>(a, p, st)
+         : r <= 128 ? go_expand<DT, kWide, 4, kEights>(a, p, st) : go_expand<DT, kWide, 8, kEights>(a, p, st);
+}
+template <int DT, bool kWide>
+hipError_t by_rank(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
+  return a.ad.rank % 8 || a.ad.d_out % 8 ? by_rank<DT, kWide, false>(a, p, st) : by_rank<DT, kWide, true>(a, p, st);
 }
 template <int DT>
 hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStream_t st) {
   const int r = a.ad.rank;
-  const hipError_t e = r <= 16 ? go_shrink<DT, 1>(a, p, st) : r <= 32 ? go_shrink<DT, 2>(a, p, st)
+  hipError_t e;
+  if (!p.few) {
+    sort_kernel<<<1, 1024, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  e = r <= 16 ? go_shrink<DT, 1>(a, p, st) : r <= 32 ? go_shrink<DT, 2>(a, p, st)
                        : r <= 64 ? go_shrink<DT, 4>(a, p, st) : r <= 128 ? go_shrink<DT, 8>(a, p, st) : go_shrink<DT, 16>(a, p, st);
   if (e != hipSuccess) return e;
-  return y == AQMB_F16 ? by_rank<DT, AQMB_F16>(a, p, st) : y == AQMB_BF16 ? by_rank<DT, AQMB_BF16>(a, p, st)
-                                                                          : by_rank<DT, AQMB_F32>(a, p, st);
+  return y == AQMB_F32 ? by_rank<DT, true>(a, p, st) : by_rank<DT, false>(a, p, st);
 }
 
 }  // namespace
@@ -379,21 +656,22 @@ AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   const int steps = (ad.d_in + 31) / 32;
   p.few = n_rows <= kRows;
   const int groups = n_rows < ad.n_adapters + 1 ? n_rows : ad.n_adapters + 1;
-  p.tiles = groups + 3 < n_rows ? groups + 3 : n_rows;
+  p.tiles = groups + (n_rows - groups) / 64;
   if (p.few) {
-    p.splits = steps / 16;
-    if (p.splits > 8) p.splits = 8;
-    p.per_wave = 64;
+    p.splits = steps / (kFewWaves * TUNE("AD_STEPS", 4));
+    p.per_wave = 128;
   } else {
-    const int blocks = (n_rows + kRows - 1) / kRows;
-    p.splits = 512 / blocks;
-    if (p.splits > steps / 8) p.splits = steps / 8;
-    if (p.splits > 8) p.splits = 8;
-    p.per_wave = 256;
+    p.splits = TUNE("AD_WG", 512) / ((n_rows + kRows - 1) / kRows);
+    if (p.splits > steps / 16) p.splits = steps / 16;
+    p.per_wave = TUNE("AD_PWM", 256);
   }
+  if (p.splits > kMaxSplits) p.splits = kMaxSplits;
   if (p.splits < 1) p.splits = 1;
   p.t_stride = (ad.rank + 15) / 16 * 16;
   p.bytes = (size_t)p.splits * n_rows * p.t_stride * 4;
+  // Many: behind t the number of tiles, the tiles and the rows' order.
+  p.at_tiles = p.bytes;
+  if (!p.few) p.bytes += 16 + (size_t)p.tiles * 16 + ((size_t)n_rows + 3) / 4 * 16;
   return p;
 }
 
@@ -401,6 +679,10 @@ hipError_t launch_adapters(AdapterArgs a, const AdapterPlan& p, aqmb_dtype y, hi
   a.t_stride = p.t_stride;
   a.splits = p.splits;
   a.per_wave = p.per_wave;
+  a.y_f16 = y == AQMB_F16;
+  a.n_tiles = (int*)((char*)a.t + p.at_tiles);
+  a.tiles = (int4*)((char*)a.t + p.at_tiles + 16);
+  a.order = (int*)(a.tiles + p.tiles);
   return a.ad.dtype == AQMB_F16 ? both<AQMB_F16>(a, p, y, st) : both<AQMB_BF16>(a, p, y, st);
 }
 

@@ -122,10 +122,12 @@ static aqmb_status check_adapters(const aqmb_adapters* a, int n_rows, const char
   if (a->n_adapters < 1 || a->rank < 1 || a->d_in < 1 || a->d_out < 1 || n_rows < 1)
     return fail(AQMB_EINVAL, "%s: n_adapters, rank, d_in, d_out and n_rows must be >= 1", where);
   if (a->rank > AQMB_MAX_RANK) return fail(AQMB_EUNSUPPORTED, "%s: rank = %d above %d", where, a->rank, AQMB_MAX_RANK);
-  if (a->n_adapters > 1 << 24 || a->d_in > 1 << 24 || a->d_out > 1 << 24)
-    return fail(AQMB_EUNSUPPORTED, "%s: n_adapters, d_in or d_out above 2^24", where);
+  if (a->n_adapters > AQMB_MAX_ADAPTERS) return fail(AQMB_EUNSUPPORTED, "%s: n_adapters = %d above %d", where, a->n_adapters, AQMB_MAX_ADAPTERS);
+  if (a->d_in > 1 << 23 || a->d_out > 1 << 23) return fail(AQMB_EUNSUPPORTED, "%s: d_in or d_out above 2^23", where);
   if (n_rows > (1 << 22) - 64) return fail(AQMB_EUNSUPPORTED, "%s: n_rows = %d above 2^22 - 64", where, n_rows);
-  if (((int64_t)n_rows + 63) / 64 * (((int64_t)a->d_out + 255) / 256) >= 1 << 23)
+  // A workgroup for every tile of up to 64 rows of an adapter and 256 outputs: fewer than 2^24.
+  const int64_t groups = n_rows <= a->n_adapters ? n_rows : a->n_adapters + 1;
+  if ((groups + n_rows / 64) * ((a->d_out + 255) / 256) >= 1 << 24)
     return fail(AQMB_EUNSUPPORTED, "%s: n_rows = %d of d_out = %d are more than one launch takes", where, n_rows, a->d_out);
   if (!a->a || !a->b) return fail(AQMB_EINVAL, "%s: a or b is NULL", where);
   if (!aligned(a->a, 2) || !aligned(a->b, 2) || !aligned(a->scales, 4) || !aligned(a->ranks, 4))

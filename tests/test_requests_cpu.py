@@ -60,10 +60,10 @@ def test_rotary_append_refuses(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(desc=False), S.EINVAL), (dict(a=None), S.EINVAL), (dict(b=None), S.EINVAL), (dict(a=17), S.EINVAL), (dict(b=17), S.EINVAL),
     (dict(s=18), S.EINVAL), (dict(r=18), S.EINVAL), (dict(dt=F32), S.EUNSUPPORTED), (dict(dt=F8), S.EUNSUPPORTED), (dict(n=0), S.EINVAL),
-    (dict(n=(1 << 24) + 1), S.EUNSUPPORTED), (dict(rank=0), S.EINVAL), (dict(rank=257), S.EUNSUPPORTED), (dict(din=0), S.EINVAL),
-    (dict(dout=0), S.EINVAL), (dict(din=(1 << 24) + 1), S.EUNSUPPORTED), (dict(dout=(1 << 24) + 1), S.EUNSUPPORTED),
+    (dict(n=8193), S.EUNSUPPORTED), (dict(rank=0), S.EINVAL), (dict(rank=257), S.EUNSUPPORTED), (dict(din=0), S.EINVAL),
+    (dict(dout=0), S.EINVAL), (dict(din=(1 << 23) + 1), S.EUNSUPPORTED), (dict(dout=(1 << 23) + 1), S.EUNSUPPORTED),
     (dict(rows=0), S.EINVAL), (dict(rows=(1 << 22) - 63), S.EUNSUPPORTED),
-    (dict(rows=1 << 21, dout=1 << 16, bs=1 << 16, os=1 << 16), S.EUNSUPPORTED),
+    (dict(rows=1 << 21, dout=1 << 17, bs=1 << 17, os=1 << 17), S.EUNSUPPORTED),
     (dict(x=None), S.EINVAL), (dict(x=17), S.EINVAL), (dict(xs=99), S.EINVAL), (dict(i=None), S.EINVAL), (dict(i=18), S.EINVAL),
     (dict(base=None), S.EINVAL), (dict(out=None), S.EINVAL), (dict(bs=59), S.EINVAL), (dict(os=59), S.EINVAL),
     (dict(out=16, os=61), S.EINVAL), (dict(out=18, yd=F32), S.EINVAL), (dict(base=17), S.EINVAL), (dict(yd=F8), S.EUNSUPPORTED),
