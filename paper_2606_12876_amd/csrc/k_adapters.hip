@@ -1,18 +1,16 @@
 // Low-rank adapters of many requests beside one projection, out_i = base_i + s_n B_n (A_n x_i), n = index_i.
 //
 // Two launches: t = A_n x (binary32, partial sums over parts of the inputs side by side in the workspace), then
-// out = base + B_n (s_n t). Both look at 64 neighbouring rows with wave-wide votes: those that share an adapter are the
-// columns of matrix instructions, 16 each, with 16 rows of A or B as their rows. So each row meets only its own
-// adapter, in any order of the indexes, without atomics. Few rows: a workgroup per 16 rows of an adapter, bound by the
-// adapters' bytes and the latency of two launches. Many: a workgroup takes the adapters of 64 rows in turn, up to 64 columns at once
-// for what it reads of A and B, bound by x, base and out.
+// out = base + B_n (s_n t). Rows that share an adapter are the columns of matrix instructions, 16 each, with 16 rows of A
+// or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows (up to
+// 64): every wave finds its 16 by votes over the indexes; the adapters' bytes and the latency of two launches bound them
+// (one row, rank 16, 4096 x 4096: 3.7 + 5.1 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
+// and out (8192 rows, rank 32, 4096 x 4096: sort 9 us, t 14.6 us, 4.6 TB/s, the outputs 38 us, 3.5 TB/s).
 #include "device.h"
 #include "ops.h"
 
 namespace aqmb {
 
-#include <cstdlib>
-static int TUNE(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
@@ -24,26 +22,13 @@ __device__ __forceinline__ void lds_order() {      // a wave's LDS accesses run 
   __builtin_amdgcn_wave_barrier();
 }
 
-#ifndef ADNW
-#define ADNW 4
-#endif
-#ifndef ADU
-#define ADU 2
-#endif
-#ifndef ADBUF
-#define ADBUF 1
-#endif
-#ifndef ADOCC
-#define ADOCC 2
-#endif
 constexpr int kRows = 64;      // rows that a wave looks at
 constexpr int kFewWaves = 8;   // of a workgroup that sums over the inputs for one tile
-constexpr int kManyWaves = ADNW;
 constexpr int kMaxSplits = 4;
 constexpr int kMaxAdapters = AQMB_MAX_ADAPTERS;     // the sort's bins
 
 // Values k .. k + 7 of a row of n, 0 from n on. Rows may start at any element.
-__device__ __forceinline__ u32x4_t load8(const uint16_t* row, int k) {
+__device__ __forceinline__ u32x4_t load8(const uint16_t* row, uint32_t k) {
   const Raw8 r = *(const Raw8*)(row + k);
   return u32x4_t{r.w[0], r.w[1], r.w[2], r.w[3]};
 }
@@ -141,31 +126,32 @@ __device__ __forceinline__ int own_rank(const AdapterArgs& a, int adapter) {
   return adapter < 0 ? 0 : a.ad.ranks ? min(max(a.ad.ranks[adapter], 0), a.ad.rank) : a.ad.rank;
 }
 
-// t of a tile over part `part` of the inputs, by a workgroup whose waves share them out.
-template <int DT, int RT, int CT, int NW>
-__device__ __forceinline__ void shrink(const AdapterArgs& a, const Tile<CT>& t, int part, float (*lds)[NW][CT * 256], int* slots) {
-  constexpr int U = CT > 1 ? ADU : RT + CT <= 3 ? 4 : RT + CT <= 6 ? 2 : 1;       // steps of 32 inputs loaded at once
+// Few rows: blockIdx.x is the row that a tile starts with, blockIdx.y a part of the inputs, which the waves share out.
+template <int DT, int RT>
+__global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
+  constexpr int U = RT <= 2 ? 4 : RT <= 4 ? 2 : 1;                 // steps of 32 inputs loaded at once
+  __shared__ __align__(16) float lds[2][kFewWaves][256];
+  __shared__ int slots[16];
+  Tile<1> t;
+  if (!tile_at(a, blockIdx.x, t)) return;
   const int rank = own_rank(a, t.adapter);
-  if (rank == 0) return;                                           // the whole workgroup
+  if (rank == 0) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, kg = lane / 16 * 8, d_in = a.ad.d_in;
-  const uint16_t* x[CT];
+  const uint16_t* x = (const uint16_t*)a.x + t.row[0] * a.x_stride + kg;
   const uint16_t* w[RT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) x[c] = (const uint16_t*)a.x + t.row[c] * a.x_stride + kg;
 #pragma unroll
   for (int m = 0; m < RT; ++m)
     w[m] = (const uint16_t*)a.ad.a + ((int64_t)t.adapter * a.ad.rank + min(16 * m + i, rank - 1)) * d_in + kg;
 
-  f32x4_t acc[RT][CT] = {};
-  const int steps = (d_in + 31) / 32, parts = a.splits * NW, p = part * NW + wave;
+  f32x4_t acc[RT] = {};
+  const int steps = (d_in + 31) / 32, parts = a.splits * kFewWaves, p = blockIdx.y * kFewWaves + wave;
   const int k0 = (int)((int64_t)steps * p / parts) * 32, k1 = min((int)((int64_t)steps * (p + 1) / parts) * 32, d_in);
   const int whole = k0 + (k1 - k0) / (32 * U) * (32 * U);
-  struct Batch { u32x4_t x[U][CT], w[U][RT]; };
+  struct Batch { u32x4_t x[U], w[U][RT]; };
   const auto load = [&](Batch& b, int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int c = 0; c < CT; ++c) b.x[u][c] = load8(x[c], k + 32 * u);
+      b.x[u] = load8(x, k + 32 * u);
 #pragma unroll
       for (int m = 0; m < RT; ++m)
         if (16 * m < rank) b.w[u][m] = load8(w[m], k + 32 * u);
@@ -176,11 +162,9 @@ __device__ __forceinline__ void shrink(const AdapterArgs& a, const Tile<CT>& t, 
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank)
-#pragma unroll
-          for (int c = 0; c < CT; ++c) acc[m][c] = mma<DT>(b.w[u][m], b.x[u][c], acc[m][c]);
+        if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m], b.x[u], acc[m]);
   };
-  if constexpr (RT + CT > 8 || (CT > 1 && !ADBUF)) {                                     // no registers left to load ahead
+  if constexpr (RT > 4) {                                          // no registers left to load ahead
     for (int k = k0; k < whole; k += 32 * U) {
       Batch now;
       load(now, k);
@@ -197,68 +181,115 @@ __device__ __forceinline__ void shrink(const AdapterArgs& a, const Tile<CT>& t, 
     multiply(now);
   }
   for (int k = whole; k < k1; k += 32) {                           // fewer than U steps, the last of fewer inputs
-    u32x4_t xv[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) xv[c] = load8(x[c] - kg, k + kg, d_in);
+    const u32x4_t xv = load8(x - kg, k + kg, d_in);
 #pragma unroll
     for (int m = 0; m < RT; ++m)
-      if (16 * m < rank) {
-        const u32x4_t wv = load8(w[m] - kg, k + kg, d_in);
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[m][c] = mma<DT>(wv, xv[c], acc[m][c]);
-      }
+      if (16 * m < rank) acc[m] = mma<DT>(load8(w[m] - kg, k + kg, d_in), xv, acc[m]);
   }
 
   // The waves' sums added up, 16 values of t at a time.
-  float* out = a.t + (int64_t)part * a.n_rows * a.t_stride;
-  if (wave == 0 && lane < 16) {
-#pragma unroll
-    for (int c = 0; c < CT; ++c) slots[16 * c + lane] = t.row[c];
-  }
+  float* out = a.t + (int64_t)blockIdx.y * a.n_rows * a.t_stride;
+  if (threadIdx.x < 16) slots[threadIdx.x] = t.row[0];
 #pragma unroll
   for (int m = 0; m < RT; ++m) {
     if (16 * m >= rank) break;                                     // the whole workgroup
-#pragma unroll
-    for (int c = 0; c < CT; ++c) *(f32x4_t*)&lds[m % 2][wave][c * 256 + lane * 4] = acc[m][c];
+    *(f32x4_t*)&lds[m % 2][wave][lane * 4] = acc[m];
     __syncthreads();
-    for (int e = threadIdx.x; e < CT * 256; e += NW * 64) {
+    for (int e = threadIdx.x; e < 256; e += 64 * kFewWaves) {
       float s = 0.f;
 #pragma unroll
-      for (int n = 0; n < NW; ++n) s += lds[m % 2][n][e];
-      const int l = e / 4 % 64, slot = e / 256 * 16 + l % 16;
+      for (int n = 0; n < kFewWaves; ++n) s += lds[m % 2][n][e];
+      const int l = e / 4, slot = l % 16;
       if (slot < t.count) out[(int64_t)slots[slot] * a.t_stride + 16 * m + l / 16 * 4 + e % 4] = s;
     }
   }
 }
 
-// Few rows: blockIdx.x is the row that a tile starts with.
+// Many rows: blockIdx.x is a tile of 64 rows, blockIdx.y a part of the inputs, a wave for 16 rows. Steps of 64 inputs go
+// through LDS, where eight lanes side by side write 128 bytes of a row: rows side by side in the lanes, as
+// the matrix instructions take them, would make every lane an access of its own to the vector cache. The eight pieces of
+// a row are swapped by the row against bank conflicts.
 template <int DT, int RT>
-__global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
-  __shared__ __align__(16) float lds[2][kFewWaves][256];
-  __shared__ int slots[16];
-  Tile<1> t;
-  if (tile_at(a, blockIdx.x, t)) shrink<DT, RT, 1, kFewWaves>(a, t, blockIdx.y, lds, slots);
-}
-// Many: blockIdx.x is a tile of 64 rows.
-template <int DT, int RT, int CT>
-__global__ __launch_bounds__(64 * kManyWaves, ADOCC) void shrink_many(AdapterArgs a) {
-  __shared__ __align__(16) float lds[2][kManyWaves][CT * 256];
-  __shared__ int slots[16 * CT];
+__global__ __launch_bounds__(256, 2) void shrink_many(AdapterArgs a) {
+  constexpr int kAhead = RT <= 2 ? 2 : 1;                          // steps whose loads are under way
+  constexpr int kW = (RT + 1) / 2;                                 // pieces of A of a thread
+  __shared__ u32x4_t xs[2][64 * 8], ws[2][RT * 16 * 8];
   if ((int)blockIdx.x >= *a.n_tiles) return;
   const int4 tile = a.tiles[blockIdx.x];
-  if (tile.x < 0) return;
-  for (int first = 0; first < tile.z; first += 16 * CT) {
-    Tile<CT> t;
-    t.adapter = tile.x;
-    t.count = min(tile.z - first, 16 * CT);
+  const int rank = own_rank(a, tile.x);
+  if (rank == 0) return;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, q = lane / 16, d_in = a.ad.d_in;
+  // This thread's pieces: of rows r and r + 32 of x, and of rows r + 32 j of A.
+  const int r = threadIdx.x / 8, piece = threadIdx.x % 8;
+  const uint16_t* x[2];
+  const uint16_t* w[kW];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const int slot = 16 * c + threadIdx.x % 16;
-      t.row[c] = a.order[tile.y + first + (slot < t.count ? slot : 0)];
+  for (int j = 0; j < 2; ++j)
+    x[j] = (const uint16_t*)a.x + a.order[tile.y + min(r + 32 * j, tile.z - 1)] * a.x_stride;
+#pragma unroll
+  for (int j = 0; j < kW; ++j) w[j] = (const uint16_t*)a.ad.a + ((int64_t)tile.x * a.ad.rank + min(r + 32 * j, rank - 1)) * d_in;
+  const int steps = d_in / 64;                                     // whole ones; the rest is the last part's
+  const int s0 = (int)((int64_t)steps * blockIdx.y / a.splits), s1 = (int)((int64_t)steps * (blockIdx.y + 1) / a.splits);
+
+  struct Step { u32x4_t x[2], w[kW]; };
+  const auto load = [&](Step& b, int s) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b.x[j] = load8(x[j], 64 * s + 8 * piece);
+#pragma unroll
+    for (int j = 0; j < kW; ++j)
+      if (32 * j < rank) b.w[j] = load8(w[j], 64 * s + 8 * piece);
+  };
+  const auto place = [&](const Step& b, int n) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) xs[n][(r + 32 * j) * 8 + (piece ^ (r % 8))] = b.x[j];
+#pragma unroll
+    for (int j = 0; j < kW; ++j)
+      if (RT % 2 == 0 || r < 16) ws[n][(r + 32 * j) * 8 + (piece ^ (r % 8))] = b.w[j];
+  };
+  f32x4_t acc[RT] = {};
+  const auto multiply = [&](int n) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = i * 8 + ((4 * h + q) ^ (i % 8));
+      const u32x4_t xv = xs[n][wave * 128 + at];
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank) acc[m] = mma<DT>(ws[n][m * 128 + at], xv, acc[m]);
     }
-    shrink<DT, RT, CT, kManyWaves>(a, t, blockIdx.y, lds, slots);
-    __syncthreads();
+  };
+  Step ahead[kAhead];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n)
+    if (s0 + n < s1) load(ahead[n], s0 + n);
+#pragma unroll 1
+  for (int first = s0; first < s1; first += 2 * kAhead) {
+#pragma unroll
+    for (int n = 0; n < 2 * kAhead; ++n) {
+      const int s = first + n;
+      if (s >= s1) break;
+      place(ahead[n % kAhead], n % 2);
+      if (s + kAhead < s1) load(ahead[n % kAhead], s + kAhead);
+      __syncthreads();
+      multiply(n % 2);
+    }
   }
+  if (d_in % 64 && blockIdx.y + 1 == (unsigned)a.splits) {
+    __syncthreads();
+    Step b;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b.x[j] = load8(x[j], 64 * steps + 8 * piece, d_in);
+#pragma unroll
+    for (int j = 0; j < kW; ++j)
+      if (32 * j < rank) b.w[j] = load8(w[j], 64 * steps + 8 * piece, d_in);
+    place(b, 0);
+    __syncthreads();
+    multiply(0);
+  }
+  if (16 * wave + i >= tile.z) return;
+  float* out = a.t + ((int64_t)blockIdx.y * a.n_rows + a.order[tile.y + 16 * wave + i]) * a.t_stride + 4 * q;
+#pragma unroll
+  for (int m = 0; m < RT; ++m)
+    if (16 * m < rank) *(f32x4_t*)(out + 16 * m) = acc[m];
 }
 
 // Eight binary32 values as 16-bit parts that add up to them: three for bf16 (exactly, short of subnormals), two for
@@ -276,20 +307,28 @@ template <> struct Parts<AQMB_F16> {
   static __device__ __forceinline__ float lo(uint32_t w) { return f16lo(w); }
   static __device__ __forceinline__ float hi(uint32_t w) { return f16hi(w); }
 };
-// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave, into to[kt][part][lane]; what
-// the results are to be multiplied by into back[slot].
-template <int DT, int KT>
-__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, u32x4_t (*to)[Parts<DT>::kN][64],
-                                         float* back) {
+// What a wave of the second launch keeps in LDS: the factor of 16 rows' results; 128 outputs' weights of a step of 32 of the
+// rank, output 8 c + n as row 16 n + c, where the matrix instructions take it, 64 bytes a row, the four pieces swapped by c / 4
+// against bank conflicts; and t's operands of every step.
+template <int DT>
+struct ExpandLds {
+  float back[16];
+  u32x4_t w[8][68];
+  u32x4_t t[1][Parts<DT>::kN][64];
+};
+template <int DT>
+constexpr size_t expand_lds(int steps) { return sizeof(ExpandLds<DT>) + (steps - 1) * sizeof(ExpandLds<DT>::t); }
+
+// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave.
+template <int DT>
+__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, ExpandLds<DT>& lds) {
   typedef Parts<DT> P;
-  const int lane = threadIdx.x % 64, q = lane / 16;
+  const int lane = threadIdx.x % 64, q = lane / 16, steps = (rank + 31) / 32;
   const float* tp = a.t + (int64_t)row * a.t_stride + 8 * q;
-  float v[KT][8];
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt) {
-    // Partial sums added up, scaled, 0 from the adapter's rank on.
+  // Partial sums added up, scaled, 0 from the adapter's rank on.
+  const auto values = [&](int kt, float* v) {
     f32x4_t lo[kMaxSplits] = {}, hi[kMaxSplits] = {};
-    if (32 * kt < a.ad.rank && 32 * kt + 8 * q < a.t_stride) {      // not by rank, which may still be on its way
+    if (32 * kt + 8 * q < a.t_stride) {                // not by rank, which may still be on its way
 #pragma unroll
       for (int p = 0; p < kMaxSplits; ++p)
         if (p < a.splits) {
@@ -299,40 +338,49 @@ __device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank
     }
 #pragma unroll
     for (int p = 1; p < kMaxSplits; ++p) lo[0] += lo[p], hi[0] += hi[p];
+    const f32x4_t l = lo[0], h = hi[0];
+    const float f[8] = {l.x, l.y, l.z, l.w, h.x, h.y, h.z, h.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[kt][j] = 32 * kt + 8 * q + j < rank ? (j < 4 ? lo[0][j % 4] : hi[0][j % 4]) * scale : 0.f;
-  }
+    for (int j = 0; j < 8; ++j) v[j] = 32 * kt + 8 * q + j < rank ? f[j] * scale : 0.f;
+  };
+  float v[8], fwd = 1.f;
+  values(0, v);
   if constexpr (DT == AQMB_F16) {
     // By a power of two, so that the row's largest magnitude is in [2^13, 2^14): in fp16's range, the parts far
     // from its subnormals.
     uint32_t big = 0;
+    const auto largest = [&](const float* f) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) big = max(big, __builtin_bit_cast(uint32_t, v[kt][j]) & 0x7FFFFFFFu);
+      for (int j = 0; j < 8; ++j) big = max(big, __builtin_bit_cast(uint32_t, f[j]) & 0x7FFFFFFFu);
+    };
+    largest(v);
+    for (int kt = 1; kt < steps; ++kt) {
+      float f[8];
+      values(kt, f);
+      largest(f);
+    }
     big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 16), (int)big));
     big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 32), (int)big));
     const int ex = min(max((int)(big >> 23), 14), 254);    // the exponent that goes to 13
-    const float fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
-    if (lane < 16) back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[kt][j] *= fwd;
+    fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
+    if (lane < 16) lds.back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
   }
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
+  for (int kt = 0;;) {
 #pragma unroll
     for (int p = 0; p < P::kN; ++p) {
-      u32x4_t w;
+      uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        w[j] = P::pack(v[kt][2 * j], v[kt][2 * j + 1]);
-        v[kt][2 * j] -= P::lo(w[j]);
-        v[kt][2 * j + 1] -= P::hi(w[j]);
+        if (p == 0 && DT == AQMB_F16) v[2 * j] *= fwd, v[2 * j + 1] *= fwd;
+        w[j] = P::pack(v[2 * j], v[2 * j + 1]);
+        v[2 * j] -= P::lo(w[j]);
+        v[2 * j + 1] -= P::hi(w[j]);
       }
-      to[kt][p][lane] = w;
+      lds.t[kt][p][lane] = u32x4_t{w[0], w[1], w[2], w[3]};
     }
+    if (++kt >= steps) return;
+    values(kt, v);
+  }
 }
 
 // 8 neighbouring outputs of a row as they are stored (16 bits or, kWide, binary32).
@@ -362,9 +410,16 @@ __device__ __forceinline__ Eight<kWide> load_y(const void* row, int o, int n) {
   }
   return r;
 }
-template <bool kWide, bool kEights>
+template <bool kWide, bool kEights, bool kStream>
 __device__ __forceinline__ void store_y(void* row, int o, int n, const Eight<kWide>& r) {
+  typedef u32x4_t __attribute__((aligned(2))) Unaligned;
   if (o >= n) return;
+  if (kStream && kEights) {
+#pragma unroll
+    for (int h = 0; h < (kWide ? 2 : 1); ++h)
+      __builtin_nontemporal_store(r.v[h], (Unaligned*)((char*)row + (int64_t)o * (kWide ? 4 : 2) + 16 * h));
+    return;
+  }
   if constexpr (kWide) {
     float* p = (float*)row + o;
     if (kEights || o + 8 <= n) {
@@ -416,36 +471,31 @@ __device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], in
   }
 }
 
-// What a wave of the second launch keeps in LDS: t's operands, and 128 outputs' weights of a step of 32, output 8 c + n as row
-// 16 n + c, where the matrix instructions take it; 64 bytes a row, the four pieces swapped by c / 4 against bank conflicts.
-template <int DT, int KT>
-struct ExpandLds {
-  u32x4_t t[KT][Parts<DT>::kN][64];
-  float back[16];
-  u32x4_t w[8][68];
-};
 // Outputs o0 .. o1 - 1 (o0 a multiple of 128) of up to 16 rows that share an adapter, by one wave. Lane (q, c) of 4 x 16 has
 // outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and writes 256 bytes of a row at once
 // (with lanes side by side on different rows every lane was an access of its own to the vector cache, which bound
 // the kernel: 8192 rows of 4096 outputs 45 us).
-template <int DT, bool kWide, int KT, bool kEights>
-__device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, int o0, int o1, ExpandLds<DT, KT>& lds) {
+template <int DT, bool kWide, bool kEights, bool kStream>
+__device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, int o0, int o1, ExpandLds<DT>& lds) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
   const int lane = threadIdx.x % 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
   const int rank = own_rank(a, t.adapter);
   if (rank == 0 && a.base == a.out) return;
-  int64_t row[4];
+  int row[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row[0]);
+  // A value that the compiler takes for new in every step: addresses made from it are not kept in registers between steps.
+  const auto fresh = [](int v) { asm volatile("" : "+v"(v)); return v; };
   const auto load_rows = [&](Eight<kWide>* y, int o) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      y[j] = load_y<kWide, kEights>((const char*)a.base + row[j] * a.base_stride * kSize, o + 8 * c, d_out);
+      y[j] = load_y<kWide, kEights>((const char*)a.base + fresh(row[j]) * (a.base_stride * kSize), o + 8 * c, d_out);
   };
   const auto store_rows = [&](const Eight<kWide>* y, int o) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (4 * q + j < t.count) store_y<kWide, kEights>((char*)a.out + row[j] * a.out_stride * kSize, o + 8 * c, d_out, y[j]);
+      if (4 * q + j < t.count)
+        store_y<kWide, kEights, kStream>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
   };
   Eight<kWide> y[4];
   if (rank == 0) {
@@ -460,22 +510,21 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
   const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * stack;
   const auto shift_of = [&](int kt) { const int left = (kt == 0 ? stack : rank) - 32 * kt; return left > 16 ? 2 : left > 8 ? 1 : 0; };
   const auto load_w = [&](u32x4_t* w, int o, int kt) {
-    const int shift = shift_of(kt);
+    const int shift = shift_of(kt), l = fresh(lane), k = 32 * kt + 8 * (l & ((1 << shift) - 1));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
-      const int at = 64 * j + lane, k = 32 * kt + 8 * (at & ((1 << shift) - 1));
-      const uint16_t* r = b + (int64_t)min(o + (at >> shift), d_out - 1) * stack;
-      if constexpr (kEights) w[j] = load8(r, min(k, stack - 8));
-      else w[j] = stack >= 8 ? load8_moved(r, k, stack) : load8(r, k, stack);
+      const uint32_t r = min(o + ((64 * j + l) >> shift), d_out - 1) * (uint32_t)stack;     // below 2^31
+      if constexpr (kEights) w[j] = load8(b, r + min(k, stack - 8));
+      else w[j] = stack >= 8 ? load8_moved(b + r, k, stack) : load8(b + r, k, stack);
     }
   };
   const auto place_w = [&](const u32x4_t* w, int kt) {
-    const int shift = shift_of(kt);
+    const int shift = shift_of(kt), l = fresh(lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
-      const int at = 64 * j + lane, o = at >> shift, piece = at & ((1 << shift) - 1);
+      const int o = (64 * j + l) >> shift, piece = l & ((1 << shift) - 1);
       lds.w[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
     }
   };
@@ -490,15 +539,13 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
   u32x4_t w[8];
   load_w(w, o0, 0);
   load_rows(y, o0);
-  operands<DT, KT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds.t, lds.back);
+  operands<DT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds);
 
   for (int o = o0; o < o1; o += 128) {
     const bool more = o + 128 < o1;
     f32x4_t acc[8] = {};
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      if (32 * kt >= rank) break;
-      const bool last = kt + 1 == KT || 32 * (kt + 1) >= rank;
+    for (int kt = 0; 32 * kt < rank; ++kt) {
+      const bool last = 32 * (kt + 1) >= rank;
       lds_order();
       place_w(w, kt);
       if (!last) load_w(w, o, kt + 1);
@@ -522,26 +569,30 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
   }
 }
 
-// Few rows: blockIdx.y is the row that a tile starts with.
-template <int DT, bool kWide, int KT, bool kEights>
+// A wave's part of the workgroup's LDS.
+template <int DT>
+__device__ __forceinline__ ExpandLds<DT>& own_lds(const AdapterArgs& a) {
+  extern __shared__ __align__(16) char all[];
+  return *(ExpandLds<DT>*)(all + threadIdx.x / 64 * expand_lds<DT>((a.ad.rank + 31) / 32));
+}
+// Few rows: blockIdx.y is the row that a tile starts with, a wave for a.per_wave outputs.
+template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
-  __shared__ ExpandLds<DT, KT> lds[4];
-  const int wave = threadIdx.x / 64, o0 = (blockIdx.x * 4 + wave) * a.per_wave;
+  const int64_t o0 = ((int64_t)blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64) * a.per_wave;
   Tile<1> t;
   if (tile_at(a, blockIdx.y, t) && o0 < a.ad.d_out)
-    expand<DT, kWide, KT, kEights>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), lds[wave]);
+    expand<DT, kWide, kEights, false>(a, t, (int)o0, (int)min(o0 + a.per_wave, (int64_t)a.ad.d_out), own_lds<DT>(a));
 }
-// Many: blockIdx.x is a tile of 64 rows, a wave for 16.
-template <int DT, bool kWide, int KT, bool kEights>
+// Many: a wave for 16 rows of a tile of 64, blockIdx.y the outputs.
+template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
-  __shared__ ExpandLds<DT, KT> lds[4];
-  const int wave = threadIdx.x / 64, o0 = blockIdx.y * a.per_wave;
-  if ((int)blockIdx.x >= *a.n_tiles) return;
-  const int4 tile = a.tiles[blockIdx.x];
-  if (16 * wave >= tile.z) return;
-  const int slot = 16 * wave + threadIdx.x % 16;
-  const Tile<1> t = {tile.x, min(tile.z - 16 * wave, 16), {a.order[tile.y + (slot < tile.z ? slot : 16 * wave)]}};
-  expand<DT, kWide, KT, kEights>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), lds[wave]);
+  const int wave = blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64, first = wave % 4 * 16, o0 = blockIdx.y * a.per_wave;
+  if (wave / 4 >= *a.n_tiles) return;
+  const int4 tile = a.tiles[wave / 4];
+  if (first >= tile.z) return;
+  const int slot = first + threadIdx.x % 16;
+  const Tile<1> t = {tile.x, min(tile.z - first, 16), {a.order[tile.y + (slot < tile.z ? slot : first)]}};
+  expand<DT, kWide, kEights, true>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), own_lds<DT>(a));
 }
 
 // Many rows sorted by adapter (those without one last), and cut into tiles of up to 64 (adapter, first, count): one workgroup
@@ -552,34 +603,35 @@ __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
   const int n_bins = a.ad.n_adapters + 1, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   for (int i = threadIdx.x; i < n_bins; i += 1024) bins[i] = 0;
   __syncthreads();
-  // use(row, its place in its bin); the places of a wave's rows that all have one adapter are taken at once.
-  const auto take = [&](auto use) {
-    for (int r0 = 0; r0 < a.n_rows; r0 += 1024 * kEach) {
-      int n[kEach];
+  // The bins of kEach rows a thread, and each one's place in its bin; a wave's rows that all have one adapter take
+  // theirs at once.
+  int n[kEach], at[kEach];
+  const auto take = [&](int r0) {
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int r = r0 + 1024 * j + threadIdx.x;
-        n[j] = r < a.n_rows ? a.index[r] : -1;
-        if ((unsigned)n[j] >= (unsigned)a.ad.n_adapters) n[j] = a.ad.n_adapters;
-      }
+    for (int j = 0; j < kEach; ++j) {
+      const int r = r0 + 1024 * j + threadIdx.x;
+      n[j] = r < a.n_rows ? a.index[r] : -1;
+      if ((unsigned)n[j] >= (unsigned)a.ad.n_adapters) n[j] = a.ad.n_adapters;
+    }
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int r = r0 + 1024 * j + threadIdx.x;
-        const uint64_t in = __ballot(r < a.n_rows);
-        if (in == 0) break;
-        const int first = __builtin_amdgcn_readfirstlane(n[j]);
-        int at = 0;
-        if ((in & ~__ballot(n[j] == first)) == 0) {
-          if (lane == 0) at = atomicAdd(&bins[first], __builtin_popcountll(in));
-          at = __builtin_amdgcn_readfirstlane(at) + lane;
-        } else if (r < a.n_rows) {
-          at = atomicAdd(&bins[n[j]], 1);
-        }
-        if (r < a.n_rows) use(r, at);
-      }
+    for (int j = 0; j < kEach; ++j) {
+      const bool in = r0 + 1024 * j + threadIdx.x < a.n_rows;
+      const uint64_t all = __ballot(in);
+      const bool one = (all & ~__ballot(n[j] == __builtin_amdgcn_readfirstlane(n[j]))) == 0;
+      at[j] = 0;
+      if (in && (!one || lane == 0)) at[j] = atomicAdd(&bins[n[j]], one ? __builtin_popcountll(all) : 1);
+      if (one) at[j] = __builtin_amdgcn_readfirstlane(at[j]) + lane;
     }
   };
-  take([](int, int) {});
+  const auto place = [&](int r0) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int r = r0 + 1024 * j + threadIdx.x;
+      if (r < a.n_rows) a.order[at[j]] = r;
+    }
+  };
+  const bool once = a.n_rows <= 1024 * kEach;          // the places of the first pass are kept
+  for (int r0 = 0; r0 < a.n_rows; r0 += 1024 * kEach) take(r0);
   __syncthreads();
   // Each thread's bins, neighbours; their rows and tiles before it.
   const int per = (n_bins + 1023) / 1024, b0 = threadIdx.x * per, b1 = min(b0 + per, n_bins);
@@ -609,31 +661,36 @@ __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
   }
   if (threadIdx.x == 1023) *a.n_tiles = before[1];
   __syncthreads();
-  take([&](int r, int at) { a.order[at] = r; });
+  if (once) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) at[j] += bins[n[j]];
+    place(0);
+  } else {
+    for (int r0 = 0; r0 < a.n_rows; r0 += 1024 * kEach) {
+      take(r0);
+      place(r0);
+    }
+  }
 }
 
 template <int DT, int RT>
 hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
   if (p.few) shrink_few<DT, RT><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
-  else shrink_many<DT, RT, (RT <= 4 ? 4 : RT <= 8 ? 2 : 1)><<<dim3(p.tiles, p.splits), 64 * kManyWaves, 0, st>>>(a);
-  return hipGetLastError();
-}
-template <int DT, bool kWide, int KT, bool kEights>
-hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
-  if (p.few) expand_few<DT, kWide, KT, kEights><<<dim3((parts + 3) / 4, a.n_rows), 256, 0, st>>>(a);
-  else expand_many<DT, kWide, KT, kEights><<<dim3(p.tiles, parts), 256, 0, st>>>(a);
+  else shrink_many<DT, RT><<<dim3(p.tiles, p.splits), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 template <int DT, bool kWide, bool kEights>
-hipError_t by_rank(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  const int r = a.ad.rank;
-  return r <= 32 ? go_expand<DT, kWide, 1, kEights>(a, p, st) : r <= 64 ? go_expand<DT, kWide, 2, kEights>(a, p, st)
-         : r <= 128 ? go_expand<DT, kWide, 4, kEights>(a, p, st) : go_expand<DT, kWide, 8, kEights>(a, p, st);
+hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
+  const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
+  const int steps = (a.ad.rank + 31) / 32, waves = steps <= 2 ? 4 : steps <= 4 ? 2 : 1;   // within 64 KiB of LDS
+  const size_t lds = waves * expand_lds<DT>(steps);
+  if (p.few) expand_few<DT, kWide, kEights><<<dim3((parts + waves - 1) / waves, a.n_rows), 64 * waves, lds, st>>>(a);
+  else expand_many<DT, kWide, kEights><<<dim3(p.tiles * (4 / waves), parts), 64 * waves, lds, st>>>(a);
+  return hipGetLastError();
 }
 template <int DT, bool kWide>
-hipError_t by_rank(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  return a.ad.rank % 8 || a.ad.d_out % 8 ? by_rank<DT, kWide, false>(a, p, st) : by_rank<DT, kWide, true>(a, p, st);
+hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
+  return a.ad.rank % 8 || a.ad.d_out % 8 ? go_expand<DT, kWide, false>(a, p, st) : go_expand<DT, kWide, true>(a, p, st);
 }
 template <int DT>
 hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStream_t st) {
@@ -646,11 +703,14 @@ hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStr
   e = r <= 16 ? go_shrink<DT, 1>(a, p, st) : r <= 32 ? go_shrink<DT, 2>(a, p, st)
                        : r <= 64 ? go_shrink<DT, 4>(a, p, st) : r <= 128 ? go_shrink<DT, 8>(a, p, st) : go_shrink<DT, 16>(a, p, st);
   if (e != hipSuccess) return e;
-  return y == AQMB_F32 ? by_rank<DT, true>(a, p, st) : by_rank<DT, false>(a, p, st);
+  return y == AQMB_F32 ? go_expand<DT, true>(a, p, st) : go_expand<DT, false>(a, p, st);
 }
 
 }  // namespace
 
+// Few: what one wave's votes sort. Above, a sort of its own (4 us for 100 rows, 9 for 8192) and tiles of 64 rows are
+// cheaper than a look at 64 rows for every 16 (1024 rows of 4 adapters: 22 us against 57, 300 rows 20 and 14, 64 of 64 adapters
+// 150 and 18). Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   AdapterPlan p;
   const int steps = (ad.d_in + 31) / 32;
@@ -658,12 +718,12 @@ AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   const int groups = n_rows < ad.n_adapters + 1 ? n_rows : ad.n_adapters + 1;
   p.tiles = groups + (n_rows - groups) / 64;
   if (p.few) {
-    p.splits = steps / (kFewWaves * TUNE("AD_STEPS", 4));
+    p.splits = steps / (kFewWaves * 4);
     p.per_wave = 128;
   } else {
-    p.splits = TUNE("AD_WG", 512) / ((n_rows + kRows - 1) / kRows);
+    p.splits = 512 / ((n_rows + kRows - 1) / kRows);
     if (p.splits > steps / 16) p.splits = steps / 16;
-    p.per_wave = TUNE("AD_PWM", 256);
+    p.per_wave = 256;
   }
   if (p.splits > kMaxSplits) p.splits = kMaxSplits;
   if (p.splits < 1) p.splits = 1;
