@@ -2,8 +2,8 @@
 //
 // Two launches: t = A_n x (binary32, partial sums over parts of the inputs side by side in the workspace), then
 // out = base + B_n (s_n t). Rows that share an adapter are the columns of matrix instructions, 16 each, with 16 rows of A
-// or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows (up to
-// 64): every wave finds its 16 by votes over the indexes; the adapters' bytes and the latency of two launches bound them
+// or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows:
+// every wave finds its 16 by votes over 64 rows' indexes; the adapters' bytes and the latency of two launches bound them
 // (one row, rank 16, 4096 x 4096: 3.7 + 5.1 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
 // and out (8192 rows, rank 32, 4096 x 4096: sort 9 us, t 14.6 us, 4.6 TB/s, the outputs 38 us, 3.5 TB/s).
 #include "device.h"
@@ -708,13 +708,15 @@ hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStr
 
 }  // namespace
 
-// Few: what one wave's votes sort. Above, a sort of its own (4 us for 100 rows, 9 for 8192) and tiles of 64 rows are
-// cheaper than a look at 64 rows for every 16 (1024 rows of 4 adapters: 22 us against 57, 300 rows 20 and 14, 64 of 64 adapters
-// 150 and 18). Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
+// Few rows take a look at 64 rows for every tile of 16; above 192 a sort of its own (4 us for 100 rows, 9 for 8192) and tiles of 64
+// rows are cheaper. Rank 16, 4096 x 4096, 4 adapters in spans: 128 rows 12.2 us against 19.3, 256 17.9 and 19.8, 512 32.1 and
+// 20.2; 64 adapters in any order: 15.3 and 24.8, 25.1 and 27.4, 43.3 and 29.5; rank 64, 11008 outputs, 8 adapters: 26.9 and 29.3,
+// 38.3 and 33.6, 65 and 46. Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
+constexpr int kFewRows = 192;
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   AdapterPlan p;
   const int steps = (ad.d_in + 31) / 32;
-  p.few = n_rows <= kRows;
+  p.few = n_rows <= kFewRows;
   const int groups = n_rows < ad.n_adapters + 1 ? n_rows : ad.n_adapters + 1;
   p.tiles = groups + (n_rows - groups) / 64;
   if (p.few) {

@@ -4,9 +4,10 @@
 //   lse = scale M + log s,  log p_t = scale (x_t - M) - log s,  entropy = log s - log 2 u / s
 //
 // A lane keeps M, s and u of what it has seen and brings them to a new M once per tile. The largest n_top values are
-// kept per wave as sorted 64-bit keys (the value's order, then the lower index) in LDS: values above the last of them
-// are few once some tiles have passed, so that a tile mostly costs one comparison of its largest value. Few rows are cut
-// into chunks, which a second launch joins. Bound by the logits' bytes for many rows, by latency for few.
+// kept per wave as sorted 64-bit keys (the value's order, then the lower index) in LDS; a new value has to reach the last of
+// them, or that of the workgroup's other waves, and few do. Few rows are cut into chunks, which a second launch joins.
+// Many rows without top values are bound by the vector instructions and the logits' bytes alike (2600 rows of 50001 bf16: 63 us, 4.1
+// TB/s, 10 instructions a value), with 20 top values by the keys (4096 rows of 32000: 103 us); few rows by latency.
 #include "device.h"
 #include "ops.h"
 #include "wave.h"
@@ -19,21 +20,36 @@ namespace aqmb {
 
 namespace {
 
+typedef uint64_t u64x2_t __attribute__((ext_vector_type(2)));
 struct __attribute__((packed, aligned(2))) Raw16 { uint32_t w[4]; };
 
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kInf = __builtin_inff();
+constexpr float kLowest = -3.402823466e38f;
 constexpr float kFar = -1000.f;  // 2^t is 0 there and below: u's factor stays finite
 constexpr int kList = 128;       // keys a wave may hold before it sorts: the top ones and a wave's 64 more
 
 template <int DT> constexpr int kEach = DT == AQMB_F32 ? 4 : 8;     // values of a 16-byte load
-constexpr int kLoads = 4;                                           // loads of a lane in a tile
-template <int DT> constexpr int kTile = 64 * kEach<DT> * kLoads;    // values of a wave's tile
+template <int DT> constexpr int kPiece = 64 * kEach<DT>;            // values of a wave's load
 
 template <int DT>
 __device__ __forceinline__ float value(const void* row, int i) {
   if constexpr (DT == AQMB_F32) return ((const float*)row)[i];
   else if constexpr (DT == AQMB_F16) return f16_to_f32(((const uint16_t*)row)[i]);
   else return bf16lo(((const uint16_t*)row)[i]);
+}
+
+template <int DT>
+__device__ __forceinline__ void widen(const Raw16& r, float* x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w = r.w[j];
+    if constexpr (DT == AQMB_F32) {
+      x[j] = __builtin_bit_cast(float, w);
+    } else {
+      x[2 * j] = DT == AQMB_F16 ? f16lo(w) : bf16lo(w);
+      x[2 * j + 1] = DT == AQMB_F16 ? f16hi(w) : bf16hi(w);
+    }
+  }
 }
 
 struct Run { float m, s, u; };
@@ -44,16 +60,15 @@ __device__ __forceinline__ Run join(const Run& a, const Run& b, float c) {
   const float fa = __builtin_amdgcn_exp2f(ta), fb = __builtin_amdgcn_exp2f(tb);
   return {m, fa * a.s + fb * b.s, fa * fmaf(fmaxf(ta, kFar), a.s, a.u) + fb * fmaf(fmaxf(tb, kFar), b.s, b.u)};
 }
-__device__ __forceinline__ Run over_wave(Run r, float c) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int at = 4 * ((threadIdx.x % 64) ^ d);
-    const auto from = [&](float x) {
-      return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(at, __builtin_bit_cast(int, x)));
-    };
-    r = join(r, Run{from(r.m), from(r.s), from(r.u)}, c);
-  }
-  return r;
+// All lanes' runs joined: the largest m first, then what they are at that.
+__device__ __forceinline__ Run over_wave(const Run& r, float c) {
+  const float m = __builtin_bit_cast(float, over_lanes<64>(__builtin_bit_cast(uint32_t, r.m), [](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  }));
+  const float t = (r.m - (m == -kInf ? 0.f : m)) * c, f = __builtin_amdgcn_exp2f(t);
+  const float s = f * r.s, u = f * fmaf(fmaxf(t, kFar), r.s, r.u);
+  return {m, __builtin_bit_cast(float, over_lanes<64>(__builtin_bit_cast(uint32_t, s), add_floats)),
+          __builtin_bit_cast(float, over_lanes<64>(__builtin_bit_cast(uint32_t, u), add_floats))};
 }
 
 // Larger for a larger value and, among equal ones (-0 and 0 are), for a lower index. Never 0 for a value above -infinity.
@@ -71,27 +86,85 @@ __device__ __forceinline__ void lds_order() {      // a wave's LDS accesses run 
   __builtin_amdgcn_wave_barrier();
 }
 
-// The list's n keys sorted, largest first, cut to `top`; the new n. Each key's place is the number of larger ones.
-__device__ __forceinline__ int sort_list(uint64_t* list, int n, int top) {
-  const int lane = threadIdx.x % 64;
-  lds_order();
-  const uint64_t a = lane < n ? list[lane] : 0, b = lane + 64 < n ? list[lane + 64] : 0;
-  int pa = 0, pb = 0;
-  for (int i = 0; i < n; ++i) {
-    const uint64_t k = list[i];
-    pa += k > a;
-    pb += k > b;
+// A wave's largest keys, in LDS: n of them, of which a new one has to reach `least`.
+struct TopList {
+  uint64_t* list;              // of kList, 16-byte aligned
+  int n, top;
+  uint64_t least;
+
+  // The list's keys sorted, largest first, and cut to `top`; if so many are there, `least` is the last. Each key's place is
+  // the number of larger ones.
+  __device__ __forceinline__ void sort() {
+    const int lane = threadIdx.x % 64;
+    if (lane < 8 && n + lane < kList) list[n + lane] = 0;        // the loop below counts in eights
+    lds_order();
+    const uint64_t a = lane < n ? list[lane] : 0, b = lane + 64 < n ? list[lane + 64] : 0;
+    int pa = 0, pb = 0;
+    for (int i = 0; i < n; i += 8) {
+      u64x2_t k[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = *(const u64x2_t*)(list + i + 2 * j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        pa += (k[j].x > a) + (k[j].y > a);
+        if (n > 64) pb += (k[j].x > b) + (k[j].y > b);
+      }
+    }
+    lds_order();
+    if (lane < n && pa < top) list[pa] = a;
+    if (lane + 64 < n && pb < top) list[pb] = b;
+    lds_order();
+    n = min(n, top);
+    if (n == top) least = list[n - 1];
   }
-  lds_order();
-  if (lane < n && pa < top) list[pa] = a;
-  if (lane + 64 < n && pb < top) list[pb] = b;
-  lds_order();
-  return min(n, top);
+  // The keys of the lanes that say so and reach `least`.
+  __device__ __forceinline__ void push(uint64_t key, bool in) {
+    in = in && key >= least;
+    uint64_t mask = __ballot(in);
+    if (mask == 0) return;
+    if (n + __builtin_popcountll(mask) > kList) {
+      sort();
+      in = in && key >= least;
+      mask = __ballot(in);
+    }
+    put(key, mask);
+  }
+  __device__ __forceinline__ void put(uint64_t key, uint64_t mask) {
+    const int lane = threadIdx.x % 64;
+    if (mask >> lane & 1) list[n + __builtin_popcountll(mask & ((1ull << lane) - 1))] = key;
+    n += __builtin_popcountll(mask);
+  }
+  // `least` from one value of every lane, in the order's bits: `top` lanes reach it, if so many lanes have one. Not
+  // quite the largest such bound: its first bits.
+  __device__ __forceinline__ void start(uint32_t o) {
+    uint32_t p = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 18; --bit)
+      if (__builtin_popcountll(__ballot(o >= (p | 1u << bit))) >= top) p |= 1u << bit;
+    least = (uint64_t)p << 32;
+  }
+};
+
+// The first 64 tokens that are asked for and their logits, on their way early; lane l has number l.
+struct Asked {
+  int64_t token;
+  float x;
+};
+template <int DT>
+__device__ __forceinline__ Asked asked(const LogProbArgs& a, int64_t row) {
+  const int lane = threadIdx.x % 64;
+  Asked r = {-1, 0.f};
+  if (lane < a.n_targets) {
+    r.token = a.targets[row * a.n_targets + lane];
+    const char* z = (const char*)a.logits + row * a.stride * (DT == AQMB_F32 ? 4 : 2);
+    if (r.token >= 0 && r.token < a.vocab) r.x = value<DT>(z, (int)r.token);
+  }
+  return r;
 }
 
 // What a row has come to, by one wave: keys sorted in `sorted`, n of them.
 template <int DT>
-__device__ __forceinline__ void finish(const LogProbArgs& a, int64_t row, const Run& r, const uint64_t* sorted, int n) {
+__device__ __forceinline__ void finish(const LogProbArgs& a, int64_t row, const Run& r, const Asked& early, const uint64_t* sorted, int n) {
   const int lane = threadIdx.x % 64;
   const char* z = (const char*)a.logits + row * a.stride * (DT == AQMB_F32 ? 4 : 2);
   const bool bad = !(r.s >= 0.f) || r.m == kInf, none = r.s == 0.f;
@@ -102,9 +175,13 @@ __device__ __forceinline__ void finish(const LogProbArgs& a, int64_t row, const 
     if (a.lse) a.lse[row] = bad ? nan : none ? -kInf : fmaf(a.scale, r.m, ls);
     if (a.entropy) a.entropy[row] = bad ? nan : none ? 0.f : fmaxf(fmaf(-kLn2, r.u / r.s, ls), 0.f);
   }
-  for (int i = lane; i < a.n_targets; i += 64) {
+  const auto answer = [&](int i, int64_t t, float x) {
+    a.logprobs[row * a.n_targets + i] = t < 0 ? 0.f : t >= a.vocab ? nan : log_p(x);
+  };
+  if (lane < a.n_targets) answer(lane, early.token, early.x);
+  for (int i = lane + 64; i < a.n_targets; i += 64) {
     const int64_t t = a.targets[row * a.n_targets + i];
-    a.logprobs[row * a.n_targets + i] = t < 0 ? 0.f : t >= a.vocab ? nan : log_p(value<DT>(z, (int)t));
+    answer(i, t, t >= 0 && t < a.vocab ? value<DT>(z, (int)t) : 0.f);
   }
   if (a.n_top == 0) return;
   int id = -1;
@@ -126,48 +203,58 @@ __device__ __forceinline__ void finish(const LogProbArgs& a, int64_t row, const 
   }
 }
 
-template <int DT, int NT, bool kTop>
+// A wave's tile is kLoads loads.
+template <int DT, int NT, int kLoads, bool kTop>
 __global__ __launch_bounds__(NT) void rows_kernel(LogProbArgs a) {
-  constexpr int kE = kEach<DT>, kN = kE * kLoads, kWaves = NT / 64;
+  constexpr int kE = kEach<DT>, kN = kE * kLoads, kWaves = NT / 64, kTile = kPiece<DT> * kLoads;
   __shared__ __align__(16) uint64_t lists[kTop ? kWaves : 1][kTop ? kList : 1];
   __shared__ Run runs[kWaves];
   __shared__ int counts[kWaves];
+  __shared__ uint32_t reached;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int64_t row = blockIdx.x;
   const char* z = (const char*)a.logits + row * a.stride * (DT == AQMB_F32 ? 4 : 2);
   const int c0 = blockIdx.y * a.chunk, c1 = min(a.vocab - c0, a.chunk) + c0;
   const float c = a.scale * kLog2E;
-  uint64_t* list = lists[kTop ? wave : 0];
-  int n = 0;                   // keys in the list
-  uint64_t least = 0;          // a key has to reach this
+  TopList top = {lists[kTop ? wave : 0], 0, a.n_top, 0};
+  if constexpr (kTop && kWaves > 1) {
+    if (threadIdx.x == 0) reached = order(-kInf);
+    __syncthreads();
+  }
   float gate = -kInf;          // a later tile's value has to be above this
+  bool sorted = true;
+  Asked early = {-1, 0.f};
+  if (a.splits == 1 && wave == 0) early = asked<DT>(a, row);
 
+  // The values of a load, -infinity, which weighs nothing, from the chunk's end on.
+  const auto piece = [&](int64_t i) {
+    constexpr uint32_t kNone = DT == AQMB_F32 ? 0xFF800000u : DT == AQMB_F16 ? 0xFC00FC00u : 0xFF80FF80u;
+    if (i + kE <= c1) return *(const Raw16*)(z + i * (16 / kE));
+    Raw16 raw = {{kNone, kNone, kNone, kNone}};
+    for (int j = 0; i + j < c1; ++j) {         // a piece that is cut: its values one by one, each into its place
+      const uint32_t w = DT == AQMB_F32 ? ((const uint32_t*)z)[i + j] : ((const uint16_t*)z)[i + j];
+      const int shift = DT == AQMB_F32 ? 0 : 16 * (j % 2), word = j * 4 / kE;
+      const uint32_t keep = DT == AQMB_F32 ? 0u : ~(0xFFFFu << shift);
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+        if (n == word) raw.w[n] = (raw.w[n] & keep) | w << shift;
+    }
+    return raw;
+  };
   Run r = {-kInf, 0.f, 0.f};
-  for (int64_t t0 = c0 + (int64_t)wave * kTile<DT>; t0 < c1; t0 += kWaves * kTile<DT>) {
+  for (int64_t t0 = c0 + (int64_t)wave * kTile; t0 < c1; t0 += kWaves * kTile) {
     float x[kN];
     Raw16 raw[kLoads];
-    if (t0 + kTile<DT> <= c1) {
+    const auto at = [&](int l) { return t0 + (l * 64 + lane) * kE; };
+    if (t0 + kTile <= c1) {
 #pragma unroll
-      for (int l = 0; l < kLoads; ++l) raw[l] = *(const Raw16*)(z + (t0 + (l * 64 + lane) * kE) * (16 / kE));
-#pragma unroll
-      for (int l = 0; l < kLoads; ++l)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t w = raw[l].w[j];
-          if constexpr (DT == AQMB_F32) {
-            x[4 * l + j] = __builtin_bit_cast(float, w);
-          } else {
-            x[8 * l + 2 * j] = DT == AQMB_F16 ? f16lo(w) : bf16lo(w);
-            x[8 * l + 2 * j + 1] = DT == AQMB_F16 ? f16hi(w) : bf16hi(w);
-          }
-        }
+      for (int l = 0; l < kLoads; ++l) raw[l] = *(const Raw16*)(z + at(l) * (16 / kE));
     } else {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        const int64_t i = t0 + (e / kE * 64 + lane) * kE + e % kE;
-        x[e] = i < c1 ? value<DT>(z, (int)i) : -kInf;
-      }
+      for (int l = 0; l < kLoads; ++l) raw[l] = piece(at(l));
     }
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) widen<DT>(raw[l], x + kE * l);
     float m = x[0];
 #pragma unroll
     for (int e = 1; e < kN; ++e) m = fmaxf(m, x[e]);
@@ -187,71 +274,69 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogProbArgs a) {
       r.u = fmaf(p, fmaxf(t, kFar), r.u);
     }
     if constexpr (kTop) {
-      if (!__ballot(m > gate)) continue;
-      if (least == 0) {
-        // As many lanes as top values have a value that reaches the n_top-th largest of the lanes' largest.
-        int above = 0;
+      // What all waves' keys have to reach: as many of one wave's do. An equal value may still be the lower token.
+      const float others = kWaves > 1 ? unorder(*(volatile uint32_t*)&reached) : kLowest;
+      if (!__ballot(m > gate && m >= others)) continue;
+      if (top.least == 0) top.start(order(m));
+      float bound = fmaxf(fmaxf(unorder((uint32_t)(top.least >> 32)), others), kLowest);
 #pragma unroll
-        for (int l = 0; l < 64; ++l) {
-          const float o = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), l));
-          above += o > m || (o == m && l < lane);
+      for (int l = 0; l < kLoads; ++l) {
+        const int64_t i0 = at(l);
+        const float* v = x + kE * l;
+        // Which values come into question; nearly always they fit into the list.
+        uint64_t masks[kE];
+        int more = 0;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          masks[e] = __ballot(v[e] >= bound);
+          more += __builtin_popcountll(masks[e]);
         }
-        const int at = __builtin_ctzll(__ballot(above == a.n_top - 1));
-        least = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)order(m), at) << 32;
-      }
+        if (more == 0) continue;
+        if (top.n + more <= kList) {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        const uint64_t key = key_of(x[e], (int)(t0 + (e / kE * 64 + lane) * kE + e % kE));
-        bool in = x[e] > -kInf && key >= least;
-        uint64_t mask = __ballot(in);
-        if (mask) {
-          if (n + __builtin_popcountll(mask) > kList) {
-            n = sort_list(list, n, a.n_top);
-            if (n == a.n_top) {
-              least = list[n - 1];
-              in = in && key >= least;
-              mask = __ballot(in);
-            }
+          for (int e = 0; e < kE; ++e)
+            if (masks[e]) top.put(key_of(v[e], (int)i0 + e), masks[e]);
+        } else {
+          // As among many equal values: one by one, sorting where the list is full.
+#pragma unroll 1
+          for (int e = 0; e < kE; ++e) {
+            const float u = i0 + e < c1 ? value<DT>(z, (int)i0 + e) : -kInf;
+            top.push(key_of(u, (int)i0 + e), u >= bound);
           }
-          if (in) list[n + __builtin_popcountll(mask & ((1ull << lane) - 1))] = key;
-          n += __builtin_popcountll(mask);
         }
       }
-      if (n >= a.n_top) {
-        n = sort_list(list, n, a.n_top);
-        least = list[n - 1];
-        gate = unorder((uint32_t)(least >> 32));
+      // Sorted once so many are there, and then when the list is half full: a bound that is a little old costs less.
+      sorted = top.n >= a.n_top && (gate == -kInf || top.n > kList / 2);
+      if (sorted) {
+        top.sort();
+        gate = unorder((uint32_t)(top.least >> 32));
+        if (kWaves > 1 && lane == 0) atomicMax(&reached, (uint32_t)(top.least >> 32));
       }
     }
   }
 
   r = over_wave(r, c);
-  if constexpr (kTop) n = sort_list(list, n, a.n_top);
+  if constexpr (kTop) {
+    if (!sorted) top.sort();
+  }
   if constexpr (kWaves > 1) {
-    if (lane == 0) runs[wave] = r, counts[wave] = n;
+    if (lane == 0) runs[wave] = r, counts[wave] = top.n;
     __syncthreads();
-    r = runs[0];
+    if (wave != 0) return;
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) r = join(r, runs[w], c);
     if constexpr (kTop) {
-      // Each key's place among all waves'.
-      const uint64_t key = lane < n ? list[lane] : 0;
-      int place = 0, all = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const int k = counts[w];
-        for (int i = 0; i < k; ++i) place += lists[w][i] > key;
-        all += k;
+#pragma unroll 1
+      for (int w = 1; w < kWaves; ++w) {
+        const bool in = lane < counts[w];
+        top.push(in ? lists[w][lane] : 0, in);
       }
-      __syncthreads();
-      if (lane < n && place < a.n_top) lists[0][place] = key;
-      __syncthreads();
-      n = min(all, a.n_top);
+      top.sort();
     }
-    if (wave != 0) return;
   }
+  const int n = top.n;
   if (a.splits == 1) {
-    finish<DT>(a, row, r, lists[0], n);
+    finish<DT>(a, row, r, early, lists[0], n);
     return;
   }
   if (lane == 0) a.stats[row * a.splits + blockIdx.y] = make_float4(r.m, r.s, r.u, 0.f);
@@ -260,48 +345,58 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogProbArgs a) {
   }
 }
 
-// A wave joins a row's chunks: lane l has chunk l's sums and its keys, of which the largest is taken n_top times.
+// A wave joins a row's chunks: lane l has chunk l's sums and its sorted keys, all lanes' largest, then all second ones...
 template <int DT>
 __global__ __launch_bounds__(64) void join_kernel(LogProbArgs a) {
-  __shared__ uint64_t sorted[64];
+  __shared__ __align__(16) uint64_t list[kList];
   const int lane = threadIdx.x;
   const int64_t row = blockIdx.x;
   const bool on = lane < a.splits;
-  Run r = {-kInf, 0.f, 0.f};
+  const Asked early = asked<DT>(a, row);
   const uint64_t* keys = a.keys + (row * a.splits + lane) * a.n_top;
-  uint64_t head = on && a.n_top ? keys[0] : 0;
+  constexpr int kAhead = 4;                    // keys of a chunk loaded at once
+  uint64_t key[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) key[j] = on && j < a.n_top ? keys[j] : 0;
+  Run r = {-kInf, 0.f, 0.f};
   if (on) {
     const float4 s = a.stats[row * a.splits + lane];
     r = {s.x, s.y, s.z};
   }
   r = over_wave(r, a.scale * kLog2E);
-  int taken = 0, n = 0;
-  while (n < a.n_top) {
-    uint32_t hi = over_lanes<64>((uint32_t)(head >> 32), max_bits);
-    const uint32_t lo = over_lanes<64>((uint32_t)(head >> 32) == hi ? (uint32_t)head : 0, max_bits);
-    const uint64_t most = (uint64_t)hi << 32 | lo;
-    if (most == 0) break;
-    if (head == most) {
-      sorted[n] = head;
-      ++taken;
-      head = taken < a.n_top ? keys[taken] : 0;
+  TopList top = {list, 0, a.n_top, 0};
+  if (a.n_top) {
+    top.start((uint32_t)(key[0] >> 32));
+    for (int j0 = 0; j0 < a.n_top; j0 += kAhead) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) top.push(key[j], key[j] != 0);
+      if (__ballot(key[kAhead - 1] != 0 && key[kAhead - 1] >= top.least) == 0) break;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) key[j] = on && j0 + kAhead + j < a.n_top ? keys[j0 + kAhead + j] : 0;
     }
-    ++n;
+    top.sort();
   }
-  lds_order();
-  finish<DT>(a, row, r, sorted, n);
+  finish<DT>(a, row, r, early, list, top.n);
 }
 
 template <int DT>
 hipError_t go(const LogProbArgs& a, hipStream_t st) {
   const dim3 grid(a.rows, a.splits);
-  const bool small = a.chunk <= kTile<DT>;
+  // A wave's work has to be short where few rows wait for it: one load a tile then (the code of a tile is unrolled, and is
+  // fetched for one use; one row of 32000 with 5 top values 6.4 us, with four loads 8.5). Many short rows: a wave each, no joining
+  // (4000 rows of 2000: 12 us against 22 by four waves; 4096 rows of 32000 with 20 top values 103 and 118, 1024 rows 41 and 31).
+  const int64_t pieces = ((int64_t)a.chunk + kPiece<DT> - 1) / kPiece<DT>, groups = (int64_t)a.rows * a.splits;
+  const int variant = pieces <= 2 ? 0 : pieces <= (groups >= 4096 ? 64 : groups >= 1024 ? 16 : 0) ? 1 : pieces <= 16 ? 2 : 3;
   if (a.n_top) {
-    if (small) rows_kernel<DT, 64, true><<<grid, 64, 0, st>>>(a);
-    else rows_kernel<DT, 256, true><<<grid, 256, 0, st>>>(a);
+    if (variant == 0) rows_kernel<DT, 64, 1, true><<<grid, 64, 0, st>>>(a);
+    else if (variant == 1) rows_kernel<DT, 64, 4, true><<<grid, 64, 0, st>>>(a);
+    else if (variant == 2) rows_kernel<DT, 256, 1, true><<<grid, 256, 0, st>>>(a);
+    else rows_kernel<DT, 256, 4, true><<<grid, 256, 0, st>>>(a);
   } else {
-    if (small) rows_kernel<DT, 64, false><<<grid, 64, 0, st>>>(a);
-    else rows_kernel<DT, 256, false><<<grid, 256, 0, st>>>(a);
+    if (variant == 0) rows_kernel<DT, 64, 1, false><<<grid, 64, 0, st>>>(a);
+    else if (variant == 1) rows_kernel<DT, 64, 4, false><<<grid, 64, 0, st>>>(a);
+    else if (variant == 2) rows_kernel<DT, 256, 1, false><<<grid, 256, 0, st>>>(a);
+    else rows_kernel<DT, 256, 4, false><<<grid, 256, 0, st>>>(a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
@@ -311,10 +406,13 @@ hipError_t go(const LogProbArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Rows are cut while they are few: at most one chunk per load of a wave, 64 per row (a lane each in the second launch), about
+// 2048 workgroups (128 rows of 131072, 20 top values: 28 us, with 1024 32, 512 30; 300 rows of 32000 17, 21 and 16), from 512
+// rows on 1024 (1024 rows of 32000: 31 us uncut, 36 in two).
 LogProbPlan log_prob_plan(aqmb_dtype dtype, int rows, int vocab, int n_top) {
-  const int unit = 4 * (dtype == AQMB_F32 ? kTile<AQMB_F32> : kTile<AQMB_F16>);
+  const int unit = dtype == AQMB_F32 ? kPiece<AQMB_F32> : kPiece<AQMB_F16>;
   LogProbPlan p;
-  int64_t splits = 1024 / rows;
+  int64_t splits = (rows < 512 ? 2048 : 1024) / rows;
   const int64_t most = ((int64_t)vocab + unit - 1) / unit;
   if (splits > most) splits = most;
   if (splits > 64) splits = 64;
