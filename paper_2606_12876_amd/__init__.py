@@ -217,6 +217,9 @@ try:
     _direct.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
         "aqmb_rms_norm", "aqmb_w4_gemv", "aqmb_paged_attention", "aqmb_paged_attention_workspace_bytes",
         "aqmb_kv_append", "aqmb_kv_copy_pages")))
+    _direct.bind_requests(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+        "aqmb_rotary", "aqmb_rotary_append", "aqmb_adapters_add", "aqmb_adapters_workspace_bytes", "aqmb_log_probs",
+        "aqmb_log_probs_workspace_bytes")))
 except ImportError as e:
     _direct = None
     warnings.warn(f"{os.path.join(os.path.dirname(LIB_PATH), '_direct.so')} is missing or was built for another PyTorch "
@@ -944,6 +947,11 @@ class KVCache:
         """aqmb_rotary_append: q [n_tokens][n_heads][head_dim] turned into q_out, k turned and v written into slots
         int64 [n_tokens], at positions int64 [n_tokens], all on the GPU."""
         where = "aqmb_rotary_append"
+        if stream is None and _direct is not None:
+            st = _direct.rotary_append(self._address, self.device_index, rotary._address, rotary.device_index, q, k, v,
+                                       positions, slots, q_out)
+            if st is not None:
+                return _check(st, where) if st else None
         dev = _current_device()
         if dev != self.device_index:
             self._current(where)
@@ -1163,6 +1171,11 @@ class Rotary:
         """aqmb_rotary: q [n_tokens][n_heads][head_dim] fp16 or bf16 turned by positions int64 [n_tokens] into q_out
         (may be q), and k into k_out alike. inverse turns back: the gradient of q from that of q_out."""
         where = "aqmb_rotary"
+        if stream is None and _direct is not None:
+            st = _direct.rotary(self._inverse_address if inverse else self._address, self.device_index, q, positions, q_out, k,
+                                k_out)
+            if st is not None:
+                return _check(st, where) if st else None
         _here(where, q=q, q_out=q_out, k=k, k_out=k_out, positions=positions, frequencies=self.frequencies)
         n, heads, dt, qs, os_ = _rotary_tensors(q, q_out, positions, None, where)
         kv, ks, ko, kp, kop = 0, 0, 0, None, None
@@ -1246,6 +1259,10 @@ class Adapters:
         that index int32 [n_rows] names (-1: none; on the GPU). base and out (may be base): [n_rows][d_out] fp16, bf16 or
         fp32, what the projection gave. Without a workspace one is taken from PyTorch's allocator."""
         where = "aqmb_adapters_add"
+        if stream is None and _direct is not None:
+            st = _direct.adapters_add(self._address, self.device_index, x, index, base, out, workspace)
+            if st is not None:
+                return _check(st, where) if st else None
         dev = _current_device()
         if dev != self.device_index:
             _refuse(where, f"the adapters are on device {self.device_index}, device {dev} is current")
@@ -1289,6 +1306,10 @@ def log_probs(logits, targets=None, logprobs=None, *, scale: float = 1.0, lse=No
     int64 [rows][n] (or both [rows]; a negative one gets 0), lse and entropy fp32 [rows], and top_ids int64,
     top_logprobs fp32 [rows][n_top] in descending order. Every output may be left out, not all."""
     where = "aqmb_log_probs"
+    if stream is None and _direct is not None:
+        st = _direct.log_probs(logits, targets, logprobs, scale, lse, entropy, top_ids, top_logprobs, workspace)
+        if st is not None:
+            return _check(st, where) if st else None
     if logits.dim() != 2:
         _refuse(where, f"logits are {tuple(logits.shape)}, not (rows, vocab)")
     _here(where, logits=logits, targets=targets, logprobs=logprobs, lse=lse, entropy=entropy, top_ids=top_ids,

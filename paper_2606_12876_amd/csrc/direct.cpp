@@ -29,6 +29,12 @@ decltype(&aqmb_paged_attention) f_attention;
 decltype(&aqmb_paged_attention_workspace_bytes) f_workspace;
 decltype(&aqmb_kv_append) f_append;
 decltype(&aqmb_kv_copy_pages) f_copy;
+decltype(&aqmb_rotary) f_rotary;
+decltype(&aqmb_rotary_append) f_rotary_append;
+decltype(&aqmb_adapters_add) f_adapters;
+decltype(&aqmb_adapters_workspace_bytes) f_adapters_workspace;
+decltype(&aqmb_log_probs) f_log_probs;
+decltype(&aqmb_log_probs_workspace_bytes) f_log_probs_workspace;
 
 struct NotUsual {};
 void need(bool usual) {
@@ -118,6 +124,24 @@ int launch(F call) {
   return s;
 }
 
+// The caller's workspace, or `bytes` bytes beside `like` from the allocator, which ties them to the current stream.
+struct Workspace {
+  Tensor own;
+  void* data = nullptr;
+  size_t bytes;
+  Workspace(PyObject* given, size_t needed, const Tensor& like, int dev) : bytes(needed) {
+    if (given != Py_None) {
+      const Tensor& t = tensor(given, dev, true);
+      need(t.is_contiguous());        // its bytes are its own
+      data = t.data_ptr();
+      bytes = (size_t)t.numel() * t.element_size();
+    } else if (needed) {
+      own = at::empty({(int64_t)needed}, like.options().dtype(ScalarType::Byte));
+      data = own.data_ptr();
+    }
+  }
+};
+
 // (x, weight, y, eps, weight_offset, residual, residual_out, scales, scale_group)
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return usual([&] {
@@ -202,23 +226,13 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     float* lse = a[9] == Py_None ? nullptr : (float*)dense(a[9], dev, ScalarType::Float, (int64_t)n * heads);
     size_t bytes = 0;
     need(f_workspace(c, heads, n, max_length, window, &bytes) == AQMB_OK);
-    Tensor own;
-    void* ws = nullptr;
-    if (a[10] != Py_None) {
-      const Tensor& t = tensor(a[10], dev, true);
-      need(t.is_contiguous());        // its bytes are its own
-      ws = t.data_ptr();
-      bytes = (size_t)t.numel() * t.element_size();
-    } else if (bytes) {               // from the allocator, which ties it to the current stream
-      own = at::empty({(int64_t)bytes}, q.options().dtype(ScalarType::Byte));
-      ws = own.data_ptr();
-    }
+    const Workspace work(a[10], bytes, q, dev);
     const void* qp = q.data_ptr();
     void* op = out.data_ptr();
     const int32_t* tp = (const int32_t*)table.data_ptr();
     const aqmb_stream_t st = stream(dev);
     return launch([&] {
-      return f_attention(c, qp, dt, qs, heads, tp, ts, lengths, n, max_length, scale, window, op, os, lse, ws, bytes, st);
+      return f_attention(c, qp, dt, qs, heads, tp, ts, lengths, n, max_length, scale, window, op, os, lse, work.data, work.bytes, st);
     });
   });
 }
@@ -240,6 +254,133 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const void *kp = k.data_ptr(), *vp = v.data_ptr();
     const aqmb_stream_t st = stream(dev);
     return launch([&] { return f_append(c, kp, ks, vp, vs, dt, slots, n, st); });
+  });
+}
+
+// (descriptor, its device, q, positions, q_out, k, k_out)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return usual([&] {
+    need(n_args == 7);
+    const aqmb_rotary_desc* r = address<const aqmb_rotary_desc*>(a[0]);
+    const Tensor& q = tensor(a[2], -1);
+    const int dev = current(q);
+    need(integer(a[1]) == dev);
+    const Tensor& out = tensor(a[4], dev);
+    need(q.dim() == 3 && out.scalar_type() == q.scalar_type());
+    const int n = whole(q.size(0)), heads = whole(q.size(1)), dim = whole(q.size(2));
+    const aqmb_dtype dt = dtype_of(q);
+    const int64_t qs = rows_of(q, n, heads, dim), os = rows_of(out, n, heads, dim);
+    const int64_t* positions = (const int64_t*)dense(a[3], dev, ScalarType::Long, n);
+    const void* kp = nullptr;
+    void* kop = nullptr;
+    int64_t ks = 0, kos = 0;
+    int kv = 0;
+    if (a[5] != Py_None || a[6] != Py_None) {
+      const Tensor &k = tensor(a[5], dev), &ko = tensor(a[6], dev);
+      need(k.dim() == 3 && k.scalar_type() == q.scalar_type() && ko.scalar_type() == q.scalar_type());
+      kv = whole(k.size(1));
+      ks = rows_of(k, n, kv, dim);
+      kos = rows_of(ko, n, kv, dim);
+      kp = k.data_ptr();
+      kop = ko.data_ptr();
+    }
+    const void* qp = q.data_ptr();
+    void* op = out.data_ptr();
+    const aqmb_stream_t st = stream(dev);
+    return launch([&] { return f_rotary(r, qp, qs, op, os, heads, kp, ks, kop, kos, kv, dt, dim, positions, n, st); });
+  });
+}
+
+// (cache's descriptor, its device, rotary's descriptor, its device, q, k, v, positions, slots, q_out)
+PyObject* rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return usual([&] {
+    need(n_args == 10);
+    const aqmb_kv_cache* c = address<const aqmb_kv_cache*>(a[0]);
+    const aqmb_rotary_desc* r = address<const aqmb_rotary_desc*>(a[2]);
+    const Tensor& q = tensor(a[4], -1);
+    const int dev = current(q);
+    need(integer(a[1]) == dev && integer(a[3]) == dev);
+    const Tensor &k = tensor(a[5], dev), &v = tensor(a[6], dev), &out = tensor(a[9], dev);
+    need(q.dim() == 3 && out.scalar_type() == q.scalar_type() && k.scalar_type() == q.scalar_type() &&
+         v.scalar_type() == q.scalar_type());
+    const int n = whole(q.size(0)), heads = whole(q.size(1));
+    const aqmb_dtype dt = dtype_of(q);
+    const int64_t qs = rows_of(q, n, heads, c->head_dim), os = rows_of(out, n, heads, c->head_dim);
+    const int64_t ks = rows_of(k, n, c->n_kv_heads, c->head_dim), vs = rows_of(v, n, c->n_kv_heads, c->head_dim);
+    const int64_t* positions = (const int64_t*)dense(a[7], dev, ScalarType::Long, n);
+    const int64_t* slots = (const int64_t*)dense(a[8], dev, ScalarType::Long, n);
+    const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
+    void* op = out.data_ptr();
+    const aqmb_stream_t st = stream(dev);
+    return launch([&] { return f_rotary_append(c, r, qp, qs, op, os, heads, kp, ks, vp, vs, dt, positions, slots, n, st); });
+  });
+}
+
+// (descriptor, its device, x, index, base, out, workspace)
+PyObject* adapters_add(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return usual([&] {
+    need(n_args == 7);
+    const aqmb_adapters* ad = address<const aqmb_adapters*>(a[0]);
+    const Tensor& x = tensor(a[2], -1);
+    const int dev = current(x);
+    need(integer(a[1]) == dev && x.dim() == 2 && dtype_of(x) == ad->dtype);
+    const Tensor &base = tensor(a[4], dev), &out = tensor(a[5], dev);
+    need(out.scalar_type() == base.scalar_type());
+    const int n = whole(x.size(0));
+    const aqmb_dtype dt = dtype_of(base);
+    const int64_t xs = rows_of(x, n, ad->d_in), bs = rows_of(base, n, ad->d_out), os = rows_of(out, n, ad->d_out);
+    const int32_t* index = (const int32_t*)dense(a[3], dev, ScalarType::Int, n);
+    size_t bytes = 0;
+    need(f_adapters_workspace(ad, n, &bytes) == AQMB_OK);
+    const Workspace work(a[6], bytes, x, dev);
+    const void *xp = x.data_ptr(), *bp = base.data_ptr();
+    void* op = out.data_ptr();
+    const aqmb_stream_t st = stream(dev);
+    return launch([&] { return f_adapters(ad, xp, xs, index, n, bp, bs, op, os, dt, work.data, work.bytes, st); });
+  });
+}
+
+// (logits, targets, logprobs, scale, lse, entropy, top_ids, top_logprobs, workspace)
+PyObject* log_probs(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return usual([&] {
+    need(n_args == 9);
+    const Tensor& z = tensor(a[0], -1);
+    const int dev = current(z);
+    need(z.dim() == 2);
+    const int rows = whole(z.size(0)), vocab = whole(z.size(1));
+    const aqmb_dtype dt = dtype_of(z);
+    const int64_t stride = rows_of(z, rows, vocab);
+    const float scale = real(a[3]);
+    // Columns of a dense tensor [rows][n] or [rows], of at least one value.
+    const auto columns = [&](PyObject* o, ScalarType type, void** data) {
+      const Tensor& t = tensor(o, dev);
+      need((t.dim() == 1 || t.dim() == 2) && t.size(0) == rows && t.scalar_type() == type && t.is_contiguous());
+      *data = t.data_ptr();
+      return whole(t.numel() / rows);
+    };
+    void *targets = nullptr, *lp = nullptr, *ids = nullptr, *tops = nullptr;
+    int n = 0, top = 0;
+    if (a[1] != Py_None || a[2] != Py_None) {
+      n = columns(a[1], ScalarType::Long, &targets);
+      lp = dense(a[2], dev, ScalarType::Float, (int64_t)rows * n);
+    }
+    float* lse = a[4] == Py_None ? nullptr : (float*)dense(a[4], dev, ScalarType::Float, rows);
+    float* entropy = a[5] == Py_None ? nullptr : (float*)dense(a[5], dev, ScalarType::Float, rows);
+    if (a[6] != Py_None) top = columns(a[6], ScalarType::Long, &ids);
+    if (a[7] != Py_None) {
+      const int k = columns(a[7], ScalarType::Float, &tops);
+      need(top == 0 || k == top);
+      top = k;
+    }
+    size_t bytes = 0;
+    need(f_log_probs_workspace(dt, rows, vocab, top, &bytes) == AQMB_OK);
+    const Workspace work(a[8], bytes, z, dev);
+    const void* zp = z.data_ptr();
+    const aqmb_stream_t st = stream(dev);
+    return launch([&] {
+      return f_log_probs(zp, dt, stride, rows, vocab, scale, (const int64_t*)targets, n, (float*)lp, lse, entropy,
+                         (int64_t*)ids, (float*)tops, top, work.data, work.bytes, st);
+    });
   });
 }
 
@@ -293,9 +434,25 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// (rotary, rotary_append, adapters_add, its workspace_bytes, log_probs, its workspace_bytes): the functions' addresses.
+PyObject* bind_requests(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* f[6];
+  if (n != 6) return PyErr_Format(PyExc_TypeError, "bind_requests takes six addresses");
+  for (int i = 0; i < 6; ++i)
+    if (!(f[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "a null address");
+  f_rotary = (decltype(f_rotary))f[0];
+  f_rotary_append = (decltype(f_rotary_append))f[1];
+  f_adapters = (decltype(f_adapters))f[2];
+  f_adapters_workspace = (decltype(f_adapters_workspace))f[3];
+  f_log_probs = (decltype(f_log_probs))f[4];
+  f_log_probs_workspace = (decltype(f_log_probs_workspace))f[5];
+  Py_RETURN_NONE;
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(rms_norm), METHOD(w4_gemv), METHOD(paged_attention),
-                         METHOD(kv_append), METHOD(kv_copy_pages), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv_append), METHOD(kv_copy_pages), METHOD(bind_requests), METHOD(rotary),
+                         METHOD(rotary_append), METHOD(adapters_add), METHOD(log_probs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_direct", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
