@@ -2,13 +2,15 @@
 
 One block of a Llama-shaped model serves several streams at once, one new token each per step:
 
-    rms_norm -> q, k, v (additive-codebook layers, one launch) -> rotary -> kv_append
-    -> paged attention -> o (additive-codebook layer) -> rms_norm with the residual, int8 output
-    -> gate, up (4-bit layers on the int8 rows) -> silu * -> down (4-bit layer)
+    rms_norm -> q, k, v (additive-codebook layers, one launch) -> each stream's own low-rank adapter beside q and v
+    -> rotary positions and the cache's writing (one launch) -> paged attention -> o (additive-codebook layer)
+    -> rms_norm with the residual, int8 output -> gate, up (4-bit layers on the int8 rows) -> silu * -> down (4-bit layer)
+
+and a head's logits are answered with the log probabilities of chosen tokens, the entropy and alternatives,
 
 with the precision level k of the additive-codebook layers chosen per step, the cache's pages
 handed out by PagePool, and a stream forked in mid-decode (its pages shared until one of the two
-writes). Rotary embedding and silu are plain torch. Run it on a GPU: ``python examples/decode_step.py``.
+writes). Silu and the head are plain torch. Run it on a GPU: ``python examples/decode_step.py``.
 """
 from __future__ import annotations
 
@@ -23,34 +25,31 @@ if __name__ == "__main__":
 import paper_2606_12876_amd as A  # noqa: E402
 
 
-def rotate(x, positions):
-    """Rotary embedding of x [n][heads][dim] at positions [n]."""
-    half = x.shape[-1] // 2
-    freq = 10000.0 ** (-torch.arange(half, device=x.device, dtype=torch.float32) / half)
-    angle = (positions.float()[:, None] * freq)[:, None, :]
-    a, b = x.float().split(half, -1)
-    return torch.cat((a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()), -1).to(x.dtype)
-
-
 class DecodeBlock:
     """Weights, cache and one step of a block. ``aq``: QuantLinear layers by name (q, k, v, o); ``w4``:
-    W4Linear layers by name (gate, up, down); ``norms``: two bf16 vectors."""
+    W4Linear layers by name (gate, up, down); ``norms``: two bf16 vectors; ``adapters``: Adapters by the names of
+    layers in aq (q, k, v), of which a step's ``index`` picks each stream's."""
 
-    def __init__(self, aq, w4, norms, heads: int, kv_heads: int, cache: A.KVCache, eps: float = 1e-5):
-        self.aq, self.w4, self.norms, self.cache, self.eps = aq, w4, norms, cache, eps
+    def __init__(self, aq, w4, norms, heads: int, kv_heads: int, cache: A.KVCache, eps: float = 1e-5, adapters=None):
+        self.aq, self.w4, self.norms, self.cache, self.eps, self.adapters = aq, w4, norms, cache, eps, adapters or {}
+        self.rotary = A.Rotary.scaled(cache.head_dim)
         self.heads, self.kv_heads, self.dim = heads, kv_heads, cache.head_dim
         self.hidden = norms[0].numel()
 
-    def step(self, h, k_level: int, positions, slots, table, lengths, max_length: int):
-        """h [n][hidden] bf16 -> the block's output; positions, slots int64 [n], table, lengths int32."""
+    def step(self, h, k_level: int, positions, slots, table, lengths, max_length: int, index=None):
+        """h [n][hidden] bf16 -> the block's output; positions, slots int64 [n], table, lengths int32; index int32 [n]:
+        each stream's adapter, -1 for none."""
         n, dev = h.shape[0], h.device
         x = torch.empty_like(h)
         A.rms_norm(h, self.norms[0], x, eps=self.eps)
         q, k, v = (torch.empty((n, heads, self.dim), dtype=h.dtype, device=dev)
                    for heads in (self.heads, self.kv_heads, self.kv_heads))
         A.gemv_multi([self.aq[name].handle for name in "qkv"], k_level, x, A.DType.BF16, n, [q, k, v], A.DType.BF16)
-        q, k = rotate(q, positions), rotate(k, positions)
-        self.cache.append(k, v, slots)
+        if index is not None:
+            for name, t in zip("qkv", (q, k, v)):
+                if name in self.adapters:
+                    self.adapters[name].add(x, index, t.view(n, -1), t.view(n, -1))
+        self.cache.rotary_append(self.rotary, q, k, v, positions, slots, q)      # q in place
         o = torch.empty_like(q)
         self.cache.attention(q, table, lengths, o, max_length=max_length, scale=self.dim ** -0.5)
         a = self.aq["o"](o.view(n, -1), k_level)
@@ -101,6 +100,30 @@ class Streams:
                 lengths.to(self.device), int(lengths.max()))
 
 
+def answer(h, head, targets, n_top: int = 3):
+    """What a stream's token gets back: (log probability of the given token, entropy, ids and log probabilities of
+    the likeliest ones), from the head's logits of the rows h."""
+    logits, n = h @ head, h.shape[0]
+    lp, entropy = (torch.empty((n,), dtype=torch.float32, device=h.device) for _ in range(2))
+    ids = torch.empty((n, n_top), dtype=torch.int64, device=h.device)
+    tops = torch.empty((n, n_top), dtype=torch.float32, device=h.device)
+    A.log_probs(logits, targets, lp, entropy=entropy, top_ids=ids, top_logprobs=tops)
+    return lp, entropy, ids, tops
+
+
+def random_adapters(block, n: int = 4, rank: int = 16, seed: int = 0):
+    """n adapters beside q and v."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def make(d_out):
+        a = torch.randn((n, rank, block.hidden), generator=g, device="cuda") * block.hidden ** -0.5
+        b = torch.randn((n, d_out, rank), generator=g, device="cuda") * 0.3 * rank ** -0.5
+        return A.Adapters(a.bfloat16(), b.bfloat16(), 0.5 + torch.rand((n,), generator=g, device="cuda"))
+
+    return {"q": make(block.heads * block.dim), "v": make(block.kv_heads * block.dim)}
+
+
 def random_block(hidden=512, heads=8, kv_heads=2, dim=64, ffn=1376, pages=64, page=16, cache_dtype=torch.bfloat16, seed=0):
     """A block with random weights, and its raw tensors for whoever wants to check it."""
     g = torch.Generator(device="cuda")
@@ -131,6 +154,8 @@ def random_block(hidden=512, heads=8, kv_heads=2, dim=64, ffn=1376, pages=64, pa
 def main():
     torch.manual_seed(0)
     block, _ = random_block(hidden=4096, heads=32, kv_heads=32, dim=128, ffn=11008, pages=256, cache_dtype=torch.float8_e4m3fn)
+    block.adapters = random_adapters(block)
+    head = (torch.randn((block.hidden, 32000), device="cuda") * 0.02).bfloat16()
     pool = A.PagePool(256, 16, 8)
     streams = Streams(pool, [block.cache])
     live = [pool.add() for _ in range(3)]
@@ -141,10 +166,13 @@ def main():
             streams.free(live.pop(1))
             streams.copy(pool.compact())
         h = torch.randn((len(live), block.hidden), device="cuda").bfloat16()
-        h = block.step(h, 4 if step % 2 else 2, *streams.advance(live))
+        index = torch.tensor([s % 5 - 1 for s in live], dtype=torch.int32).to("cuda")      # stream 0 has no adapter
+        h = block.step(h, 4 if step % 2 else 2, *streams.advance(live), index=index)
+        lp, entropy, ids, _ = answer(h, head, torch.zeros((len(live),), dtype=torch.int64, device="cuda"))
         if step % 10 == 9:
             print(f"step {step + 1}: {len(live)} streams of {[pool.length(s) for s in live]} tokens, "
-                  f"{pool.counts()[0]} pages free, |h| = {h.float().norm(dim=1).mean().item():.3f}")
+                  f"{pool.counts()[0]} pages free, |h| = {h.float().norm(dim=1).mean().item():.3f}, entropy "
+                  f"{entropy.mean().item():.3f}, likeliest tokens {ids[:, 0].tolist()}")
 
 
 if __name__ == "__main__":
