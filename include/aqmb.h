@@ -370,7 +370,8 @@ double aqmb_bits_per_weight(const aqmb_desc* desc, int k);
  * ---------------------------------------------------------------------------------------------
  * The operators between the layers of a decode step: the norm that feeds a projection, the product
  * with plain 4-bit weights (for the layers of a model that are not additively coded), attention of
- * one new token over a paged key-value cache, and the cache's upkeep. The conventions above hold,
+ * one new token over a paged key-value cache, the cache's upkeep, and what requests bring and get
+ * back (rotary positions, low-rank adapters, log probabilities). The conventions above hold,
  * except that data pointers need only the alignment of their elements and rows may be strided
  * (strides in elements, the last dimension dense). Sums, softmax statistics and scales are held in
  * binary32. Nothing here allocates device memory except aqmb_w4_create.
