@@ -1,0 +1,117 @@
+"""Rotary positions, adapters and log probabilities on rows whose offsets pass 32 bits: equal, to the bit, to the same rows
+close together (GPU)."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2606_12876_amd as A  # noqa: E402
+from ops_helpers import gen, normal  # noqa: E402
+
+BF16 = torch.bfloat16
+FAR = 2 ** 31 + 64                     # elements from row to row
+
+
+@pytest.fixture(scope="module")
+def space():
+    if torch.cuda.mem_get_info()[0] < 40 * 2 ** 30:
+        pytest.skip("needs 40 GiB of free device memory")
+    t = torch.empty((2 * FAR + 2 ** 20,), dtype=BF16, device="cuda")
+    yield t
+    del t
+    torch.cuda.empty_cache()
+
+
+def spread(space, t, at=0):
+    """t [rows <= 3][...] with its rows FAR elements apart."""
+    v = space.as_strided((t.shape[0],) + t[0].shape, (FAR,) + t[0].contiguous().stride(), at)
+    v.copy_(t)
+    return v
+
+
+def test_rotary(space):
+    g = gen(1)
+    q, pos, r = normal(g, 3, 8, 128, dtype=BF16), torch.tensor([3, 70000, 9], device="cuda"), A.Rotary.scaled(128)
+    want = torch.empty_like(q)
+    r.apply(q, pos, want)
+    far, out = spread(space, q), spread(space, torch.zeros_like(q), 4096)
+    r.apply(far, pos, out)
+    assert torch.equal(out, want)
+    r.apply(far, pos, far)
+    assert torch.equal(far, want)
+
+
+def test_rotary_append(space):
+    """Pages FAR elements apart."""
+    g = gen(2)
+    rows, pos, slots = normal(g, 3, 6, 64, dtype=BF16), torch.arange(3, device="cuda"), torch.tensor([0, 9, 19], device="cuda")
+    near = A.KVCache.allocate(3, 8, 2, 64, BF16)
+    k, v = (space.as_strided((3, 2, 8, 64), (FAR, 512, 64, 1), at) for at in (0, 4096))
+    for t in (near.k, near.v, k, v):
+        t.zero_()
+    far, r, o = A.KVCache(k, v), A.Rotary.scaled(64), torch.empty((3, 2, 64), dtype=BF16, device="cuda")
+    for c in (near, far):
+        c.rotary_append(r, rows[:, :2], rows[:, 2:4], rows[:, 4:], pos, slots, o)
+    assert torch.equal(near.k, far.k) and torch.equal(near.v, far.v) and near.k.any()
+
+
+def test_adapters(space):
+    g = gen(3)
+    ad = A.Adapters(normal(g, 2, 16, 512, dtype=BF16), normal(g, 2, 256, 16, dtype=BF16))
+    x, base, index = normal(g, 3, 512, dtype=BF16), normal(g, 3, 256, dtype=BF16), torch.tensor([1, -1, 0], dtype=torch.int32, device="cuda")
+    want = torch.empty_like(base)
+    ad.add(x, index, base, want)
+    fx, fb, fo = spread(space, x), spread(space, base, 4096), spread(space, torch.zeros_like(base), 8192)
+    ad.add(fx, index, fb, fo)
+    assert torch.equal(fo, want)
+    # many rows, of which three are these: the sorted way
+    rows, at = 256, torch.tensor([0, 150, 255], device="cuda")
+    wide = space.as_strided((rows, 512), (2 ** 24, 1))
+    wide.copy_(normal(g, rows, 512, dtype=BF16))
+    assert 255 * 2 ** 24 > 2 ** 31
+    idx, b = torch.randint(-1, 2, (rows,), generator=g, device="cuda").to(torch.int32), normal(g, rows, 256, dtype=BF16)
+    got, want = torch.empty_like(b), torch.empty_like(b)
+    ad.add(wide, idx, b, got)
+    ad.add(wide.contiguous(), idx, b, want)
+    assert torch.equal(got, want) and not torch.equal(got[at], b[at])
+
+
+def test_a_large_stack(space):
+    """An adapter whose weights begin past 2^31 bytes, in either matrix, few rows and many."""
+    g = gen(4)
+    n, rank, d = 3, 256, 2 ** 21 + 2 ** 20
+    a = space[:n * rank * d].view(n, rank, d)
+    assert 2 * rank * d * 2 > 2 ** 31
+    small = normal(g, 256, 64, dtype=BF16)
+    for rows in (2, 200):
+        index = torch.full((rows,), 2, dtype=torch.int32, device="cuda")
+        a[2].zero_()
+        a[2, :, -64:] = small
+        x = torch.zeros((rows, d), dtype=BF16, device="cuda") if rows == 2 else torch.zeros((1, d), dtype=BF16, device="cuda").expand(rows, d).contiguous()
+        x[:, -64:] = normal(g, rows, 64, dtype=BF16)
+        b, base = normal(g, n, 40, rank, dtype=BF16), normal(g, rows, 40)
+        got, want = torch.empty_like(base), torch.empty_like(base)
+        A.Adapters(a, b).add(x, index, base, got)
+        t = x[:, -64:].double() @ small.double().t()
+        want = base.double() + t @ b[2].double().t()
+        # 2^-24 (64 products, 16 parts and 24 steps of the second sum, doubled) of what is summed: 2^-16 is ample
+        size = (x[:, -64:].double().abs() @ small.double().t().abs()) @ b[2].double().t().abs()
+        assert ((got.double() - want).abs() <= 2.0 ** -16 * (size + base.double().abs())).all()
+        del x
+
+
+def test_log_probs(space):
+    g = gen(5)
+    z, t = normal(g, 3, 30000, dtype=BF16, std=3.0), torch.tensor([5, 29999, 7], device="cuda")
+    far = spread(space, z)
+    got = []
+    for v in (z, far):
+        out = [torch.empty((3,), device="cuda"), torch.empty((3,), device="cuda"), torch.empty((3, 9), dtype=torch.int64, device="cuda")]
+        A.log_probs(v, t, out[0], entropy=out[1], top_ids=out[2])
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
