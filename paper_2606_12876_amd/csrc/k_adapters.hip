@@ -319,9 +319,18 @@ struct ExpandLds {
 template <int DT>
 constexpr size_t expand_lds(int steps) { return sizeof(ExpandLds<DT>) + (steps - 1) * sizeof(ExpandLds<DT>::t); }
 
-// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave.
+
+// Which of a lane's 8 values are an adapter's own, the first `left`, as a mask.
+__device__ __forceinline__ u32x4_t own_values(int left) {
+  return u32x4_t{left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0, left >= 4 ? 0xFFFFFFFFu : left == 3 ? 0xFFFFu : 0,
+                 left >= 6 ? 0xFFFFFFFFu : left == 5 ? 0xFFFFu : 0, left >= 8 ? 0xFFFFFFFFu : left == 7 ? 0xFFFFu : 0};
+}
+
+// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave, into to[step][part][lane]; the
+// factor of the rows' results (fp16) into back.
 template <int DT>
-__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, ExpandLds<DT>& lds) {
+__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, u32x4_t (*to)[Parts<DT>::kN][64],
+                                         float* back) {
   typedef Parts<DT> P;
   const int lane = threadIdx.x % 64, q = lane / 16, steps = (rank + 31) / 32;
   const float* tp = a.t + (int64_t)row * a.t_stride + 8 * q;
@@ -363,7 +372,7 @@ __device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank
     big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 32), (int)big));
     const int ex = min(max((int)(big >> 23), 14), 254);    // the exponent that goes to 13
     fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
-    if (lane < 16) lds.back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
+    if (lane < 16) back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
   }
   for (int kt = 0;;) {
 #pragma unroll
@@ -376,7 +385,7 @@ __device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank
         v[2 * j] -= P::lo(w[j]);
         v[2 * j + 1] -= P::hi(w[j]);
       }
-      lds.t[kt][p][lane] = u32x4_t{w[0], w[1], w[2], w[3]};
+      to[kt][p][lane] = u32x4_t{w[0], w[1], w[2], w[3]};
     }
     if (++kt >= steps) return;
     values(kt, v);
@@ -479,8 +488,7 @@ template <int DT, bool kWide, bool kEights, bool kStream>
 __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, int o0, int o1, ExpandLds<DT>& lds) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
   const int lane = threadIdx.x % 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
-  const int rank = own_rank(a, t.adapter);
-  if (rank == 0 && a.base == a.out) return;
+  int rank = stack;
   int row[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row[0]);
@@ -497,15 +505,6 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
       if (4 * q + j < t.count)
         store_y<kWide, kEights, kStream>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
   };
-  Eight<kWide> y[4];
-  if (rank == 0) {
-    for (int o = o0; o < o1; o += 128) {
-      load_rows(y, o);
-      store_rows(y, o);
-    }
-    return;
-  }
-
   // Weights in pieces of 8: `pieces` lanes side by side (a power of two) to an output's row of a step.
   const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * stack;
   const auto shift_of = [&](int kt) { const int left = (kt == 0 ? stack : rank) - 32 * kt; return left > 16 ? 2 : left > 8 ? 1 : 0; };
@@ -528,18 +527,21 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
       lds.w[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
     }
   };
-  const int left = rank - (rank - 1) / 32 * 32 - 8 * q;  // own values in the lane's piece of the last step
-  u32x4_t mask;
-  mask.x = left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0;
-  mask.y = left >= 4 ? 0xFFFFFFFFu : left == 3 ? 0xFFFFu : 0;
-  mask.z = left >= 6 ? 0xFFFFFFFFu : left == 5 ? 0xFFFFu : 0;
-  mask.w = left >= 8 ? 0xFFFFFFFFu : left == 7 ? 0xFFFFu : 0;
-
   // The first weights and rows of base are on their way while t comes; so are the next ones later.
   u32x4_t w[8];
-  load_w(w, o0, 0);
+  Eight<kWide> y[4];
+  if (t.adapter >= 0) load_w(w, o0, 0);
   load_rows(y, o0);
-  operands<DT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds);
+  rank = own_rank(a, t.adapter);                         // only now: the loads above do not wait for it
+  if (rank == 0) {
+    for (int o = o0; a.base != a.out && o < o1; o += 128) {
+      if (o != o0) load_rows(y, o);
+      store_rows(y, o);
+    }
+    return;
+  }
+  const u32x4_t mask = own_values(rank - (rank - 1) / 32 * 32 - 8 * q);      // of the last step
+  operands<DT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds.t, lds.back);
 
   for (int o = o0; o < o1; o += 128) {
     const bool more = o + 128 < o1;
@@ -583,16 +585,108 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
   if (tile_at(a, blockIdx.y, t) && o0 < a.ad.d_out)
     expand<DT, kWide, kEights, false>(a, t, (int)o0, (int)min(o0 + a.per_wave, (int64_t)a.ad.d_out), own_lds<DT>(a));
 }
-// Many: a wave for 16 rows of a tile of 64, blockIdx.y the outputs.
+// Many: a tile of 64 rows, four waves with 16 each, and a.per_wave outputs. As expand, but the waves bring the weights into LDS
+// together, into one of two places while the other is read.
 template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
-  const int wave = blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64, first = wave % 4 * 16, o0 = blockIdx.y * a.per_wave;
-  if (wave / 4 >= *a.n_tiles) return;
-  const int4 tile = a.tiles[wave / 4];
-  if (first >= tile.z) return;
-  const int slot = first + threadIdx.x % 16;
-  const Tile<1> t = {tile.x, min(tile.z - first, 16), {a.order[tile.y + (slot < tile.z ? slot : first)]}};
-  expand<DT, kWide, kEights, true>(a, t, o0, min(o0 + a.per_wave, a.ad.d_out), own_lds<DT>(a));
+  typedef Parts<DT> P;
+  constexpr int kParts = P::kN, kSize = kWide ? 4 : 2;
+  extern __shared__ __align__(16) char all[];
+  u32x4_t(*const shared)[8][68] = (u32x4_t(*)[8][68])all;                    // [2][8][68]
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
+  // Neighbours in the grid take neighbouring outputs of the same rows.
+  const int parts = (d_out + a.per_wave - 1) / a.per_wave, at_tile = blockIdx.x / parts;
+  if (at_tile >= *a.n_tiles) return;
+  const int4 tile = a.tiles[at_tile];
+  const int first = 16 * wave, count = min(max(tile.z - first, 0), 16), rank = own_rank(a, tile.x);
+  const int o0 = (blockIdx.x - at_tile * parts) * a.per_wave, o1 = min(o0 + a.per_wave, d_out);
+  if (rank == 0 && (a.base == a.out || count == 0)) return;                  // of a whole tile, or of a wave that copies nothing
+  // The wave's rows 4 q + j; for those that do not exist the tile's first.
+  int row[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) row[j] = a.order[tile.y + (4 * q + j < count ? first + 4 * q + j : 0)];
+  const auto fresh = [](int v) { asm volatile("" : "+v"(v)); return v; };
+  const auto load_rows = [&](Eight<kWide>* y, int o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = load_y<kWide, kEights>((const char*)a.base + fresh(row[j]) * (a.base_stride * kSize), o + 8 * c, d_out);
+  };
+  const auto store_rows = [&](const Eight<kWide>* y, int o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (4 * q + j < count)
+        store_y<kWide, kEights, true>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
+  };
+  Eight<kWide> y[4];
+  if (rank == 0) {
+    for (int o = o0; o < o1; o += 128) {
+      load_rows(y, o);
+      store_rows(y, o);
+    }
+    return;
+  }
+
+  // A thread's one or two pieces of 8 of a step's 128 x 32 weights; `pieces` threads side by side to an output's row.
+  const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)tile.x * d_out * stack;
+  const auto load_w = [&](u32x4_t* w, int o, int kt) {
+    const int left = rank - 32 * kt, shift = left > 16 ? 2 : left > 8 ? 1 : 0, k = 32 * kt + 8 * (threadIdx.x & ((1 << shift) - 1));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = (256 * j + (int)threadIdx.x) >> shift;
+      if (at >= 128) continue;
+      const uint32_t r = min(o + at, d_out - 1) * (uint32_t)stack;           // below 2^31
+      if constexpr (kEights) w[j] = load8(b, r + min(k, stack - 8));
+      else w[j] = stack >= 8 ? load8_moved(b + r, k, stack) : load8(b + r, k, stack);
+    }
+  };
+  const auto place_w = [&](const u32x4_t* w, u32x4_t (*to)[68], int kt) {
+    const int left = rank - 32 * kt, shift = left > 16 ? 2 : left > 8 ? 1 : 0, piece = threadIdx.x & ((1 << shift) - 1);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = (256 * j + (int)threadIdx.x) >> shift;
+      if (at < 128) to[at % 8][at / 8 * 4 + (piece ^ (at / 32))] = w[j];
+    }
+  };
+  u32x4_t w[2];
+  load_w(w, o0, 0);
+  load_rows(y, o0);
+  u32x4_t(*const t)[kParts][64] = (u32x4_t(*)[kParts][64])(all + 2 * sizeof(*shared)) + wave * ((stack + 31) / 32);
+  __shared__ float backs[4][16];
+  if (count) operands<DT>(a, a.order[tile.y + (c < count ? first + c : 0)], rank, a.ad.scales ? a.ad.scales[tile.x] : 1.f, t, backs[wave]);
+
+  int n = 0;
+  for (int o = o0; o < o1; o += 128) {
+    const bool more = o + 128 < o1;
+    Eight<kWide> next[4];
+    if (more && count) load_rows(next, o + 128);
+    f32x4_t acc[8] = {};
+    for (int kt = 0; 32 * kt < rank; ++kt, n ^= 1) {
+      const bool last = 32 * (kt + 1) >= rank;
+      place_w(w, shared[n], kt);
+      if (!last) load_w(w, o, kt + 1);
+      else if (more) load_w(w, o + 128, 0);
+      __syncthreads();
+      if (count == 0) continue;
+      u32x4_t tv[kParts];
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) tv[p] = t[kt][p][lane];
+      u32x4_t mask;
+      if (last) mask = own_values(rank - 32 * kt - 8 * q);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        u32x4_t wv = shared[n][m][c * 4 + (q ^ (c / 4))];
+        if (last) wv &= mask;
+#pragma unroll
+        for (int p = kParts - 1; p >= 0; --p) acc[m] = mma<DT>(tv[p], wv, acc[m]);
+      }
+    }
+    if (count == 0) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? backs[wave][4 * q + j] : 1.f, a.y_f16);
+    store_rows(y, o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = next[j];
+  }
 }
 
 // Many rows sorted by adapter (those without one last), and cut into tiles of up to 64 (adapter, first, count): one workgroup
@@ -653,19 +747,26 @@ __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
 #pragma unroll
   for (int k = 0; k < 2; ++k)
     for (int w = 0; w < wave; ++w) before[k] += sums[k][w];
+  // No store to memory before the barriers: they would wait for it.
+  int start = before[0];
   for (int i = b0; i < b1; ++i) {
     const int count = bins[i];
-    bins[i] = before[0];
-    for (int j = 0; j < count; j += 64) a.tiles[before[1]++] = make_int4(i < a.ad.n_adapters ? i : -1, before[0] + j, min(count - j, 64), 0);
-    before[0] += count;
+    bins[i] = start;
+    start += count;
   }
-  if (threadIdx.x == 1023) *a.n_tiles = before[1];
   __syncthreads();
+  int at_tile = before[1];
+  for (int i = b0; i < b1; ++i) {
+    const int r0 = bins[i], count = (i + 1 < n_bins ? bins[i + 1] : a.n_rows) - r0;
+    for (int j = 0; j < count; j += 64) a.tiles[at_tile++] = make_int4(i < a.ad.n_adapters ? i : -1, r0 + j, min(count - j, 64), 0);
+  }
+  if (threadIdx.x == 1023) *a.n_tiles = at_tile;
   if (once) {
 #pragma unroll
     for (int j = 0; j < kEach; ++j) at[j] += bins[n[j]];
     place(0);
   } else {
+    __syncthreads();
     for (int r0 = 0; r0 < a.n_rows; r0 += 1024 * kEach) {
       take(r0);
       place(r0);
@@ -683,9 +784,17 @@ template <int DT, bool kWide, bool kEights>
 hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
   const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
   const int steps = (a.ad.rank + 31) / 32, waves = steps <= 2 ? 4 : steps <= 4 ? 2 : 1;   // within 64 KiB of LDS
-  const size_t lds = waves * expand_lds<DT>(steps);
-  if (p.few) expand_few<DT, kWide, kEights><<<dim3((parts + waves - 1) / waves, a.n_rows), 64 * waves, lds, st>>>(a);
-  else expand_many<DT, kWide, kEights><<<dim3(p.tiles * (4 / waves), parts), 64 * waves, lds, st>>>(a);
+  if (p.few) {
+    expand_few<DT, kWide, kEights><<<dim3((parts + waves - 1) / waves, a.n_rows), 64 * waves, waves * expand_lds<DT>(steps), st>>>(a);
+  } else {
+    const size_t lds = 2 * sizeof(u32x4_t[8][68]) + 4 * steps * sizeof(u32x4_t[Parts<DT>::kN][64]);
+    const auto kernel = expand_many<DT, kWide, kEights>;
+    if (lds + 256 > 65536) {           // with the kernel's own
+      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    kernel<<<p.tiles * parts, 256, lds, st>>>(a);
+  }
   return hipGetLastError();
 }
 template <int DT, bool kWide>

@@ -114,6 +114,17 @@ def test_strides_no_scales_and_foreign_indexes(rows):
     assert torch.equal(wide[:, :5], kept[:, :5]) and torch.equal(wide[:, 104:], kept[:, 104:])
 
 
+@pytest.mark.parametrize("n", [1, 3, 8192])
+@pytest.mark.parametrize("spans", [False, True])
+def test_more_rows_than_are_sorted_at_once(n, spans):
+    g = gen(n)
+    ad = make(g, n, 4, 16, 24, BF16)
+    x, base = normal(g, 20011, 16, dtype=BF16), normal(g, 20011, 24, dtype=BF16)
+    index, out = index_of(g, 20011, n, spans), torch.empty_like(base)
+    ad.add(x, index, base, out)
+    check(ad, x, index, base, out)
+
+
 def test_no_row_has_an_adapter():
     g = gen(3)
     ad = make(g, 2, 8, 64, 70, F16)
