@@ -4,8 +4,8 @@
 // out = base + B_n (s_n t). Rows that share an adapter are the columns of matrix instructions, 16 each, with 16 rows of A
 // or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows:
 // every wave finds its 16 by votes over 64 rows' indexes; the adapters' bytes and the latency of two launches bound them
-// (one row, rank 16, 4096 x 4096: 3.7 + 5.1 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
-// and out (8192 rows, rank 32, 4096 x 4096: sort 9 us, t 14.6 us, 4.6 TB/s, the outputs 38 us, 3.5 TB/s).
+// (one row, rank 16, 4096 x 4096: 3.4 + 5.3 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
+// and out (8192 rows, rank 32, 4096 x 4096: sort 10 us, t 14.5 us, 4.6 TB/s, the outputs 34 us, 4.0 TB/s).
 #include "device.h"
 #include "ops.h"
 
@@ -87,38 +87,33 @@ __device__ __forceinline__ Rows rows_at(const AdapterArgs& a, int row0) {
   if ((unsigned)r.adapter >= (unsigned)a.ad.n_adapters) r.adapter = -1;
   return r;
 }
-// Up to 16 CT of them that share an adapter. Slot 16 c + i of them is column i of c.
-template <int CT>
+// Up to 16 of them that share an adapter.
 struct Tile {
   int adapter, count;
-  int row[CT];         // of slots 16 c + lane % 16; those past count repeat the first
+  int row;             // of slot lane % 16; slots past count repeat the first
 };
 // The rows of `mask` from number `first` on. All lanes of the wave take part.
-template <int CT>
-__device__ __forceinline__ Tile<CT> tile_of(const Rows& r, uint64_t mask, int adapter, int first) {
+__device__ __forceinline__ Tile tile_of(const Rows& r, uint64_t mask, int adapter, int first) {
   const int lane = threadIdx.x % 64;
-  Tile<CT> t;
+  Tile t;
   t.adapter = adapter;
-  t.count = min(__builtin_popcountll(mask) - first, 16 * CT);
+  t.count = min(__builtin_popcountll(mask) - first, 16);
   // Each row's lane sends its number to its slot; the others to lane 63, which is no slot then. Then all read theirs.
   const int at = __builtin_popcountll(mask & ((1ull << lane) - 1)) - first;
   const bool mine = (mask >> lane & 1) && at >= 0 && at < t.count;
   const int sent = __builtin_amdgcn_ds_permute((mine ? at : 63) * 4, r.row);
-#pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int slot = 16 * c + lane % 16;
-    t.row[c] = __builtin_amdgcn_ds_bpermute((slot < t.count ? slot : 0) * 4, sent);
-  }
+  const int slot = lane % 16;
+  t.row = __builtin_amdgcn_ds_bpermute((slot < t.count ? slot : 0) * 4, sent);
   return t;
 }
 // The tile of 16 that starts with row `start`, if one does: every 16th of its adapter's rows among its 64 starts one.
-__device__ __forceinline__ bool tile_at(const AdapterArgs& a, int start, Tile<1>& t) {
+__device__ __forceinline__ bool tile_at(const AdapterArgs& a, int start, Tile& t) {
   const Rows r = rows_at(a, start / kRows * kRows);
   const int l = start % kRows, n = __builtin_amdgcn_readlane(r.adapter, l);
   const uint64_t mask = __ballot(r.in && r.adapter == n);
   const int first = __builtin_popcountll(mask & ((1ull << l) - 1));
   if (first % 16) return false;
-  t = tile_of<1>(r, mask, n, first);
+  t = tile_of(r, mask, n, first);
   return true;
 }
 
@@ -132,12 +127,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
   constexpr int U = RT <= 2 ? 4 : RT <= 4 ? 2 : 1;                 // steps of 32 inputs loaded at once
   __shared__ __align__(16) float lds[2][kFewWaves][256];
   __shared__ int slots[16];
-  Tile<1> t;
+  Tile t;
   if (!tile_at(a, blockIdx.x, t)) return;
   const int rank = own_rank(a, t.adapter);
   if (rank == 0) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, kg = lane / 16 * 8, d_in = a.ad.d_in;
-  const uint16_t* x = (const uint16_t*)a.x + t.row[0] * a.x_stride + kg;
+  const uint16_t* x = (const uint16_t*)a.x + t.row * a.x_stride + kg;
   const uint16_t* w[RT];
 #pragma unroll
   for (int m = 0; m < RT; ++m)
@@ -189,7 +184,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
 
   // The waves' sums added up, 16 values of t at a time.
   float* out = a.t + (int64_t)blockIdx.y * a.n_rows * a.t_stride;
-  if (threadIdx.x < 16) slots[threadIdx.x] = t.row[0];
+  if (threadIdx.x < 16) slots[threadIdx.x] = t.row;
 #pragma unroll
   for (int m = 0; m < RT; ++m) {
     if (16 * m >= rank) break;                                     // the whole workgroup
@@ -307,18 +302,11 @@ template <> struct Parts<AQMB_F16> {
   static __device__ __forceinline__ float lo(uint32_t w) { return f16lo(w); }
   static __device__ __forceinline__ float hi(uint32_t w) { return f16hi(w); }
 };
-// What a wave of the second launch keeps in LDS: the factor of 16 rows' results; 128 outputs' weights of a step of 32 of the
-// rank, output 8 c + n as row 16 n + c, where the matrix instructions take it, 64 bytes a row, the four pieces swapped by c / 4
-// against bank conflicts; and t's operands of every step.
-template <int DT>
-struct ExpandLds {
-  float back[16];
-  u32x4_t w[8][68];
-  u32x4_t t[1][Parts<DT>::kN][64];
-};
-template <int DT>
-constexpr size_t expand_lds(int steps) { return sizeof(ExpandLds<DT>) + (steps - 1) * sizeof(ExpandLds<DT>::t); }
-
+// What the second launch keeps in LDS: 128 outputs' weights of a step of 32 of the rank, output 8 c + n as row 16 n + c,
+// where the matrix instructions take it, 64 bytes a row, the four pieces swapped by c / 4 against bank conflicts; and t's
+// operands of every step and part.
+typedef u32x4_t WeightsLds[8][68];
+template <int DT> using OperandsLds = u32x4_t[Parts<DT>::kN][64];
 
 // Which of a lane's 8 values are an adapter's own, the first `left`, as a mask.
 __device__ __forceinline__ u32x4_t own_values(int left) {
@@ -329,8 +317,7 @@ __device__ __forceinline__ u32x4_t own_values(int left) {
 // s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave, into to[step][part][lane]; the
 // factor of the rows' results (fp16) into back.
 template <int DT>
-__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, u32x4_t (*to)[Parts<DT>::kN][64],
-                                         float* back) {
+__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, OperandsLds<DT>* to, float* back) {
   typedef Parts<DT> P;
   const int lane = threadIdx.x % 64, q = lane / 16, steps = (rank + 31) / 32;
   const float* tp = a.t + (int64_t)row * a.t_stride + 8 * q;
@@ -480,18 +467,26 @@ __device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], in
   }
 }
 
-// Outputs o0 .. o1 - 1 (o0 a multiple of 128) of up to 16 rows that share an adapter, by one wave. Lane (q, c) of 4 x 16 has
-// outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and writes 256 bytes of a row at once
-// (with lanes side by side on different rows every lane was an access of its own to the vector cache, which bound
-// the kernel: 8192 rows of 4096 outputs 45 us).
-template <int DT, bool kWide, bool kEights, bool kStream>
-__device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, int o0, int o1, ExpandLds<DT>& lds) {
+// Few rows: blockIdx.y is the row that a tile starts with, each of four waves takes a.per_wave outputs (a multiple of
+// 128). Lane (q, c) of 4 x 16 has outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and
+// writes 256 bytes of a row at once (with lanes side by side on different rows every lane was an access of its own to the
+// vector cache, which bound the kernel: 8192 rows of 4096 outputs 45 us). Bound by latency (5.1 us) or the adapters' bytes
+// (32 rows with 8 adapters of rank 64, 4096 x 11008: 16 us).
+template <int DT, bool kWide, bool kEights>
+__global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
-  const int lane = threadIdx.x % 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
+  extern __shared__ __align__(16) char all[];            // the waves' weights, t's operands
+  __shared__ float back[16];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
+  WeightsLds& weights = ((WeightsLds*)all)[wave];
+  OperandsLds<DT>* const operand = (OperandsLds<DT>*)(all + 4 * sizeof(WeightsLds));
+  Tile t;
+  if (!tile_at(a, blockIdx.y, t)) return;                // the whole workgroup
+  const int o0 = (int)min(((int64_t)blockIdx.x * 4 + wave) * a.per_wave, (int64_t)d_out), o1 = min(o0 + a.per_wave, d_out);
   int rank = stack;
   int row[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row[0]);
+  for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row);
   // A value that the compiler takes for new in every step: addresses made from it are not kept in registers between steps.
   const auto fresh = [](int v) { asm volatile("" : "+v"(v)); return v; };
   const auto load_rows = [&](Eight<kWide>* y, int o) {
@@ -503,7 +498,7 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (4 * q + j < t.count)
-        store_y<kWide, kEights, kStream>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
+        store_y<kWide, kEights, false>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
   };
   // Weights in pieces of 8: `pieces` lanes side by side (a power of two) to an output's row of a step.
   const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * stack;
@@ -524,14 +519,16 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
       const int o = (64 * j + l) >> shift, piece = l & ((1 << shift) - 1);
-      lds.w[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
+      weights[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
     }
   };
   // The first weights and rows of base are on their way while t comes; so are the next ones later.
   u32x4_t w[8];
   Eight<kWide> y[4];
-  if (t.adapter >= 0) load_w(w, o0, 0);
-  load_rows(y, o0);
+  if (o0 < o1) {
+    if (t.adapter >= 0) load_w(w, o0, 0);
+    load_rows(y, o0);
+  }
   rank = own_rank(a, t.adapter);                         // only now: the loads above do not wait for it
   if (rank == 0) {
     for (int o = o0; a.base != a.out && o < o1; o += 128) {
@@ -541,7 +538,8 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
     return;
   }
   const u32x4_t mask = own_values(rank - (rank - 1) / 32 * 32 - 8 * q);      // of the last step
-  operands<DT>(a, t.row[0], rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, lds.t, lds.back);
+  if (wave == 0) operands<DT>(a, t.row, rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, operand, back);
+  __syncthreads();
 
   for (int o = o0; o < o1; o += 128) {
     const bool more = o + 128 < o1;
@@ -555,44 +553,32 @@ __device__ __forceinline__ void expand(const AdapterArgs& a, const Tile<1>& t, i
       lds_order();
       u32x4_t tv[kParts];
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) tv[p] = lds.t[kt][p][lane];
+      for (int p = 0; p < kParts; ++p) tv[p] = operand[kt][p][lane];
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
-        u32x4_t wv = lds.w[n][c * 4 + (q ^ (c / 4))];
+        u32x4_t wv = weights[n][c * 4 + (q ^ (c / 4))];
         if (last) wv &= mask;
 #pragma unroll
         for (int p = kParts - 1; p >= 0; --p) acc[n] = mma<DT>(tv[p], wv, acc[n]);
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? lds.back[4 * q + j] : 1.f, a.y_f16);
+    for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? back[4 * q + j] : 1.f, a.y_f16);
     store_rows(y, o);
     if (more) load_rows(y, o + 128);
   }
 }
 
-// A wave's part of the workgroup's LDS.
-template <int DT>
-__device__ __forceinline__ ExpandLds<DT>& own_lds(const AdapterArgs& a) {
-  extern __shared__ __align__(16) char all[];
-  return *(ExpandLds<DT>*)(all + threadIdx.x / 64 * expand_lds<DT>((a.ad.rank + 31) / 32));
-}
-// Few rows: blockIdx.y is the row that a tile starts with, a wave for a.per_wave outputs.
+// Many: a tile of 64 rows, four waves with 16 each, and a.per_wave outputs. As expand_few, but the waves bring the weights
+// into LDS together, into one of two places while the other is read (each its own: 8192 rows of 4096 outputs at rank 32
+// 41 us, now 34; a call at rank 128 165 us, now 134), and the next outputs of base are loaded a step ahead. As many waves
+// as registers allow without spills (two for each of four units, not four: 38 us).
 template <int DT, bool kWide, bool kEights>
-__global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
-  const int64_t o0 = ((int64_t)blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64) * a.per_wave;
-  Tile<1> t;
-  if (tile_at(a, blockIdx.y, t) && o0 < a.ad.d_out)
-    expand<DT, kWide, kEights, false>(a, t, (int)o0, (int)min(o0 + a.per_wave, (int64_t)a.ad.d_out), own_lds<DT>(a));
-}
-// Many: a tile of 64 rows, four waves with 16 each, and a.per_wave outputs. As expand, but the waves bring the weights into LDS
-// together, into one of two places while the other is read.
-template <int DT, bool kWide, bool kEights>
-__global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
+__global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(AdapterArgs a) {
   typedef Parts<DT> P;
   constexpr int kParts = P::kN, kSize = kWide ? 4 : 2;
   extern __shared__ __align__(16) char all[];
-  u32x4_t(*const shared)[8][68] = (u32x4_t(*)[8][68])all;                    // [2][8][68]
+  WeightsLds* const shared = (WeightsLds*)all;                               // two
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
   // Neighbours in the grid take neighbouring outputs of the same rows.
   const int parts = (d_out + a.per_wave - 1) / a.per_wave, at_tile = blockIdx.x / parts;
@@ -639,7 +625,7 @@ __global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
       else w[j] = stack >= 8 ? load8_moved(b + r, k, stack) : load8(b + r, k, stack);
     }
   };
-  const auto place_w = [&](const u32x4_t* w, u32x4_t (*to)[68], int kt) {
+  const auto place_w = [&](const u32x4_t* w, WeightsLds& to, int kt) {
     const int left = rank - 32 * kt, shift = left > 16 ? 2 : left > 8 ? 1 : 0, piece = threadIdx.x & ((1 << shift) - 1);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -650,7 +636,7 @@ __global__ __launch_bounds__(256) void expand_many(AdapterArgs a) {
   u32x4_t w[2];
   load_w(w, o0, 0);
   load_rows(y, o0);
-  u32x4_t(*const t)[kParts][64] = (u32x4_t(*)[kParts][64])(all + 2 * sizeof(*shared)) + wave * ((stack + 31) / 32);
+  OperandsLds<DT>* const t = (OperandsLds<DT>*)(all + 2 * sizeof(WeightsLds)) + wave * ((stack + 31) / 32);
   __shared__ float backs[4][16];
   if (count) operands<DT>(a, a.order[tile.y + (c < count ? first + c : 0)], rank, a.ad.scales ? a.ad.scales[tile.x] : 1.f, t, backs[wave]);
 
@@ -783,17 +769,17 @@ hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st)
 template <int DT, bool kWide, bool kEights>
 hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
   const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
-  const int steps = (a.ad.rank + 31) / 32, waves = steps <= 2 ? 4 : steps <= 4 ? 2 : 1;   // within 64 KiB of LDS
-  if (p.few) {
-    expand_few<DT, kWide, kEights><<<dim3((parts + waves - 1) / waves, a.n_rows), 64 * waves, waves * expand_lds<DT>(steps), st>>>(a);
+  const size_t operands = (a.ad.rank + 31) / 32 * sizeof(OperandsLds<DT>);
+  if (p.few) {                         // within 64 KiB of LDS at any rank
+    expand_few<DT, kWide, kEights><<<dim3((parts + 3) / 4, a.n_rows), 256, 4 * sizeof(WeightsLds) + operands, st>>>(a);
   } else {
-    const size_t lds = 2 * sizeof(u32x4_t[8][68]) + 4 * steps * sizeof(u32x4_t[Parts<DT>::kN][64]);
+    const size_t lds = 2 * sizeof(WeightsLds) + 4 * operands;
     const auto kernel = expand_many<DT, kWide, kEights>;
     if (lds + 256 > 65536) {           // with the kernel's own
       const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
       if (e != hipSuccess) return e;
     }
-    kernel<<<p.tiles * parts, 256, lds, st>>>(a);
+    kernel<<<p.tiles * parts, 256, lds, st>>>(a);      // below 2^24: check_adapters
   }
   return hipGetLastError();
 }
@@ -817,10 +803,11 @@ hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStr
 
 }  // namespace
 
-// Few rows take a look at 64 rows for every tile of 16; above 192 a sort of its own (4 us for 100 rows, 9 for 8192) and tiles of 64
+// Few rows take a look at 64 rows for every tile of 16; above 192 a sort of its own (4 us for 100 rows, 10 for 8192) and tiles of 64
 // rows are cheaper. Rank 16, 4096 x 4096, 4 adapters in spans: 128 rows 12.2 us against 19.3, 256 17.9 and 19.8, 512 32.1 and
 // 20.2; 64 adapters in any order: 15.3 and 24.8, 25.1 and 27.4, 43.3 and 29.5; rank 64, 11008 outputs, 8 adapters: 26.9 and 29.3,
-// 38.3 and 33.6, 65 and 46. Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
+// 38.3 and 33.6, 65 and 46. Many: 256 outputs a workgroup (8192 rows: 128 take 76 us against 67, 512 70), 128 where that
+// leaves fewer than 512 (1024 rows 20.9 us against 23.0, 300 18.4 against 21.0). Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
 constexpr int kFewRows = 192;
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   AdapterPlan p;
@@ -834,7 +821,7 @@ AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   } else {
     p.splits = 512 / ((n_rows + kRows - 1) / kRows);
     if (p.splits > steps / 16) p.splits = steps / 16;
-    p.per_wave = 256;
+    p.per_wave = (int64_t)p.tiles * ((ad.d_out + 255) / 256) < 512 ? 128 : 256;
   }
   if (p.splits > kMaxSplits) p.splits = kMaxSplits;
   if (p.splits < 1) p.splits = 1;
