@@ -4,7 +4,7 @@
 // out = base + B_n (s_n t). Rows that share an adapter are the columns of matrix instructions, 16 each, with 16 rows of A
 // or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows:
 // every wave finds its 16 by votes over 64 rows' indexes; the adapters' bytes and the latency of two launches bound them
-// (one row, rank 16, 4096 x 4096: 3.4 + 5.3 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
+// (one row, rank 16, 4096 x 4096: 3.5 + 4.9 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
 // and out (8192 rows, rank 32, 4096 x 4096: sort 10 us, t 14.5 us, 4.6 TB/s, the outputs 34 us, 4.0 TB/s).
 #include "device.h"
 #include "ops.h"
@@ -467,11 +467,10 @@ __device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], in
   }
 }
 
-// Few rows: blockIdx.y is the row that a tile starts with, each of four waves takes a.per_wave outputs (a multiple of
-// 128). Lane (q, c) of 4 x 16 has outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and
+// Few rows: blockIdx.y is the row that a tile starts with, each of four waves takes 128 outputs. Lane (q, c) of 4 x 16 has outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and
 // writes 256 bytes of a row at once (with lanes side by side on different rows every lane was an access of its own to the
-// vector cache, which bound the kernel: 8192 rows of 4096 outputs 45 us). Bound by latency (5.1 us) or the adapters' bytes
-// (32 rows with 8 adapters of rank 64, 4096 x 11008: 16 us).
+// vector cache, which bound the kernel: 8192 rows of 4096 outputs 45 us). Bound by latency (4.9 us) or the adapters' bytes
+// (32 rows of some 25 adapters of rank 64, 11008 outputs: 13 us).
 template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
@@ -482,29 +481,22 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
   OperandsLds<DT>* const operand = (OperandsLds<DT>*)(all + 4 * sizeof(WeightsLds));
   Tile t;
   if (!tile_at(a, blockIdx.y, t)) return;                // the whole workgroup
-  const int o0 = (int)min(((int64_t)blockIdx.x * 4 + wave) * a.per_wave, (int64_t)d_out), o1 = min(o0 + a.per_wave, d_out);
+  const int o = (blockIdx.x * 4 + wave) * 128;
   int rank = stack;
   int row[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_ds_bpermute(4 * (4 * q + j), t.row);
-  // A value that the compiler takes for new in every step: addresses made from it are not kept in registers between steps.
-  const auto fresh = [](int v) { asm volatile("" : "+v"(v)); return v; };
-  const auto load_rows = [&](Eight<kWide>* y, int o) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      y[j] = load_y<kWide, kEights>((const char*)a.base + fresh(row[j]) * (a.base_stride * kSize), o + 8 * c, d_out);
-  };
-  const auto store_rows = [&](const Eight<kWide>* y, int o) {
+  const auto store_rows = [&](const Eight<kWide>* y) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (4 * q + j < t.count)
-        store_y<kWide, kEights, false>((char*)a.out + fresh(row[j]) * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
+        store_y<kWide, kEights, false>((char*)a.out + row[j] * (a.out_stride * kSize), o + 8 * c, d_out, y[j]);
   };
   // Weights in pieces of 8: `pieces` lanes side by side (a power of two) to an output's row of a step.
   const uint16_t* b = (const uint16_t*)a.ad.b + (int64_t)t.adapter * d_out * stack;
-  const auto shift_of = [&](int kt) { const int left = (kt == 0 ? stack : rank) - 32 * kt; return left > 16 ? 2 : left > 8 ? 1 : 0; };
-  const auto load_w = [&](u32x4_t* w, int o, int kt) {
-    const int shift = shift_of(kt), l = fresh(lane), k = 32 * kt + 8 * (l & ((1 << shift) - 1));
+  const auto shift_of = [&](int kt) { const int left = (kt < 2 ? stack : rank) - 32 * kt; return left > 16 ? 2 : left > 8 ? 1 : 0; };
+  const auto load_w = [&](u32x4_t* w, int kt) {
+    const int shift = shift_of(kt), l = lane, k = 32 * kt + 8 * (l & ((1 << shift) - 1));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
@@ -514,7 +506,7 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
     }
   };
   const auto place_w = [&](const u32x4_t* w, int kt) {
-    const int shift = shift_of(kt), l = fresh(lane);
+    const int shift = shift_of(kt), l = lane;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
@@ -522,54 +514,53 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
       weights[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
     }
   };
-  // The first weights and rows of base are on their way while t comes; so are the next ones later.
-  u32x4_t w[8];
+  // Two steps' weights and the rows of base are on their way while t and the adapter's rank come.
+  u32x4_t w[2][8];
   Eight<kWide> y[4];
-  if (o0 < o1) {
-    if (t.adapter >= 0) load_w(w, o0, 0);
-    load_rows(y, o0);
+  if (o < d_out) {
+    if (t.adapter >= 0) load_w(w[0], 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = load_y<kWide, kEights>((const char*)a.base + row[j] * (a.base_stride * kSize), o + 8 * c, d_out);
+    if (t.adapter >= 0 && stack > 32) load_w(w[1], 1);
   }
-  rank = own_rank(a, t.adapter);                         // only now: the loads above do not wait for it
+  rank = own_rank(a, t.adapter);
   if (rank == 0) {
-    for (int o = o0; a.base != a.out && o < o1; o += 128) {
-      if (o != o0) load_rows(y, o);
-      store_rows(y, o);
-    }
+    if (a.base != a.out && o < d_out) store_rows(y);
     return;
   }
   const u32x4_t mask = own_values(rank - (rank - 1) / 32 * 32 - 8 * q);      // of the last step
   if (wave == 0) operands<DT>(a, t.row, rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, operand, back);
   __syncthreads();
+  if (o >= d_out) return;
 
-  for (int o = o0; o < o1; o += 128) {
-    const bool more = o + 128 < o1;
-    f32x4_t acc[8] = {};
-    for (int kt = 0; 32 * kt < rank; ++kt) {
-      const bool last = 32 * (kt + 1) >= rank;
-      lds_order();
-      place_w(w, kt);
-      if (!last) load_w(w, o, kt + 1);
-      else if (more) load_w(w, o + 128, 0);
-      lds_order();
-      u32x4_t tv[kParts];
+  f32x4_t acc[8] = {};
+  const auto step = [&](u32x4_t* w, int kt) {
+    lds_order();
+    place_w(w, kt);
+    if (32 * (kt + 2) < rank) load_w(w, kt + 2);
+    lds_order();
+    u32x4_t tv[kParts];
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) tv[p] = operand[kt][p][lane];
+    for (int p = 0; p < kParts; ++p) tv[p] = operand[kt][p][lane];
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        u32x4_t wv = weights[n][c * 4 + (q ^ (c / 4))];
-        if (last) wv &= mask;
+    for (int n = 0; n < 8; ++n) {
+      u32x4_t wv = weights[n][c * 4 + (q ^ (c / 4))];
+      if (32 * (kt + 1) >= rank) wv &= mask;
 #pragma unroll
-        for (int p = kParts - 1; p >= 0; --p) acc[n] = mma<DT>(tv[p], wv, acc[n]);
-      }
+      for (int p = kParts - 1; p >= 0; --p) acc[n] = mma<DT>(tv[p], wv, acc[n]);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? back[4 * q + j] : 1.f, a.y_f16);
-    store_rows(y, o);
-    if (more) load_rows(y, o + 128);
+  };
+  for (int kt = 0; 32 * kt < rank; kt += 2) {
+    step(w[0], kt);
+    if (32 * (kt + 1) < rank) step(w[1], kt + 1);
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) add_y<kWide, DT == AQMB_F16>(y[j], acc, j, DT == AQMB_F16 ? back[4 * q + j] : 1.f, a.y_f16);
+  store_rows(y);
 }
 
-// Many: a tile of 64 rows, four waves with 16 each, and a.per_wave outputs. As expand_few, but the waves bring the weights
+// Many: a tile of 64 rows, four waves with 16 each, and a.per_group outputs. As expand_few, but the waves bring the weights
 // into LDS together, into one of two places while the other is read (each its own: 8192 rows of 4096 outputs at rank 32
 // 41 us, now 34; a call at rank 128 165 us, now 134), and the next outputs of base are loaded a step ahead. As many waves
 // as registers allow without spills (two for each of four units, not four: 38 us).
@@ -581,16 +572,17 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(Ad
   WeightsLds* const shared = (WeightsLds*)all;                               // two
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
   // Neighbours in the grid take neighbouring outputs of the same rows.
-  const int parts = (d_out + a.per_wave - 1) / a.per_wave, at_tile = blockIdx.x / parts;
+  const int parts = (d_out + a.per_group - 1) / a.per_group, at_tile = blockIdx.x / parts;
   if (at_tile >= *a.n_tiles) return;
   const int4 tile = a.tiles[at_tile];
   const int first = 16 * wave, count = min(max(tile.z - first, 0), 16), rank = own_rank(a, tile.x);
-  const int o0 = (blockIdx.x - at_tile * parts) * a.per_wave, o1 = min(o0 + a.per_wave, d_out);
+  const int o0 = (blockIdx.x - at_tile * parts) * a.per_group, o1 = min(o0 + a.per_group, d_out);
   if (rank == 0 && (a.base == a.out || count == 0)) return;                  // of a whole tile, or of a wave that copies nothing
   // The wave's rows 4 q + j; for those that do not exist the tile's first.
   int row[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) row[j] = a.order[tile.y + (4 * q + j < count ? first + 4 * q + j : 0)];
+  // A value that the compiler takes for new in every step: addresses made from it are not kept in registers between steps.
   const auto fresh = [](int v) { asm volatile("" : "+v"(v)); return v; };
   const auto load_rows = [&](Eight<kWide>* y, int o) {
 #pragma unroll
@@ -768,11 +760,11 @@ hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st)
 }
 template <int DT, bool kWide, bool kEights>
 hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  const unsigned parts = (a.ad.d_out + a.per_wave - 1) / a.per_wave;
   const size_t operands = (a.ad.rank + 31) / 32 * sizeof(OperandsLds<DT>);
   if (p.few) {                         // within 64 KiB of LDS at any rank
-    expand_few<DT, kWide, kEights><<<dim3((parts + 3) / 4, a.n_rows), 256, 4 * sizeof(WeightsLds) + operands, st>>>(a);
+    expand_few<DT, kWide, kEights><<<dim3((a.ad.d_out + 511) / 512, a.n_rows), 256, 4 * sizeof(WeightsLds) + operands, st>>>(a);
   } else {
+    const int parts = (a.ad.d_out + a.per_group - 1) / a.per_group;
     const size_t lds = 2 * sizeof(WeightsLds) + 4 * operands;
     const auto kernel = expand_many<DT, kWide, kEights>;
     if (lds + 256 > 65536) {           // with the kernel's own
@@ -803,25 +795,26 @@ hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStr
 
 }  // namespace
 
-// Few rows take a look at 64 rows for every tile of 16; above 192 a sort of its own (4 us for 100 rows, 10 for 8192) and tiles of 64
-// rows are cheaper. Rank 16, 4096 x 4096, 4 adapters in spans: 128 rows 12.2 us against 19.3, 256 17.9 and 19.8, 512 32.1 and
-// 20.2; 64 adapters in any order: 15.3 and 24.8, 25.1 and 27.4, 43.3 and 29.5; rank 64, 11008 outputs, 8 adapters: 26.9 and 29.3,
-// 38.3 and 33.6, 65 and 46. Many: 256 outputs a workgroup (8192 rows: 128 take 76 us against 67, 512 70), 128 where that
-// leaves fewer than 512 (1024 rows 20.9 us against 23.0, 300 18.4 against 21.0). Parts of the inputs: four steps for each wave at least, few rows; about 512 workgroups, many.
-constexpr int kFewRows = 192;
+// Few rows take a look at 64 rows for every tile of 16; above 256 a sort of its own (4 us for 100 rows, 10 for 8192) and
+// tiles of 64 rows are cheaper. Rank 16, 4096 x 4096, 4 adapters in spans: 128 rows 11.8 us against 17.4, 256 16.1 and 18.2,
+// 384 22.7 and 18.4; 64 adapters in any order: 12.1 and 20.5, 20.3 and 22.4, 27.3 and 23.8; rank 64, 11008 outputs, 8
+// adapters: 25.7 and 26.7, 32.2 and 31.5, 46 and 33.7. Parts of the inputs: four steps for each wave at least, few rows;
+// about 512 workgroups, many. Many: 256 outputs a workgroup (8192 rows: 128 take 76 us against 67, 512 70), 128 where that
+// leaves fewer than 512 (1024 rows 20.9 us against 23.0, 300 18.4 against 21.0).
+constexpr int kFewRows = 256;
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   AdapterPlan p;
   const int steps = (ad.d_in + 31) / 32;
   p.few = n_rows <= kFewRows;
   const int groups = n_rows < ad.n_adapters + 1 ? n_rows : ad.n_adapters + 1;
   p.tiles = groups + (n_rows - groups) / 64;
+  p.per_group = 0;
   if (p.few) {
     p.splits = steps / (kFewWaves * 4);
-    p.per_wave = 128;
   } else {
     p.splits = 512 / ((n_rows + kRows - 1) / kRows);
     if (p.splits > steps / 16) p.splits = steps / 16;
-    p.per_wave = (int64_t)p.tiles * ((ad.d_out + 255) / 256) < 512 ? 128 : 256;
+    p.per_group = (int64_t)p.tiles * ((ad.d_out + 255) / 256) < 512 ? 128 : 256;
   }
   if (p.splits > kMaxSplits) p.splits = kMaxSplits;
   if (p.splits < 1) p.splits = 1;
@@ -836,7 +829,7 @@ AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
 hipError_t launch_adapters(AdapterArgs a, const AdapterPlan& p, aqmb_dtype y, hipStream_t st) {
   a.t_stride = p.t_stride;
   a.splits = p.splits;
-  a.per_wave = p.per_wave;
+  a.per_group = p.per_group;
   a.y_f16 = y == AQMB_F16;
   a.n_tiles = (int*)((char*)a.t + p.at_tiles);
   a.tiles = (int4*)((char*)a.t + p.at_tiles + 16);

@@ -96,15 +96,15 @@ struct AdapterArgs {
   void* out;
   int64_t x_stride, base_stride, out_stride;
   float* t;                // [splits][n_rows][t_stride]: A x, partial sums over parts of the inputs
-  int n_rows, t_stride, splits, per_wave;
+  int n_rows, t_stride, splits, per_group;
   bool y_f16;
   int* n_tiles;            // many rows: sorted by adapter into `order`, and cut into tiles (adapter, first, count, -)
   int4* tiles;
   int* order;
 };
-// How a call is cut: few rows by 16 of an adapter, many sorted, by 64 (tiles: at most so many); per_wave: outputs of a
-// wave in the second launch.
-struct AdapterPlan { bool few; int tiles, splits, per_wave, t_stride; size_t at_tiles, bytes; };
+// How a call is cut: few rows by 16 of an adapter, many sorted, by 64 (tiles: at most so many); per_group: outputs
+// of a workgroup of the latter's second launch.
+struct AdapterPlan { bool few; int tiles, splits, per_group, t_stride; size_t at_tiles, bytes; };
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows);
 hipError_t launch_adapters(AdapterArgs a, const AdapterPlan& p, aqmb_dtype y, hipStream_t st);
 

@@ -71,7 +71,8 @@ def index_of(g, n_rows, n, spans):
 @pytest.mark.parametrize("rows,n,rank,d_in,d_out,spans", [
     (1, 1, 16, 512, 512, False), (1, 3, 8, 8, 8, False), (2, 4, 1, 1, 1, False), (16, 20, 16, 264, 136, False), (33, 7, 20, 257, 131, False),
     (64, 64, 64, 520, 300, False), (63, 2, 33, 1000, 65, True), (65, 3, 128, 96, 64, True), (200, 70, 12, 100, 77, False),
-    (300, 4, 256, 40, 333, True), (17, 2, 5, 7, 63, True), (129, 1, 32, 320, 257, False), (1000, 5, 40, 72, 48, True)])
+    (300, 4, 256, 40, 333, True), (17, 2, 5, 7, 63, True), (129, 1, 32, 320, 257, False), (1000, 5, 40, 72, 48, True),
+    (257, 9, 20, 257, 131, False), (700, 3, 200, 520, 300, False), (520, 40, 64, 136, 264, True), (4100, 3, 16, 72, 2100, False)])
 def test_adapters(rows, n, rank, d_in, d_out, spans, dtype, out):
     g = gen(rows + rank + d_in)
     ad = make(g, n, rank, d_in, d_out, dtype)
@@ -86,7 +87,7 @@ def test_adapters(rows, n, rank, d_in, d_out, spans, dtype, out):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("rows", [1, 40, 100])
+@pytest.mark.parametrize("rows", [1, 40, 100, 300])
 @pytest.mark.parametrize("rank,ranks", [(16, [16, 1, 0, 9]), (64, [64, 8, 33, 32, -3, 17, 100]), (24, [24, 5, 12]), (200, [200, 31, 129, 64])])
 def test_mixed_ranks(rank, ranks, rows, dtype):
     g = gen(rank + rows)
@@ -98,7 +99,7 @@ def test_mixed_ranks(rank, ranks, rows, dtype):
     check(ad, x, index, base, out)
 
 
-@pytest.mark.parametrize("rows", [3, 90])
+@pytest.mark.parametrize("rows", [3, 90, 400])
 def test_strides_no_scales_and_foreign_indexes(rows):
     """Rows of a wider tensor, unaligned; what lies between them stays; indexes outside the stack mean none."""
     g = gen(rows)
@@ -128,7 +129,7 @@ def test_more_rows_than_are_sorted_at_once(n, spans):
 def test_no_row_has_an_adapter():
     g = gen(3)
     ad = make(g, 2, 8, 64, 70, F16)
-    for rows in (1, 20, 100):
+    for rows in (1, 20, 100, 300):
         x, base = normal(g, rows, 64, dtype=F16), normal(g, rows, 70, dtype=F16)
         out = torch.zeros_like(base)
         ad.add(x, torch.full((rows,), -1, dtype=torch.int32, device="cuda"), base, out)
@@ -136,7 +137,7 @@ def test_no_row_has_an_adapter():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("rows", [20, 80])
+@pytest.mark.parametrize("rows", [20, 80, 400])
 def test_rows_do_not_touch_each_other(rows, dtype):
     """NaN and infinity in one row's x, in another adapter's weights, in rows without an adapter: only theirs."""
     g = gen(rows)
@@ -172,7 +173,7 @@ def test_large_and_small_values_fp16():
 
 def test_a_row_does_not_depend_on_the_others():
     g = gen(13)
-    for rows in (30, 150):
+    for rows in (30, 150, 600):
         ad = make(g, 6, 32, 300, 200, BF16)
         x, base = normal(g, rows, 300, dtype=BF16), normal(g, rows, 200, dtype=BF16)
         index = torch.randint(-1, 6, (rows,), generator=g, device="cuda").to(torch.int32)
@@ -186,7 +187,7 @@ def test_a_row_does_not_depend_on_the_others():
 def test_a_wide_layer_and_a_given_workspace():
     g = gen(17)
     ad = make(g, 4, 16, 4096, 11008, BF16)
-    for rows in (2, 70):
+    for rows in (2, 70, 330):
         x, base = normal(g, rows, 4096, dtype=BF16), normal(g, rows, 11008, dtype=BF16)
         index = torch.randint(0, 4, (rows,), generator=g, device="cuda").to(torch.int32)
         ws = torch.full((A.adapters_workspace_bytes(ad, rows) + 64,), 255, dtype=torch.uint8, device="cuda")
