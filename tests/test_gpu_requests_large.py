@@ -70,10 +70,10 @@ def test_adapters(space):
     ad.add(fx, index, fb, fo)
     assert torch.equal(fo, want)
     # many rows, of which three are these: the sorted way
-    rows, at = 256, torch.tensor([0, 150, 255], device="cuda")
-    wide = space.as_strided((rows, 512), (2 ** 24, 1))
+    rows, at = 300, torch.tensor([0, 150, 299], device="cuda")
+    wide = space.as_strided((rows, 512), (2 ** 23, 1))
     wide.copy_(normal(g, rows, 512, dtype=BF16))
-    assert 255 * 2 ** 24 > 2 ** 31
+    assert 299 * 2 ** 23 > 2 ** 31
     idx, b = torch.randint(-1, 2, (rows,), generator=g, device="cuda").to(torch.int32), normal(g, rows, 256, dtype=BF16)
     got, want = torch.empty_like(b), torch.empty_like(b)
     ad.add(wide, idx, b, got)
@@ -88,7 +88,7 @@ def test_a_large_stack(space):
     a = space[:n * rank * d].view(n, rank, d)
     assert 2 * rank * d * 2 > 2 ** 31
     small = normal(g, 256, 64, dtype=BF16)
-    for rows in (2, 200):
+    for rows in (2, 200, 300):
         index = torch.full((rows,), 2, dtype=torch.int32, device="cuda")
         a[2].zero_()
         a[2, :, -64:] = small

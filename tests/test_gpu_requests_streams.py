@@ -75,7 +75,7 @@ def expected(seed, n):
     return s.results()
 
 
-SIZES = [3, 250]
+SIZES = [3, 250, 300]
 
 
 @pytest.mark.parametrize("n", SIZES)
