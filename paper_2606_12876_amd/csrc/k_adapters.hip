@@ -175,11 +175,31 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
     }
     multiply(now);
   }
-  for (int k = whole; k < k1; k += 32) {                           // fewer than U steps, the last of fewer inputs
-    const u32x4_t xv = load8(x - kg, k + kg, d_in);
+  if (d_in < 8) {                                                  // one step, by single values
+    if (whole < k1) {
+      const u32x4_t xv = load8(x - kg, kg, d_in);
 #pragma unroll
-    for (int m = 0; m < RT; ++m)
-      if (16 * m < rank) acc[m] = mma<DT>(load8(w[m] - kg, k + kg, d_in), xv, acc[m]);
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank) acc[m] = mma<DT>(load8(w[m] - kg, kg, d_in), xv, acc[m]);
+    }
+  } else if (whole < k1) {                                         // fewer than U steps, the last of fewer inputs, loaded at once
+    Batch b;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = whole + 32 * u;
+      if (k >= k1) break;
+      b.x[u] = load8_moved(x - kg, k + kg, d_in);
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank) b.w[u][m] = load8_moved(w[m] - kg, k + kg, d_in);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (whole + 32 * u >= k1) break;
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+        if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m], b.x[u], acc[m]);
+    }
   }
 
   // The waves' sums added up, 16 values of t at a time.
@@ -314,68 +334,84 @@ __device__ __forceinline__ u32x4_t own_values(int left) {
                  left >= 6 ? 0xFFFFFFFFu : left == 5 ? 0xFFFFu : 0, left >= 8 ? 0xFFFFFFFFu : left == 7 ? 0xFFFFu : 0};
 }
 
-// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, by one wave, into to[step][part][lane]; the
-// factor of the rows' results (fp16) into back.
-template <int DT>
-__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, OperandsLds<DT>* to, float* back) {
+// s_n t of 16 rows (`row` for slot lane % 16) as the second product's operands, into to[step][part][lane]; the factor of the
+// rows' results (fp16) into back. By one wave, or by kWaves of a workgroup (all of them), a step each in turn.
+template <int DT, int kWaves>
+__device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank, float scale, OperandsLds<DT>* to, float* back,
+                                         uint32_t (*bigs)[16]) {
   typedef Parts<DT> P;
-  const int lane = threadIdx.x % 64, q = lane / 16, steps = (rank + 31) / 32;
+  const int lane = threadIdx.x % 64, q = lane / 16, steps = (rank + 31) / 32, wave = kWaves > 1 ? threadIdx.x / 64 : 0;
   const float* tp = a.t + (int64_t)row * a.t_stride + 8 * q;
-  // Partial sums added up, scaled, 0 from the adapter's rank on.
-  const auto values = [&](int kt, float* v) {
-    f32x4_t lo[kMaxSplits] = {}, hi[kMaxSplits] = {};
-    if (32 * kt + 8 * q < a.t_stride) {                // not by rank, which may still be on its way
+  struct Sums { f32x4_t lo[kMaxSplits], hi[kMaxSplits]; };
+  const auto load = [&](int kt, Sums& s) {
 #pragma unroll
-      for (int p = 0; p < kMaxSplits; ++p)
-        if (p < a.splits) {
-          const f32x4_t* from = (const f32x4_t*)(tp + p * (int64_t)a.n_rows * a.t_stride + 32 * kt);
-          lo[p] = from[0], hi[p] = from[1];
-        }
+    for (int p = 0; p < kMaxSplits; ++p) {
+      s.lo[p] = s.hi[p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (p < a.splits && 32 * kt + 8 * q < a.t_stride) {    // not by rank, which may still be on its way
+        const f32x4_t* from = (const f32x4_t*)(tp + p * (int64_t)a.n_rows * a.t_stride + 32 * kt);
+        s.lo[p] = from[0], s.hi[p] = from[1];
+      }
     }
-#pragma unroll
-    for (int p = 1; p < kMaxSplits; ++p) lo[0] += lo[p], hi[0] += hi[p];
-    const f32x4_t l = lo[0], h = hi[0];
-    const float f[8] = {l.x, l.y, l.z, l.w, h.x, h.y, h.z, h.w};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 32 * kt + 8 * q + j < rank ? f[j] * scale : 0.f;
   };
-  float v[8], fwd = 1.f;
-  values(0, v);
-  if constexpr (DT == AQMB_F16) {
-    // By a power of two, so that the row's largest magnitude is in [2^13, 2^14): in fp16's range, the parts far
-    // from its subnormals.
-    uint32_t big = 0;
-    const auto largest = [&](const float* f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) big = max(big, __builtin_bit_cast(uint32_t, f[j]) & 0x7FFFFFFFu);
-    };
-    largest(v);
-    for (int kt = 1; kt < steps; ++kt) {
-      float f[8];
-      values(kt, f);
-      largest(f);
-    }
-    big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 16), (int)big));
-    big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 32), (int)big));
-    const int ex = min(max((int)(big >> 23), 14), 254);    // the exponent that goes to 13
-    fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
-    if (lane < 16) back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
-  }
-  for (int kt = 0;;) {
+  const auto put = [&](int kt, float* v) {
 #pragma unroll
     for (int p = 0; p < P::kN; ++p) {
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (p == 0 && DT == AQMB_F16) v[2 * j] *= fwd, v[2 * j + 1] *= fwd;
         w[j] = P::pack(v[2 * j], v[2 * j + 1]);
         v[2 * j] -= P::lo(w[j]);
         v[2 * j + 1] -= P::hi(w[j]);
       }
       to[kt][p][lane] = u32x4_t{w[0], w[1], w[2], w[3]};
     }
-    if (++kt >= steps) return;
-    values(kt, v);
+  };
+  uint32_t big = 0;
+  // Partial sums added up, scaled, 0 from the adapter's rank on. fp16's are kept where their parts will be.
+  const auto take = [&](int kt, Sums& s) {
+#pragma unroll
+    for (int p = 1; p < kMaxSplits; ++p) s.lo[0] += s.lo[p], s.hi[0] += s.hi[p];
+    const f32x4_t l = s.lo[0], h = s.hi[0];
+    float v[8] = {l.x, l.y, l.z, l.w, h.x, h.y, h.z, h.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 32 * kt + 8 * q + j < rank ? v[j] * scale : 0.f;
+    if constexpr (DT == AQMB_F16) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) big = max(big, __builtin_bit_cast(uint32_t, v[j]) & 0x7FFFFFFFu);
+      to[kt][0][lane] = __builtin_bit_cast(u32x4_t, f32x4_t{v[0], v[1], v[2], v[3]});
+      to[kt][1][lane] = __builtin_bit_cast(u32x4_t, f32x4_t{v[4], v[5], v[6], v[7]});
+    } else {
+      put(kt, v);
+    }
+  };
+  Sums s[2];                                                 // two steps are on their way at once
+  load(wave, s[0]);
+  for (int kt = wave; kt < steps; kt += 2 * kWaves) {
+    const bool two = kt + kWaves < steps;
+    if (kt != wave) load(kt, s[0]);
+    if (two) load(kt + kWaves, s[1]);
+    take(kt, s[0]);
+    if (two) take(kt + kWaves, s[1]);
+  }
+  if constexpr (DT == AQMB_F16) {
+    // By a power of two, so that the row's largest magnitude is in [2^13, 2^14): in fp16's range, the parts far
+    // from its subnormals.
+    big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 16), (int)big));
+    big = max(big, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane ^ 32), (int)big));
+    if constexpr (kWaves > 1) {
+      if (lane < 16) bigs[wave][lane] = big;
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < kWaves; ++n) big = max(big, bigs[n][lane % 16]);
+    }
+    const int ex = min(max((int)(big >> 23), 14), 254);      // the exponent that goes to 13
+    const float fwd = __builtin_bit_cast(float, (uint32_t)(267 - ex) << 23);
+    if (wave == 0 && lane < 16) back[lane] = __builtin_bit_cast(float, (uint32_t)(ex - 13) << 23);
+    for (int kt = wave; kt < steps; kt += kWaves) {
+      const f32x4_t l = __builtin_bit_cast(f32x4_t, to[kt][0][lane]) * fwd, h = __builtin_bit_cast(f32x4_t, to[kt][1][lane]) * fwd;
+      float v[8] = {l.x, l.y, l.z, l.w, h.x, h.y, h.z, h.w};
+      put(kt, v);
+    }
   }
 }
 
@@ -476,6 +512,7 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
   extern __shared__ __align__(16) char all[];            // the waves' weights, t's operands
   __shared__ float back[16];
+  __shared__ uint32_t bigs[4][16];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane % 16, q = lane / 16, d_out = a.ad.d_out, stack = a.ad.rank;
   WeightsLds& weights = ((WeightsLds*)all)[wave];
   OperandsLds<DT>* const operand = (OperandsLds<DT>*)(all + 4 * sizeof(WeightsLds));
@@ -530,7 +567,7 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
     return;
   }
   const u32x4_t mask = own_values(rank - (rank - 1) / 32 * 32 - 8 * q);      // of the last step
-  if (wave == 0) operands<DT>(a, t.row, rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, operand, back);
+  operands<DT, 4>(a, t.row, rank, a.ad.scales ? a.ad.scales[t.adapter] : 1.f, operand, back, bigs);
   __syncthreads();
   if (o >= d_out) return;
 
@@ -630,7 +667,8 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(Ad
   load_rows(y, o0);
   OperandsLds<DT>* const t = (OperandsLds<DT>*)(all + 2 * sizeof(WeightsLds)) + wave * ((stack + 31) / 32);
   __shared__ float backs[4][16];
-  if (count) operands<DT>(a, a.order[tile.y + (c < count ? first + c : 0)], rank, a.ad.scales ? a.ad.scales[tile.x] : 1.f, t, backs[wave]);
+  if (count)
+    operands<DT, 1>(a, a.order[tile.y + (c < count ? first + c : 0)], rank, a.ad.scales ? a.ad.scales[tile.x] : 1.f, t, backs[wave], nullptr);
 
   int n = 0;
   for (int o = o0; o < o1; o += 128) {
