@@ -51,9 +51,10 @@ __device__ __forceinline__ u32x4_t load8(const uint16_t* row, int k, int n) {
   return u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
-// The same without a branch, n >= 8: a row's last 8 values, moved down by those before k.
-__device__ __forceinline__ u32x4_t load8_moved(const uint16_t* row, int k, int n) {
-  const u32x4_t v = load8(row, min(k, n - 8));
+// The same in two steps without a branch, n >= 8: a row's last 8 values, and these moved down by those before k. Many loads
+// first, then the moves: each in one piece would wait for its own.
+__device__ __forceinline__ u32x4_t load8_last(const uint16_t* row, int k, int n) { return load8(row, min(k, n - 8)); }
+__device__ __forceinline__ u32x4_t moved8(u32x4_t v, int k, int n) {
   const int past = max(k - (n - 8), 0);
   uint32_t a = v.x, b = v.y, c = v.z, d = v.w;
   const bool four = past & 4, two = past & 2;
@@ -188,17 +189,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
     for (int u = 0; u < U; ++u) {
       const int k = whole + 32 * u;
       if (k >= k1) break;
-      b.x[u] = load8_moved(x - kg, k + kg, d_in);
+      b.x[u] = load8_last(x - kg, k + kg, d_in);
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) b.w[u][m] = load8_moved(w[m] - kg, k + kg, d_in);
+        if (16 * m < rank) b.w[u][m] = load8_last(w[m] - kg, k + kg, d_in);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (whole + 32 * u >= k1) break;
+      const int k = whole + 32 * u;
+      if (k >= k1) break;
+      const u32x4_t xv = moved8(b.x[u], k + kg, d_in);
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m], b.x[u], acc[m]);
+        if (16 * m < rank) acc[m] = mma<DT>(moved8(b.w[u][m], k + kg, d_in), xv, acc[m]);
     }
   }
 
@@ -539,7 +542,7 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
       if (j >= 2 << shift) break;
       const uint32_t r = min(o + ((64 * j + l) >> shift), d_out - 1) * (uint32_t)stack;     // below 2^31
       if constexpr (kEights) w[j] = load8(b, r + min(k, stack - 8));
-      else w[j] = stack >= 8 ? load8_moved(b + r, k, stack) : load8(b + r, k, stack);
+      else w[j] = stack >= 8 ? load8_last(b + r, k, stack) : load8(b + r, k, stack);
     }
   };
   const auto place_w = [&](const u32x4_t* w, int kt) {
@@ -548,7 +551,7 @@ __global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
     for (int j = 0; j < 8; ++j) {
       if (j >= 2 << shift) break;
       const int o = (64 * j + l) >> shift, piece = l & ((1 << shift) - 1);
-      weights[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = w[j];
+      weights[o % 8][o / 8 * 4 + (piece ^ (o / 32))] = kEights || stack < 8 ? w[j] : moved8(w[j], 32 * kt + 8 * piece, stack);
     }
   };
   // Two steps' weights and the rows of base are on their way while t and the adapter's rank come.
@@ -651,7 +654,7 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(Ad
       if (at >= 128) continue;
       const uint32_t r = min(o + at, d_out - 1) * (uint32_t)stack;           // below 2^31
       if constexpr (kEights) w[j] = load8(b, r + min(k, stack - 8));
-      else w[j] = stack >= 8 ? load8_moved(b + r, k, stack) : load8(b + r, k, stack);
+      else w[j] = stack >= 8 ? load8_last(b + r, k, stack) : load8(b + r, k, stack);
     }
   };
   const auto place_w = [&](const u32x4_t* w, WeightsLds& to, int kt) {
@@ -659,7 +662,8 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(Ad
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int at = (256 * j + (int)threadIdx.x) >> shift;
-      if (at < 128) to[at % 8][at / 8 * 4 + (piece ^ (at / 32))] = w[j];
+      if (at < 128)
+        to[at % 8][at / 8 * 4 + (piece ^ (at / 32))] = kEights || stack < 8 ? w[j] : moved8(w[j], 32 * kt + 8 * piece, stack);
     }
   };
   u32x4_t w[2];
