@@ -67,6 +67,28 @@ __device__ __forceinline__ u32x4_t moved8(u32x4_t v, int k, int n) {
   return u32x4_t{none ? 0 : a, none ? 0 : b, none ? 0 : c, none ? 0 : d};
 }
 
+// Eight values from p on, loaded and then put together. A 16-byte load that does not start at a multiple of 4 bytes takes
+// several times as long, so where such addresses come (kOdd) it starts 2 bytes lower, inside the same aligned 4 bytes as *p,
+// and the last value has a load of its own.
+template <bool kOdd> struct Loaded8 {
+  u32x4_t v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = load8(p, 0u); }
+  __device__ __forceinline__ u32x4_t value(const uint16_t*) const { return v; }
+};
+template <> struct Loaded8<true> {
+  u32x4_t v;
+  uint32_t last;
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    v = load8((const uint16_t*)((uintptr_t)p & ~(uintptr_t)2), 0u);
+    last = p[7];
+  }
+  __device__ __forceinline__ u32x4_t value(const uint16_t* p) const {
+    const uint32_t s = ((uintptr_t)p & 2) * 8;
+    return u32x4_t{__builtin_amdgcn_alignbit(v.y, v.x, s), __builtin_amdgcn_alignbit(v.z, v.y, s),
+                   __builtin_amdgcn_alignbit(v.w, v.z, s), __builtin_amdgcn_alignbit(last, v.w, s)};
+  }
+};
+
 template <int DT>
 __device__ __forceinline__ f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
   if constexpr (DT == AQMB_F16)
@@ -123,7 +145,7 @@ __device__ __forceinline__ int own_rank(const AdapterArgs& a, int adapter) {
 }
 
 // Few rows: blockIdx.x is the row that a tile starts with, blockIdx.y a part of the inputs, which the waves share out.
-template <int DT, int RT>
+template <int DT, int RT, bool kOdd>
 __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
   constexpr int U = RT <= 2 ? 4 : RT <= 4 ? 2 : 1;                 // steps of 32 inputs loaded at once
   __shared__ __align__(16) float lds[2][kFewWaves][256];
@@ -143,22 +165,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
   const int steps = (d_in + 31) / 32, parts = a.splits * kFewWaves, p = blockIdx.y * kFewWaves + wave;
   const int k0 = (int)((int64_t)steps * p / parts) * 32, k1 = min((int)((int64_t)steps * (p + 1) / parts) * 32, d_in);
   const int whole = k0 + (k1 - k0) / (32 * U) * (32 * U);
-  struct Batch { u32x4_t x[U], w[U][RT]; };
+  struct Batch { Loaded8<kOdd> x[U], w[U][RT]; };
   const auto load = [&](Batch& b, int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      b.x[u] = load8(x, k + 32 * u);
+      b.x[u].load(x + (uint32_t)(k + 32 * u));
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) b.w[u][m] = load8(w[m], k + 32 * u);
+        if (16 * m < rank) b.w[u][m].load(w[m] + (uint32_t)(k + 32 * u));
     }
   };
   const auto multiply = [&](const Batch& b) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const u32x4_t xv = b.x[u].value(x);                          // steps of 32: p's two low bits are those of the row
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m], b.x[u], acc[m]);
+        if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m].value(w[m]), xv, acc[m]);
+    }
   };
   if constexpr (RT > 4) {                                          // no registers left to load ahead
     for (int k = k0; k < whole; k += 32 * U) {
@@ -189,19 +213,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
     for (int u = 0; u < U; ++u) {
       const int k = whole + 32 * u;
       if (k >= k1) break;
-      b.x[u] = load8_last(x - kg, k + kg, d_in);
+      b.x[u].load(x - kg + min(k + kg, d_in - 8));
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) b.w[u][m] = load8_last(w[m] - kg, k + kg, d_in);
+        if (16 * m < rank) b.w[u][m].load(w[m] - kg + min(k + kg, d_in - 8));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = whole + 32 * u;
       if (k >= k1) break;
-      const u32x4_t xv = moved8(b.x[u], k + kg, d_in);
+      const u32x4_t xv = moved8(b.x[u].value(x - kg + min(k + kg, d_in - 8)), k + kg, d_in);
 #pragma unroll
       for (int m = 0; m < RT; ++m)
-        if (16 * m < rank) acc[m] = mma<DT>(moved8(b.w[u][m], k + kg, d_in), xv, acc[m]);
+        if (16 * m < rank) acc[m] = mma<DT>(moved8(b.w[u][m].value(w[m] - kg + min(k + kg, d_in - 8)), k + kg, d_in), xv, acc[m]);
     }
   }
 
@@ -796,7 +820,10 @@ __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
 
 template <int DT, int RT>
 hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  if (p.few) shrink_few<DT, RT><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
+  // Rows at addresses that are no multiples of 4 bytes. Above rank 128 no registers are left for it.
+  const bool odd = RT <= 8 && (((uintptr_t)a.x | (uintptr_t)a.ad.a) % 4 || a.x_stride % 2 || a.ad.d_in % 2);
+  if (p.few && odd) shrink_few<DT, RT, RT <= 8><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
+  else if (p.few) shrink_few<DT, RT, false><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
   else shrink_many<DT, RT><<<dim3(p.tiles, p.splits), 256, 0, st>>>(a);
   return hipGetLastError();
 }
