@@ -144,22 +144,25 @@ __device__ __forceinline__ int own_rank(const AdapterArgs& a, int adapter) {
   return adapter < 0 ? 0 : a.ad.ranks ? min(max(a.ad.ranks[adapter], 0), a.ad.rank) : a.ad.rank;
 }
 
-// Few rows: blockIdx.x is the row that a tile starts with, blockIdx.y a part of the inputs, which the waves share out.
-template <int DT, int RT, bool kOdd>
-__global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
-  constexpr int U = RT <= 2 ? 4 : RT <= 4 ? 2 : 1;                 // steps of 32 inputs loaded at once
+// Few rows: blockIdx.x is the row that a tile starts with, blockIdx.y a part of the inputs, which the waves share out,
+// blockIdx.z 64 values of t (with all of a rank above 64 in one workgroup no loads were ahead of the products: 3 adapters of
+// rank 128, 1552 x 2104, one row 21 us a call, now 12).
+// kOne: one workgroup a unit, by the registers that it may take.
+template <int DT, int RT, bool kOdd, bool kOne>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2, kOne ? 2 : 8))) void shrink_few(AdapterArgs a) {
+  constexpr int U = RT <= 2 ? 4 : 2;                 // steps of 32 inputs loaded at once
   __shared__ __align__(16) float lds[2][kFewWaves][256];
   __shared__ int slots[16];
   Tile t;
   if (!tile_at(a, blockIdx.x, t)) return;
-  const int rank = own_rank(a, t.adapter);
-  if (rank == 0) return;
+  const int m0 = 64 * blockIdx.z, rank = own_rank(a, t.adapter) - m0;
+  if (rank <= 0) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, kg = lane / 16 * 8, d_in = a.ad.d_in;
   const uint16_t* x = (const uint16_t*)a.x + t.row * a.x_stride + kg;
   const uint16_t* w[RT];
 #pragma unroll
   for (int m = 0; m < RT; ++m)
-    w[m] = (const uint16_t*)a.ad.a + ((int64_t)t.adapter * a.ad.rank + min(16 * m + i, rank - 1)) * d_in + kg;
+    w[m] = (const uint16_t*)a.ad.a + ((int64_t)t.adapter * a.ad.rank + m0 + min(16 * m + i, rank - 1)) * d_in + kg;
 
   f32x4_t acc[RT] = {};
   const int steps = (d_in + 31) / 32, parts = a.splits * kFewWaves, p = blockIdx.y * kFewWaves + wave;
@@ -184,13 +187,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
         if (16 * m < rank) acc[m] = mma<DT>(b.w[u][m].value(w[m]), xv, acc[m]);
     }
   };
-  if constexpr (RT > 4) {                                          // no registers left to load ahead
-    for (int k = k0; k < whole; k += 32 * U) {
-      Batch now;
-      load(now, k);
-      multiply(now);
-    }
-  } else if (whole > k0) {
+  if (whole > k0) {
     Batch now, next;
     load(now, k0);
     for (int k = k0 + 32 * U; k < whole; k += 32 * U) {
@@ -230,7 +227,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void shrink_few(AdapterArgs a) {
   }
 
   // The waves' sums added up, 16 values of t at a time.
-  float* out = a.t + (int64_t)blockIdx.y * a.n_rows * a.t_stride;
+  float* out = a.t + (int64_t)blockIdx.y * a.n_rows * a.t_stride + m0;
   if (threadIdx.x < 16) slots[threadIdx.x] = t.row;
 #pragma unroll
   for (int m = 0; m < RT; ++m) {
@@ -820,11 +817,21 @@ __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
 
 template <int DT, int RT>
 hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st) {
-  // Rows at addresses that are no multiples of 4 bytes. Above rank 128 no registers are left for it.
-  const bool odd = RT <= 8 && (((uintptr_t)a.x | (uintptr_t)a.ad.a) % 4 || a.x_stride % 2 || a.ad.d_in % 2);
-  if (p.few && odd) shrink_few<DT, RT, RT <= 8><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
-  else if (p.few) shrink_few<DT, RT, false><<<dim3(a.n_rows, p.splits), 64 * kFewWaves, 0, st>>>(a);
-  else shrink_many<DT, RT><<<dim3(p.tiles, p.splits), 256, 0, st>>>(a);
+  if (p.few) {
+    constexpr int kMost = RT <= 4 ? RT : 4;
+    const dim3 grid(a.n_rows, p.splits, (a.ad.rank + 63) / 64);
+    // Rows at addresses that are no multiples of 4 bytes.
+    const bool odd = ((uintptr_t)a.x | (uintptr_t)a.ad.a) % 4 || a.x_stride % 2 || a.ad.d_in % 2;
+    // Most workgroups have no tile and end at once; where few have one, two of them would share a unit while others are idle
+    // (150 rows, 4 adapters of rank 64, 4096 x 4096: 19.5 us a call, one a unit 16.8; 64 adapters: 34.5 and 39.3).
+    const int groups = (a.n_rows + kRows - 1) / kRows * min(a.ad.n_adapters, kRows);
+    const bool one = max(a.n_rows / 16, min(groups, a.n_rows)) * (int)(grid.y * grid.z) <= 100;
+    const auto kernel = odd ? one ? shrink_few<DT, kMost, true, true> : shrink_few<DT, kMost, true, false>
+                            : one ? shrink_few<DT, kMost, false, true> : shrink_few<DT, kMost, false, false>;
+    kernel<<<grid, 64 * kFewWaves, 0, st>>>(a);
+  } else {
+    shrink_many<DT, RT><<<dim3(p.tiles, p.splits), 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 template <int DT, bool kWide, bool kEights>
@@ -867,9 +874,9 @@ hipError_t both(const AdapterArgs& a, const AdapterPlan& p, aqmb_dtype y, hipStr
 // Few rows take a look at 64 rows for every tile of 16; above 256 a sort of its own (4 us for 100 rows, 10 for 8192) and
 // tiles of 64 rows are cheaper. Rank 16, 4096 x 4096, 4 adapters in spans: 128 rows 11.8 us against 17.4, 256 16.1 and 18.2,
 // 384 22.7 and 18.4; 64 adapters in any order: 12.1 and 20.5, 20.3 and 22.4, 27.3 and 23.8; rank 64, 11008 outputs, 8
-// adapters: 25.7 and 26.7, 32.2 and 31.5, 46 and 33.7. Parts of the inputs: four steps for each wave at least, few rows;
-// about 512 workgroups, many. Many: 256 outputs a workgroup (8192 rows: 128 take 76 us against 67, 512 70), 128 where that
-// leaves fewer than 512 (1024 rows 20.9 us against 23.0, 300 18.4 against 21.0).
+// adapters: 25.7 and 26.7, 32.2 and 31.5, 46 and 33.7. Parts of the inputs: as many steps for each wave as it loads at
+// once, at least, few rows; about 512 workgroups, many. Many: 256 outputs a workgroup (8192 rows: 128 take 76 us against 67,
+// 512 70), 128 where that leaves fewer than 512 (1024 rows 20.9 us against 23.0, 300 18.4 against 21.0).
 constexpr int kFewRows = 256;
 AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   AdapterPlan p;
@@ -879,7 +886,7 @@ AdapterPlan adapter_plan(const aqmb_adapters& ad, int n_rows) {
   p.tiles = groups + (n_rows - groups) / 64;
   p.per_group = 0;
   if (p.few) {
-    p.splits = steps / (kFewWaves * 4);
+    p.splits = steps / (kFewWaves * (ad.rank <= 32 ? 4 : 2));
   } else {
     p.splits = 512 / ((n_rows + kRows - 1) / kRows);
     if (p.splits > steps / 16) p.splits = steps / 16;
