@@ -408,14 +408,16 @@ __device__ __forceinline__ void operands(const AdapterArgs& a, int row, int rank
       put(kt, v);
     }
   };
-  Sums s[2];                                                 // two steps are on their way at once
+  constexpr int kAhead = kWaves > 1 ? 1 : 2;                 // steps on their way at once
+  Sums s[kAhead];
   load(wave, s[0]);
-  for (int kt = wave; kt < steps; kt += 2 * kWaves) {
-    const bool two = kt + kWaves < steps;
-    if (kt != wave) load(kt, s[0]);
-    if (two) load(kt + kWaves, s[1]);
-    take(kt, s[0]);
-    if (two) take(kt + kWaves, s[1]);
+  for (int kt = wave; kt < steps; kt += kAhead * kWaves) {
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if ((n || kt != wave) && kt + n * kWaves < steps) load(kt + n * kWaves, s[n]);
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if (kt + n * kWaves < steps) take(kt + n * kWaves, s[n]);
   }
   if constexpr (DT == AQMB_F16) {
     // By a power of two, so that the row's largest magnitude is in [2^13, 2^14): in fp16's range, the parts far
@@ -532,7 +534,7 @@ __device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], in
 // vector cache, which bound the kernel: 8192 rows of 4096 outputs 45 us). Bound by latency (4.9 us) or the adapters' bytes
 // (32 rows of some 25 adapters of rank 64, 11008 outputs: 13 us).
 template <int DT, bool kWide, bool kEights>
-__global__ __launch_bounds__(256) void expand_few(AdapterArgs a) {
+__global__ __launch_bounds__(256, kWide || !kEights ? 2 : 3) void expand_few(AdapterArgs a) {
   constexpr int kParts = Parts<DT>::kN, kSize = kWide ? 4 : 2;
   extern __shared__ __align__(16) char all[];            // the waves' weights, t's operands
   __shared__ float back[16];
