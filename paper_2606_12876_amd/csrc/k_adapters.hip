@@ -625,8 +625,8 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 2 : 3) void expand_few(Ada
 
 // Many: a tile of 64 rows, four waves with 16 each, and a.per_group outputs. As expand_few, but the waves bring the weights
 // into LDS together, into one of two places while the other is read (each its own: 8192 rows of 4096 outputs at rank 32
-// 41 us, now 34; a call at rank 128 165 us, now 134), and the next outputs of base are loaded a step ahead. As many waves
-// as registers allow without spills (two for each of four units, not four: 38 us).
+// 41 us, now 34; a call at rank 128 165 us, now 134), and the next outputs of base are loaded a step ahead. Four
+// waves a SIMD where the registers suffice (two: 38 us; five spill).
 template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(AdapterArgs a) {
   typedef Parts<DT> P;
