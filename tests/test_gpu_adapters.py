@@ -115,6 +115,20 @@ def test_strides_no_scales_and_foreign_indexes(rows):
     assert torch.equal(wide[:, :5], kept[:, :5]) and torch.equal(wide[:, 104:], kept[:, 104:])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,n,d_in", [(1, 1, 9), (2, 3, 1001), (130, 64, 333), (250, 40, 1431)])
+@pytest.mark.parametrize("rank", [8, 24, 56, 150])
+def test_rows_at_odd_elements(rank, rows, n, d_in, dtype):
+    """x begins at an odd element of its memory, and so does every other row of A."""
+    g = gen(rows + rank)
+    ad = make(g, n, rank, d_in, 40, dtype)
+    x = normal(g, 1 + rows * d_in, dtype=dtype)[1:].view(rows, d_in)
+    index, base = index_of(g, rows, n, False), normal(g, rows, 40, dtype=dtype)
+    out = torch.empty_like(base)
+    ad.add(x, index, base, out)
+    check(ad, x, index, base, out)
+
+
 @pytest.mark.parametrize("n", [1, 3, 8192])
 @pytest.mark.parametrize("spans", [False, True])
 def test_more_rows_than_are_sorted_at_once(n, spans):
