@@ -157,7 +157,14 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a) {
           }
         }
       }
-      const Raw8 y0 = turned ? narrow8<DT>(f0) : x0[b], y1 = turned ? narrow8<DT>(f1) : x1[b];
+      Raw8 y0 = turned ? narrow8<DT>(f0) : x0[b], y1 = turned ? narrow8<DT>(f1) : x1[b];
+      if constexpr (kPairs != kHalves8) {                // values behind the pairs, in words of two: their own bits, also a NaN's
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y0.w[j] = e0 + 2 * j < rot ? y0.w[j] : x0[b].w[j];
+          y1.w[j] = e1 + 2 * j < rot ? y1.w[j] : x1[b].w[j];
+        }
+      }
       const int64_t token = token0 + u.token;
       if (kCache == 0 || k < 0) {
         uint16_t* out = k < 0 ? (uint16_t*)a.r.q_out + token * a.r.q_out_stride + (int64_t)u.head * dim
