@@ -151,7 +151,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a) {
             float& x = kPairs == kHalves8 ? f0[j] : j < 4 ? f0[2 * (j % 4)] : f1[2 * (j % 4)];
             float& y = kPairs == kHalves8 ? f1[j] : j < 4 ? f0[2 * (j % 4) + 1] : f1[2 * (j % 4) + 1];
             const float tx = fmaf(x, t.x, -y * t.y), ty = fmaf(y, t.x, x * t.y);
-            const bool in = kPairs == kHalves8 || pair < half;
+            // Behind the pairs: 16 bits take the words that were loaded, below.
+            const bool in = kPairs == kHalves8 || kCache != 2 || pair < half;
             x = in ? tx : x;
             y = in ? ty : y;
           }
