@@ -638,9 +638,9 @@ aqmb_status aqmb_rotary_frequencies(int rotary_dim, double base, const aqmb_rota
                                     double* frequencies, float* amplitude);
 
 /*
- * Turns the queries and keys of n_tokens tokens. Angles are binary64 products of the position and the frequency,
- * reduced by whole turns before they are rounded; sines, cosines and the turn are binary32 (sine and cosine to
- * 2^-22), one rounding to `dtype`.
+ * Turns the queries and keys of n_tokens tokens. An angle is the binary64 product of the position (as a binary64
+ * number) and the frequency, reduced by whole turns before it is rounded further: sine and cosine are within 2^-22 of that
+ * angle's, up to 2^75 radians. They and the turn are binary32, with one rounding to `dtype`.
  *   q, q_out   [n_tokens][n_heads][head_dim] F16 or BF16 (`dtype`), stride between tokens q_stride / q_out_stride
  *   k, k_out   the same with n_kv_heads; both NULL (n_kv_heads 0): no keys
  *   positions  int64 [n_tokens], device memory, of any size and sign

@@ -45,6 +45,16 @@ __device__ __forceinline__ Raw8 narrow8(const float* f) {
   return r;
 }
 
+// An angle in turns, less whole ones. 1 / (2 pi) in two parts, and what the first one's product rounds off: an angle of one
+// part only would be off by 2^-53 of itself, more than sine and cosine are from 2^30 on.
+__device__ __forceinline__ double turns_of(double angle) {
+#pragma clang fp contract(off)               // t is the rounded product everywhere
+  constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;
+  const double t = angle * kHi, rest = fma(angle, kLo, fma(angle, kHi, -t));
+  const double f = (t - rint(t)) + rest;       // rest is above a half where t's steps are whole turns
+  return f - rint(f);
+}
+
 // (cos, sin) of an angle in turns, within half a turn: reduced to an eighth of a turn around the nearest quarter, then
 // the Taylor polynomials, whose first left out terms are below 2^-28 there.
 __device__ __forceinline__ float2 cos_sin(double turns) {
@@ -109,8 +119,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a) {
     if (first == (int)(threadIdx.x / L)) {               // the first time: the whole workgroup
       for (int i = threadIdx.x; i < n_tokens * half; i += 256) {
         const int t = i / half, pair = i - t * half;
-        const double f = (double)a.r.positions[token0 + t] * (a.r.rot.frequencies[pair] * 0.15915494309189535);
-        float2 cs = cos_sin(f - rint(f));
+        float2 cs = cos_sin(turns_of((double)a.r.positions[token0 + t] * a.r.rot.frequencies[pair]));
         if (a.r.rot.inverse) cs.y = -cs.y;
         table[i] = make_float2(cs.x * a.r.rot.amplitude, cs.y * a.r.rot.amplitude);
       }
