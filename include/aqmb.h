@@ -727,8 +727,8 @@ aqmb_status aqmb_adapters_workspace_bytes(const aqmb_adapters* adapters, int n_r
  * or +infinity: everything NaN, top_ids -1. Sums are binary32, relative to the largest value. A row's results do not depend on the others' contents.
  * workspace: aqmb_log_probs_workspace_bytes bytes of device memory, 16-byte aligned, written by the call (calls that
  * share one must be ordered); 0 bytes: NULL is fine.
- * Errors: EINVAL (null or misaligned pointer, sizes < 1, n_targets < 0, n_top < 0 or > vocab, stride below vocab, scale not finite
- * or below 2^-120, outputs without inputs, no output at all, workspace too small), EUNSUPPORTED (dtype, n_top > AQMB_MAX_TOP, rows above 2^22), EHIP.
+ * Errors: EINVAL (null or misaligned pointer, sizes < 1, n_targets < 0, n_top < 0 or > vocab, stride below vocab, scale NaN, below
+ * 2^-120 or above 2.35e38 (the largest binary32 number times log 2), outputs without inputs, no output at all, workspace too small), EUNSUPPORTED (dtype, n_top > AQMB_MAX_TOP, rows above 2^22), EHIP.
  */
 #define AQMB_MAX_TOP 64
 aqmb_status aqmb_log_probs(const void* logits, aqmb_dtype dtype, int64_t stride, int rows, int vocab, float scale,

@@ -587,8 +587,10 @@ aqmb_status aqmb_log_probs(const void* logits, aqmb_dtype dtype, int64_t stride,
   if (s != AQMB_OK) return s;
   if (!logits) return fail(AQMB_EINVAL, "%s: logits is NULL", where);
   if (stride < vocab) return fail(AQMB_EINVAL, "%s: stride is below vocab = %d", where, vocab);
-  // Below, what overflows a difference of two logits would still have a weight.
-  if (!std::isfinite(scale) || scale < 0x1p-120f) return fail(AQMB_EINVAL, "%s: scale must be finite and >= 2^-120", where);
+  // Below, what overflows a difference of two logits would still have a weight; above, the kernels' factor, scale / log 2,
+  // is infinite, and its product with the largest value's difference of 0 no number.
+  if (!(scale >= 0x1p-120f) || !std::isfinite(scale * 1.4426950408889634f))
+    return fail(AQMB_EINVAL, "%s: scale must be within 2^-120 and 2.35e38", where);
   if (n_targets < 0) return fail(AQMB_EINVAL, "%s: n_targets = %d is negative", where, n_targets);
   if (!targets != (n_targets == 0) || !targets != !logprobs)
     return fail(AQMB_EINVAL, "%s: targets, logprobs and n_targets go together", where);

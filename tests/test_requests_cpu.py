@@ -167,3 +167,9 @@ def test_the_oracle_itself():
     a, b = rng.standard_normal((2, 3, 4)), rng.standard_normal((2, 5, 3))
     y = decode.adapted(rng.standard_normal((3, 4)), [1, -1, 2], a, b, np.ones(2), [3, 3])
     assert np.any(y[0]) and not np.any(y[1:])
+
+
+@pytest.mark.parametrize("scale", [2.36e38, 2.4e38, 3.4028234663852886e38, -3e38])
+def test_log_probs_refuse_scales_without_a_finite_factor(scale):
+    assert A.lib.aqmb_log_probs(16, BF16, 100, 2, 100, scale, None, 0, None, 16, None, None, None, 0, None, 0, None) == S.EINVAL
+    assert "scale" in A.last_error()
