@@ -846,7 +846,9 @@ hipError_t go_expand(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st)
     const size_t lds = 2 * sizeof(WeightsLds) + 4 * operands;
     const auto kernel = expand_many<DT, kWide, kEights>;
     if (lds + 256 > 65536) {           // with the kernel's own
-      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      // The limit is the kernel's, not the call's: what the largest rank takes, so that no thread lowers another's.
+      constexpr int kMost = 2 * sizeof(WeightsLds) + 4 * ((AQMB_MAX_RANK + 31) / 32) * sizeof(OperandsLds<DT>);
+      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
       if (e != hipSuccess) return e;
     }
     kernel<<<p.tiles * parts, 256, lds, st>>>(a);      // below 2^24: check_adapters
