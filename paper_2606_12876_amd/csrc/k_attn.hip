@@ -36,6 +36,9 @@ constexpr int kTile = 32, kChunkMax = 4096, kXcds = 8;
 constexpr int kWavesSplit = 4, kWavesWhole = 8;   // per workgroup, where sequences are split and where not
 // The kernel's own LDS beside its dynamic part, at most: statistics, offsets and scales of 8 waves, joined statistics.
 constexpr size_t kStaticLds = kWavesWhole * (2 * 16 * 4 + 32 * 8 + 64 * 4) + 2 * 16 * 4;
+// The dynamic part at most: outputs of 16 heads of 256 by 8 waves, or a chunk's page numbers.
+constexpr size_t kMostLds = kWavesWhole * 16 * (256 + 4) * sizeof(float);
+static_assert(kMostLds >= (kChunkMax + 2) * sizeof(int), "launch attribute");
 
 // The binary32 number next to another one on the side of 0; 0 for 0 (but not for -0).
 __device__ __forceinline__ float below(float x) {
@@ -597,7 +600,8 @@ static hipError_t go(const AttnArgs& a, hipStream_t st) {
   const dim3 grid = A.block ? folded(ids) : dim3(a.n_kv, a.n_seqs, a.n_splits);
   hipError_t e = hipSuccess;
   auto run = [&](auto kernel) {
-    if (lds + kStaticLds > 65536) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    // The limit is the kernel's, not the call's: always the most, so that no thread lowers another's.
+    if (lds + kStaticLds > 65536) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds);
     if (e == hipSuccess) kernel<<<grid, 64 * a.waves, lds, st>>>(A);
     if (e == hipSuccess) e = hipGetLastError();
   };

@@ -95,3 +95,10 @@ def test_adapters_of_every_rank_set_one_limit(notes_of):
     calls = [dict(op="adapters", dt=dt, y=y, rank=rank, rows=300, d_out=d_out)
              for dt in (0, 1) for y in (0, 1, 2) for d_out in (64, 63) for rank in (160, 256, 8, 192, 224, 161)]
     assert set(check_limits(notes_of(calls)).values()) == {82944, 115712}
+
+
+def test_attention_of_every_size_sets_one_limit(notes_of):
+    calls = [dict(op="attention", dt=dt, dim=dim, heads=heads, page=page, seqs=seqs, length=length)
+             for dt in (0, 1) for dim in (256, 248, 232) for heads in (16, 15) for page, seqs, length in
+             ((8, 2, 256), (1, 2048, 36000), (1, 4000, 20000), (1, 1, 256))]
+    check_limits(notes_of(calls))
