@@ -700,6 +700,7 @@ typedef struct {
  *   index  int32 [n_rows], device memory, in any order
  *   base   [n_rows][d_out] y_dtype in {F16, BF16, F32}, row stride base_stride; what aqmb_gemv or aqmb_w4_gemv gave
  *   out    the same type, row stride out_stride
+ * Where x or a starts at an odd element, the two bytes before it, in the same aligned four, are read too (and not used).
  * out may be base (same stride; then rows without an adapter are not touched); no other overlap. A row's sums do not depend on the
  * other rows' contents, only on their number.
  * workspace: aqmb_adapters_workspace_bytes bytes of device memory, 16-byte aligned, written by the call (calls that

@@ -4,8 +4,10 @@
 // out = base + B_n (s_n t). Rows that share an adapter are the columns of matrix instructions, 16 each, with 16 rows of A
 // or outputs of B: each row meets only its own adapter, in any order of the indexes, without atomics on results. Few rows:
 // every wave finds its 16 by votes over 64 rows' indexes; the adapters' bytes and the latency of two launches bound them
-// (one row, rank 16, 4096 x 4096: 3.5 + 4.9 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base
-// and out (8192 rows, rank 32, 4096 x 4096: sort 10 us, t 14.5 us, 4.6 TB/s, the outputs 34 us, 4.0 TB/s).
+// (one row, rank 16, 4096 x 4096: 3.5 + 4.9 us). Many: a first launch sorts the rows by adapter into tiles of 64; bound by x, base,
+// out and t, which all eight L2s read, since neighbouring workgroups take other outputs of the same rows (8192 rows, 4096 x
+// 4096, rank 32: sort 10 us, t 14.3 us, 4.7 TB/s, the outputs 34 us, 165 MB at 4.9 TB/s, 28 of them t; rank 128: 9.9, 31
+// and 83 us, the last 263 MB at 3.2 TB/s, 118 of them t).
 #include "device.h"
 #include "ops.h"
 
@@ -68,8 +70,8 @@ __device__ __forceinline__ u32x4_t moved8(u32x4_t v, int k, int n) {
 }
 
 // Eight values from p on, loaded and then put together. A 16-byte load that does not start at a multiple of 4 bytes takes
-// several times as long, so where such addresses come (kOdd) it starts 2 bytes lower, inside the same aligned 4 bytes as *p,
-// and the last value has a load of its own.
+// several times as long, so where such addresses come (kOdd) it starts 2 bytes lower, inside the same aligned 4 bytes as *p
+// (of a tensor's first row these are the two bytes before the tensor; they are shifted out), and the last value has a load of its own.
 template <bool kOdd> struct Loaded8 {
   u32x4_t v;
   __device__ __forceinline__ void load(const uint16_t* p) { v = load8(p, 0u); }
@@ -531,7 +533,7 @@ __device__ __forceinline__ void add_y(Eight<kWide>& r, const f32x4_t (&d)[8], in
 
 // Few rows: blockIdx.y is the row that a tile starts with, each of four waves takes 128 outputs. Lane (q, c) of 4 x 16 has outputs 8 c .. 8 c + 7 of 128 of rows 4 q .. 4 q + 3: a quarter of the wave reads and
 // writes 256 bytes of a row at once (with lanes side by side on different rows every lane was an access of its own to the
-// vector cache, which bound the kernel: 8192 rows of 4096 outputs 45 us). Bound by latency (4.9 us) or the adapters' bytes
+// vector cache, which bound the kernel). Bound by latency (4.9 us) or the adapters' bytes
 // (32 rows of some 25 adapters of rank 64, 11008 outputs: 13 us).
 template <int DT, bool kWide, bool kEights>
 __global__ __launch_bounds__(256, kWide || !kEights ? 2 : 3) void expand_few(AdapterArgs a) {
@@ -733,7 +735,8 @@ __global__ __launch_bounds__(256, kWide || !kEights ? 3 : 4) void expand_many(Ad
 }
 
 // Many rows sorted by adapter (those without one last), and cut into tiles of up to 64 (adapter, first, count): one workgroup
-// counts, adds up and places. Rows of one adapter come in any order, which nothing depends on.
+// counts, adds up and places. Rows of one adapter come in any order, which nothing depends on. 8192 rows 10 us; above, the
+// indexes are read twice: 65536 rows in spans of 8 adapters 66 us, of 64 in any order 74.
 __global__ __launch_bounds__(1024) void sort_kernel(AdapterArgs a) {
   __shared__ int bins[kMaxAdapters + 1], sums[2][16];
   constexpr int kEach = 8;       // rows of a thread at once
@@ -824,8 +827,11 @@ hipError_t go_shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t st)
     const dim3 grid(a.n_rows, p.splits, (a.ad.rank + 63) / 64);
     // Rows at addresses that are no multiples of 4 bytes.
     const bool odd = ((uintptr_t)a.x | (uintptr_t)a.ad.a) % 4 || a.x_stride % 2 || a.ad.d_in % 2;
-    // Most workgroups have no tile and end at once; where few have one, two of them would share a unit while others are idle
-    // (150 rows, 4 adapters of rank 64, 4096 x 4096: 19.5 us a call, one a unit 16.8; 64 adapters: 34.5 and 39.3).
+    // Most workgroups have no tile and end at once; where few have one, two of them would share a unit while others are idle.
+    // 4096 x 4096, shared and one a unit: 48 workgroups with a tile at least (150 rows, 4 adapters of rank 64) 21.2 us a call and
+    // 18.1, 96 (8 adapters) 21.4 and 18.1, 144 (12) 21.5 and 21.7; 64 (250 rows, 4 of rank 32) 15.4 and 14.3, 96 (6) 15.2 and 15.0,
+    // 160 (10) 15.0 and 16.5; 128 (128 rows, 16 of rank 16) 11.5 and 12.3; 104 (40 rows, 13 of
+    // rank 128, 11008 outputs) 30.4 and 26.2. Else up to 64 rows the same.
     const int groups = (a.n_rows + kRows - 1) / kRows * min(a.ad.n_adapters, kRows);
     const bool one = max(a.n_rows / 16, min(groups, a.n_rows)) * (int)(grid.y * grid.z) <= 100;
     const auto kernel = odd ? one ? shrink_few<DT, kMost, true, true> : shrink_few<DT, kMost, true, false>

@@ -384,7 +384,10 @@ hipError_t go(const LogProbArgs& a, hipStream_t st) {
   const dim3 grid(a.rows, a.splits);
   // A wave's work has to be short where few rows wait for it: one load a tile then (the code of a tile is unrolled, and is
   // fetched for one use; one row of 32000 with 5 top values 6.4 us, with four loads 8.5). Many short rows: a wave each, no joining
-  // (4000 rows of 2000: 12 us against 22 by four waves; 4096 rows of 32000 with 20 top values 103 and 118, 1024 rows 41 and 31).
+  // (4000 rows of 2000: 12 us against 22 by four waves; 4096 rows of 32000 with 20 top values 103 and 118, 1024 rows 41 and 31;
+  // 16 rows of 131072 in 64 parts of 4 loads of 16 bits 10.1 and 12.9, of 8 in binary32 12.6 and 12.6; 2000 rows of 8000 21.4 and 26.7;
+  // 4200 of 16000 62 and 78). The bounds by their number are not the best everywhere: 1100 rows of 8000 20.2 and 18.2, 4000 of 16000 75 by
+  // four waves and 60 by one, and rows without top values are up to a fifth slower by one (1100 of 8000 9.3 and 7.6, 4200 of 16000 33 and 29).
   const int64_t pieces = ((int64_t)a.chunk + kPiece<DT> - 1) / kPiece<DT>, groups = (int64_t)a.rows * a.splits;
   const int variant = pieces <= 2 ? 0 : pieces <= (groups >= 4096 ? 64 : groups >= 1024 ? 16 : 0) ? 1 : pieces <= 16 ? 2 : 3;
   if (a.n_top) {

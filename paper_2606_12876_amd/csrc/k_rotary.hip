@@ -262,7 +262,9 @@ hipError_t launch_rotary(const RotaryArgs& r, aqmb_dtype dtype, hipStream_t st) 
   const int lanes = r.head_dim <= 64 ? 4 : r.head_dim <= 128 ? 8 : 16, at_once = 256 / lanes;
   // Few tokens: a head per lane group and workgroups over the heads, short code. Many: all heads of some tokens in a
   // workgroup, about kMany per lane group. 40 heads of 128: 1 token 2.3 us against 2.9, 512 tokens 3.6 and 4.8, 4096 14.9 and
-  // 15.4, 8192 the same; 16 heads of 64: 2048 tokens 3.8 and 4.9, 4096 6.3 and 5.8, 32768 35.4 and 32.8.
+  // 15.4, 8192 the same; 16 heads of 64: 2048 tokens 3.8 and 4.9, 4096 6.3 and 5.8, 32768 35.4 and 32.8. More heads of a token than a workgroup
+  // takes at once go the way of few at any number of tokens: 136 heads of 128, 1024 tokens 13.9 and 13.3, 4096 48.5 and 52; 68 of 256
+  // 14.2 and 13.6, 48.5 and 52.
   const bool few = (int64_t)r.n_tokens * a.n_total < (int64_t)512 * kMany * at_once || a.n_total > kMany * at_once;
   a.tokens = few ? 1 : kMany * at_once / a.n_total < kTokens ? kMany * at_once / a.n_total : kTokens;
   a.heads = few && a.n_total > at_once ? at_once : a.n_total;
