@@ -695,8 +695,8 @@ typedef struct {
  * out[i] = base[i] + scales[n] * B_n (A_n x[i]) with n = index[i]; out[i] = base[i] where index[i] is outside
  * [0, n_adapters) (-1: a request without an adapter). Products are exact and summed in binary32 on the matrix cores;
  * A_n x times the scale enters the second product as two (F16, 22 bits of the row's largest) or three (BF16, 24 bits)
- * 16-bit parts; one rounding to y_dtype. A row whose A_n x holds a value that is not finite (BF16:
- * or is above 3.38e38 times the scale, where 16 bits end) gives values that are not finite.
+ * 16-bit parts; one rounding to y_dtype. A row whose A_n x holds a value that is not finite, or
+ * with BF16 one that times the scale is above 3.38e38, where 16 bits end, gives values that are not finite.
  *   x      [n_rows][d_in] of the adapters' dtype, row stride x_stride
  *   index  int32 [n_rows], device memory, in any order
  *   base   [n_rows][d_out] y_dtype in {F16, BF16, F32}, row stride base_stride; what aqmb_gemv or aqmb_w4_gemv gave
